@@ -291,6 +291,56 @@ int pacer_linear(const void *x, const void *w, float *y, int rows, int N, int K,
 #define PACER_LINEAR_STATIC_BYTES (4u << 20)
 int pacer_linear_static(const void *x, const void *w, float *y, int rows, int N, int K, void *cuda_stream);
 
+/* Operators on rows of logits: what a server returns beside the tokens, what a scoring program needs, and the loss that
+ * trains a draft model towards its target.  logits: device, [rows][vocab] of type dtype (PACER_F32 / _BF16 / _F16) with ld >=
+ * vocab elements from row to row (any ld and any element-aligned address; whole 16-byte pieces are moved at a time where rows of
+ * input and output lie alike modulo 16 bytes).  rows <= 2^24, vocab <= 2^21; rows = 0 does nothing.  All other arrays are device,
+ * contiguous, f32 or int32 as declared.  Sums and statistics are fp32.  A logit of -inf has probability 0; a row of -inf only has lse -inf,
+ * every log probability -inf, entropy 0 and gradient 0; a NaN or +inf logit makes the results of its row NaN.  The calls enqueue
+ * one kernel on `cuda_stream` (of the current device), use no workspace and no atomics on global memory: they give the same bits every time,
+ * may overlap and may be captured into a graph. */
+enum { PACER_F32 = 0, PACER_BF16 = 1, PACER_F16 = 2 };
+#define PACER_MAX_TOP 128
+#define PACER_MAX_DISTILL_K 256
+
+/* Log probabilities of given tokens, with entropy and the best alternatives of every row:
+ *   lse = log sum_v exp(z_v), logp = z[token] - lse, entropy = -sum_v p_v log p_v (nats).
+ * tokens: int32 [rows] or NULL; a token outside [0, vocab) (-1, say) names nothing: logp 0.  top (0 .. min(PACER_MAX_TOP, vocab)):
+ * top_ids int32 [rows][top] and top_logp f32 [rows][top] are the best tokens in order: larger logit first, of equal ones the
+ * lower id, NaN last.  Every output may be NULL. */
+int pacer_logprobs(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens, int top, float *logp,
+                   float *entropy, float *lse, int32_t *top_ids, float *top_logp, void *cuda_stream);
+
+/* Gradient of the above: dlogits[r][v] = g_logp[r] ([v = token] - p_v) + g_lse[r] p_v - g_entropy[r] p_v (log p_v + entropy[r]),
+ * in the logits' type.  lse and entropy: as pacer_logprobs left them.  Each of g_logp, g_entropy, g_lse may be NULL, not all
+ * three; tokens may be NULL where g_logp is, entropy where g_entropy is.  A row whose token names nothing has no g_logp term.
+ * dlogits may be the logits themselves (same ld). */
+int pacer_logprobs_backward(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens, const float *lse,
+                            const float *entropy, const float *g_logp, const float *g_entropy, const float *g_lse, void *dlogits,
+                            int64_t ld_dlogits, void *cuda_stream);
+
+/* Distillation from a teacher's top logits.  Per row, with p = softmax(z / temperature) of the student's whole row and
+ * q the teacher's distribution over its k listed tokens:
+ *   loss = sum_k q_k (log q_k - log p[ids_k])  [ + q_t (log q_t - log p_t) ]
+ * ids: int32 [rows][k], 1 <= k <= PACER_MAX_DISTILL_K; an id outside [0, vocab) is no entry, an id listed twice counts twice.
+ * teacher: [rows][k] logits (or log probabilities) of type teacher_dtype.  teacher_lse NULL: q = softmax(teacher / temperature)
+ * over the list.  teacher_lse f32 [rows]: the log-sum-exp of the teacher's whole row AT THIS TEMPERATURE;
+ * q_k = exp(teacher_k / temperature - teacher_lse), and all tokens outside the list form one further class with
+ * q_t = max(0, 1 - sum_k q_k), p_t the student's mass outside the list.
+ * A row without entries has loss 0 and gradient 0.  loss, lse (of z / temperature), tail_lse (the log-sum-exp of z / temperature
+ * over the tokens outside the list; only with teacher_lse): f32 [rows], each may be NULL.
+ * dlogits (may be NULL): weight[row] (f32 [rows]) times the gradient of loss[row], in the logits' type, in the same pass; it may be
+ * the logits themselves (same ld).  Nothing is multiplied by temperature^2. */
+int pacer_distill(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *ids, const void *teacher,
+                  int teacher_dtype, int k, const float *teacher_lse, float temperature, float *loss, float *lse, float *tail_lse,
+                  const float *weight, void *dlogits, int64_t ld_dlogits, void *cuda_stream);
+
+/* The gradient alone, from the lse and tail_lse (with teacher_lse) of a pacer_distill call with the same arguments:
+ * dlogits = g_loss[row] times the gradient of loss[row]. */
+int pacer_distill_backward(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *ids, const void *teacher,
+                           int teacher_dtype, int k, const float *teacher_lse, float temperature, const float *lse,
+                           const float *tail_lse, const float *g_loss, void *dlogits, int64_t ld_dlogits, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -96,6 +96,13 @@ _lib.pacer_linear_scratch_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
 _lib.pacer_linear.argtypes = [_P, _P, _P, C.c_int, C.c_int, C.c_int, _P, C.c_size_t, _P]
 _lib.pacer_linear_static.argtypes = [_P, _P, _P, C.c_int, C.c_int, C.c_int, _P]
 PACER_LINEAR_STATIC_BYTES = 4 << 20
+_I, _L, _F = C.c_int, C.c_int64, C.c_float
+_lib.pacer_logprobs.argtypes = [_P, _I, _L, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P]
+_lib.pacer_logprobs_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _L, _P]
+_lib.pacer_distill.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P]
+_lib.pacer_distill_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _L, _P]
+PACER_F32, PACER_BF16, PACER_F16 = 0, 1, 2
+_DTYPES = {torch.float32: PACER_F32, torch.bfloat16: PACER_BF16, torch.float16: PACER_F16}
 
 
 class PacerError(RuntimeError):
@@ -108,7 +115,8 @@ def exported_symbols():
             "pacer_load_weights", "pacer_prefill", "pacer_draft_step", "pacer_preverify", "pacer_verify",
             "pacer_accept_rollback", "pacer_read_state", "pacer_read_buffer", "pacer_generate", "pacer_generate_sched",
             "pacer_generate_ar", "pacer_debug_set_device_status",
-            "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static"]
+            "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
+            "pacer_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward"]
 
 
 def _model_cfg(s) -> ModelCfg:
@@ -348,6 +356,129 @@ def pacer_linear_static(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor) -> 
                                       torch.cuda.current_stream(x.device).cuda_stream)
     if rc != 0:
         raise PacerError(f"pacer_linear_static: {_lib.pacer_strerror(rc).decode()}: {_lib.pacer_last_error(None).decode()}")
+    return out
+
+
+# ----------------------------------------------------------------------------- operators on rows of logits
+
+
+def _rows(t: torch.Tensor, name: str = "logits") -> torch.Tensor:
+    """`t` as the library takes it: on the GPU, [rows][vocab], one of three types, elements of a row side by side."""
+    assert t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES, f"{name}: f32, bf16 or f16 [rows][vocab] on the GPU"
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
+def _vec(t: Optional[torch.Tensor], name: str, like: torch.Tensor, dtype, *more) -> Optional[torch.Tensor]:
+    """A side input: [rows] or [rows][more], of the given type, contiguous, beside the logits.  None stays None."""
+    if t is None:
+        return None
+    assert t.device == like.device and t.dtype == dtype and tuple(t.shape) == (like.shape[0], *more), \
+        f"{name}: {dtype} of shape {(like.shape[0], *more)} on {like.device}"
+    return t.contiguous()
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _gradient_like(z: torch.Tensor) -> torch.Tensor:
+    """Rows that lie as the logits' do (so that they are written 16 bytes at a time), where those are padded by little."""
+    rows, vocab = z.shape
+    if vocab < z.stride(0) <= vocab + 1024 and rows > 1:
+        return torch.empty(rows, z.stride(0), dtype=z.dtype, device=z.device)[:, :vocab]
+    return torch.empty(rows, vocab, dtype=z.dtype, device=z.device)
+
+
+def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        return _gradient_like(z)
+    assert out.device == z.device and out.dtype == z.dtype and out.shape == z.shape and out.stride(1) == 1, "out: like the logits"
+    return out
+
+
+def _call(name: str, like: torch.Tensor, *args):
+    """The C entry point on the tensors' device and torch's current stream there."""
+    dev = like.device
+    with contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev):
+        rc = getattr(_lib, name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc != 0:
+        raise PacerError(f"{name}: {_lib.pacer_strerror(rc).decode()}: {_lib.pacer_last_error(None).decode()}")
+
+
+def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
+    """Log probabilities of given tokens under rows of logits [rows][vocab] (f32, bf16 or f16): returns
+    (logp [rows], entropy [rows], lse [rows], top_ids int32 [rows][top], top_logp [rows][top]).  tokens int32 [rows]; one outside
+    the vocabulary (-1, say) has logp 0.  Alternatives: larger logit first, of equal ones the lower id.  No gradient: see
+    pacer_logprobs_backward, and losses.token_logprobs for autograd."""
+    z = _rows(logits)
+    tokens = _vec(tokens, "tokens", z, torch.int32)
+    rows, vocab = z.shape
+    logp, entropy, lse = torch.empty(3, rows, dtype=torch.float32, device=z.device).unbind(0)
+    ids = torch.empty(rows, max(top, 0), dtype=torch.int32, device=z.device)
+    top_logp = torch.empty(rows, max(top, 0), dtype=torch.float32, device=z.device)
+    _call("pacer_logprobs", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), vocab), rows, vocab, _ptr(tokens), top, logp.data_ptr(),
+          entropy.data_ptr(), lse.data_ptr(), ids.data_ptr(), top_logp.data_ptr())
+    return logp, entropy, lse, ids, top_logp
+
+
+def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, grad_lse=None, out=None):
+    """The gradient of pacer_logprobs' logp, entropy and lse with respect to the logits, in their type.  Each incoming gradient
+    (f32 [rows]) may be None; `out` may be the logits themselves."""
+    z = _rows(logits)
+    f32 = torch.float32
+    tokens, lse, entropy = _vec(tokens, "tokens", z, torch.int32), _vec(lse, "lse", z, f32), _vec(entropy, "entropy", z, f32)
+    gl, gh, gs = _vec(grad_logp, "grad_logp", z, f32), _vec(grad_entropy, "grad_entropy", z, f32), _vec(grad_lse, "grad_lse", z, f32)
+    out = _out_like(z, out)
+    _call("pacer_logprobs_backward", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], _ptr(tokens),
+          _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), out.data_ptr(), max(out.stride(0), z.shape[1]))
+    return out
+
+
+def _teacher(z, ids, teacher, teacher_lse):
+    k = ids.shape[1] if ids.dim() == 2 else -1
+    ids = _vec(ids, "ids", z, torch.int32, k)
+    assert teacher.dtype in _DTYPES, "teacher: f32, bf16 or f16"
+    return ids, _vec(teacher, "teacher", z, teacher.dtype, k), _vec(teacher_lse, "teacher_lse", z, torch.float32), k
+
+
+def pacer_distill(logits, ids, teacher, temperature: float = 1.0, teacher_lse=None):
+    """Distillation from a teacher's top logits: per row KL(q || p) with p = softmax(logits / temperature) and q over the listed
+    tokens ids int32 [rows][k] with logits teacher [rows][k] (f32, bf16 or f16), renormalised; with teacher_lse f32 [rows] (the
+    teacher's log-sum-exp over its whole row, at this temperature) the tokens outside the list are one further class.  An id
+    outside the vocabulary is no entry.  Returns (loss [rows], lse [rows], tail_lse [rows] or None)."""
+    z = _rows(logits)
+    ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
+    loss, lse, tail = torch.empty(3, z.shape[0], dtype=torch.float32, device=z.device).unbind(0)
+    tail = None if teacher_lse is None else tail
+    _call("pacer_distill", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
+          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), lse.data_ptr(), _ptr(tail), None, None,
+          0)
+    return loss, lse, tail
+
+
+def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, teacher_lse=None, out=None):
+    """pacer_distill's loss [rows] and, in the same pass, weight[row] times its gradient with respect to the logits (in their
+    type; `out` may be the logits themselves): (loss, dlogits)."""
+    z = _rows(logits)
+    ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
+    weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
+    loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
+    _call("pacer_distill", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
+          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, weight.data_ptr(),
+          out.data_ptr(), max(out.stride(0), z.shape[1]))
+    return loss, out
+
+
+def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, temperature: float = 1.0, teacher_lse=None, out=None):
+    """The gradient of pacer_distill's loss from what that call left (lse, tail_lse) and f32 [rows] grad_loss."""
+    z = _rows(logits)
+    ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
+    f32 = torch.float32
+    lse, tail_lse, grad_loss = _vec(lse, "lse", z, f32), _vec(tail_lse, "tail_lse", z, f32), _vec(grad_loss, "grad_loss", z, f32)
+    out = _out_like(z, out)
+    _call("pacer_distill_backward", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
+          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
+          out.data_ptr(), max(out.stride(0), z.shape[1]))
     return out
 
 

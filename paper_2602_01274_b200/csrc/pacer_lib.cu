@@ -17,6 +17,7 @@
 #include "fwd_few.h"
 #include "fwd_kernel.cuh"
 #include "gemm.cuh"
+#include "logits.h"
 #include "prefill.h"
 
 struct pacer_ctx {
@@ -944,5 +945,101 @@ extern "C" int pacer_linear_static(const void *x, const void *w, float *y, int r
         return fail(nullptr, PACER_ENOMEM, "pacer_linear_static: shape needs more than PACER_LINEAR_STATIC_BYTES of scratch");
     if ((uintptr_t)w & 15) return fail(nullptr, PACER_EINVAL, "pacer_linear_static: misaligned pointer");
     CK(lin_run((const bf16 *)x, (const bf16 *)w, y, rows, N, K, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+// ------------------------------------------------------------------ operators on rows of logits
+
+// NULL if the rows can be worked on, else what is wrong with them.
+static const char *bad_rows(const void *z, int dtype, int64_t ld, int rows, int vocab) {
+    if (dtype != PACER_F32 && dtype != PACER_BF16 && dtype != PACER_F16) return "unknown type of logits";
+    if (rows < 0 || rows > lg::MAX_ROWS) return "rows out of range";
+    if (vocab < 1 || vocab > lg::MAX_VOCAB) return "vocab out of range";
+    if (ld < vocab) return "ld is less than vocab";
+    if (!z && rows) return "logits is null";
+    if ((uintptr_t)z % (dtype == PACER_F32 ? 4 : 2)) return "misaligned logits";
+    return nullptr;
+}
+static const char *bad_grad(const void *z, int dtype, int64_t ld, int rows, int vocab, const void *dz, int64_t ld_dz) {
+    if (ld_dz < vocab) return "ld_dlogits is less than vocab";
+    if (!dz && rows) return "dlogits is null";
+    if ((uintptr_t)dz % (dtype == PACER_F32 ? 4 : 2)) return "misaligned dlogits";
+    const int64_t e = dtype == PACER_F32 ? 4 : 2;
+    const uintptr_t z0 = (uintptr_t)z, d0 = (uintptr_t)dz;
+    const uintptr_t z1 = z0 + e * ((int64_t)(rows - 1) * ld + vocab), d1 = d0 + e * ((int64_t)(rows - 1) * ld_dz + vocab);
+    if (rows && z0 < d1 && d0 < z1 && !(z0 == d0 && ld == ld_dz)) return "dlogits overlaps the logits";
+    return nullptr;
+}
+#define REFUSE_IF(cond, what) \
+    if (cond) return fail(nullptr, PACER_EINVAL, std::string(__func__) + ": " + what)
+#define REFUSE_BAD(call) \
+    if (const char *bad_ = call) return fail(nullptr, PACER_EINVAL, std::string(__func__) + ": " + bad_)
+
+extern "C" int pacer_logprobs(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens, int top, float *logp,
+                              float *entropy, float *lse, int32_t *top_ids, float *top_logp, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_rows(logits, dtype, ld, rows, vocab));
+    REFUSE_IF(top < 0 || top > PACER_MAX_TOP || top > vocab, "top out of range");
+    REFUSE_IF(logp && !tokens && rows, "logp without tokens");
+    if (!rows) return PACER_OK;
+    if (!top_ids && !top_logp) top = 0;
+    CK(lg::logprobs({logits, dtype, ld, rows, vocab}, tokens, {}, {logp, entropy, lse, top, top_ids, top_logp}, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+extern "C" int pacer_logprobs_backward(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens,
+                                       const float *lse, const float *entropy, const float *g_logp, const float *g_entropy,
+                                       const float *g_lse, void *dlogits, int64_t ld_dlogits, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_rows(logits, dtype, ld, rows, vocab));
+    REFUSE_BAD(bad_grad(logits, dtype, ld, rows, vocab, dlogits, ld_dlogits));
+    if (!rows) return PACER_OK;
+    REFUSE_IF(!lse, "lse is null");
+    REFUSE_IF(!g_logp && !g_entropy && !g_lse, "no gradient comes in");
+    REFUSE_IF(g_logp && !tokens, "g_logp without tokens");
+    REFUSE_IF(g_entropy && !entropy, "g_entropy without entropy");
+    CK(lg::logprobs_backward({logits, dtype, ld, rows, vocab}, tokens, lse, entropy, g_logp, g_entropy, g_lse, dlogits, ld_dlogits,
+                             (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+static const char *bad_teacher(int rows, const int32_t *ids, const void *teacher, int teacher_dtype, int k, float temperature) {
+    if (k < 1 || k > PACER_MAX_DISTILL_K) return "k out of range";
+    if (teacher_dtype != PACER_F32 && teacher_dtype != PACER_BF16 && teacher_dtype != PACER_F16) return "unknown type of teacher";
+    if (!(temperature >= 1e-3f && temperature <= 1e3f)) return "temperature out of range";
+    if (rows && (!ids || !teacher)) return "ids or teacher is null";
+    return nullptr;
+}
+
+extern "C" int pacer_distill(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *ids, const void *teacher,
+                             int teacher_dtype, int k, const float *teacher_lse, float temperature, float *loss, float *lse,
+                             float *tail_lse, const float *weight, void *dlogits, int64_t ld_dlogits, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_rows(logits, dtype, ld, rows, vocab));
+    REFUSE_BAD(bad_teacher(rows, ids, teacher, teacher_dtype, k, temperature));
+    REFUSE_IF(tail_lse && !teacher_lse, "tail_lse without teacher_lse");
+    if (dlogits) {
+        REFUSE_BAD(bad_grad(logits, dtype, ld, rows, vocab, dlogits, ld_dlogits));
+        REFUSE_IF(rows && !weight, "dlogits without weight");
+    }
+    if (!rows) return PACER_OK;
+    CK(lg::distill({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, 1.f / temperature}, loss, lse, tail_lse,
+                   weight, dlogits, ld_dlogits, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+extern "C" int pacer_distill_backward(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *ids,
+                                      const void *teacher, int teacher_dtype, int k, const float *teacher_lse, float temperature,
+                                      const float *lse, const float *tail_lse, const float *g_loss, void *dlogits, int64_t ld_dlogits,
+                                      void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_rows(logits, dtype, ld, rows, vocab));
+    REFUSE_BAD(bad_teacher(rows, ids, teacher, teacher_dtype, k, temperature));
+    REFUSE_BAD(bad_grad(logits, dtype, ld, rows, vocab, dlogits, ld_dlogits));
+    if (!rows) return PACER_OK;
+    REFUSE_IF(!lse || !g_loss, "lse or g_loss is null");
+    REFUSE_IF(teacher_lse && !tail_lse, "teacher_lse without tail_lse");
+    CK(lg::distill_backward({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, 1.f / temperature}, lse, tail_lse,
+                            g_loss, dlogits, ld_dlogits, (cudaStream_t)cuda_stream));
     return PACER_OK;
 }
