@@ -341,6 +341,21 @@ int pacer_distill_backward(const void *logits, int dtype, int64_t ld, int rows, 
                            int teacher_dtype, int k, const float *teacher_lse, float temperature, const float *lse,
                            const float *tail_lse, const float *g_loss, void *dlogits, int64_t ld_dlogits, void *cuda_stream);
 
+/* The LM head fused with the scoring: z = hidden head^T (+ bias on the token bias_ids[r] of row r), of which only
+ * lse, logp (of tokens[r]) and entropy leave the chip, as pacer_logprobs defines them.  The logits are never written.
+ * hidden: device bf16 [rows][d] (final-norm output, rounded), head: device bf16 [vocab][d]; ld_hidden and ld_head elements from
+ * row to row; both addresses 16-byte aligned, d and both strides multiples of 8, d <= 65536; rows <= 2^20, vocab <= 2^21.  Plain
+ * bf16 products with fp32 sums on tcgen05.  tokens: device int32 [rows] or NULL (then logp too); bias_ids: device int32
+ * [rows] or NULL, an id outside the vocabulary adds nothing.  logp, entropy, lse: device f32 [rows], each may be NULL.
+ * scratch: device, 256-byte aligned, at least pacer_head_logprobs_scratch_bytes(rows, vocab) bytes, in use until the call's kernels
+ * have run (two calls that may overlap need one each).  Inputs must be finite: infinities and NaN make results NaN or infinite;
+ * so does, for its rows, a wait inside the kernel that ran out.  Enqueues two kernels; may be captured into a graph (not as the
+ * first call on a device: it sets the kernel's shared-memory attribute). */
+size_t pacer_head_logprobs_scratch_bytes(int rows, int vocab);
+int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
+                        const int32_t *tokens, const int32_t *bias_ids, float bias, float *logp, float *entropy, float *lse,
+                        void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

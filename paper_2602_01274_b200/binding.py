@@ -101,6 +101,9 @@ _lib.pacer_logprobs.argtypes = [_P, _I, _L, _I, _I, _P, _I, _P, _P, _P, _P, _P, 
 _lib.pacer_logprobs_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _L, _P]
 _lib.pacer_distill.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P]
 _lib.pacer_distill_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _L, _P]
+_lib.pacer_head_logprobs_scratch_bytes.restype = C.c_size_t
+_lib.pacer_head_logprobs_scratch_bytes.argtypes = [_I, _I]
+_lib.pacer_head_logprobs.argtypes = [_P, _L, _P, _L, _I, _I, _I, _P, _P, _F, _P, _P, _P, _P, C.c_size_t, _P]
 PACER_F32, PACER_BF16, PACER_F16 = 0, 1, 2
 _DTYPES = {torch.float32: PACER_F32, torch.bfloat16: PACER_BF16, torch.float16: PACER_F16}
 
@@ -116,7 +119,8 @@ def exported_symbols():
             "pacer_accept_rollback", "pacer_read_state", "pacer_read_buffer", "pacer_generate", "pacer_generate_sched",
             "pacer_generate_ar", "pacer_debug_set_device_status",
             "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
-            "pacer_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward"]
+            "pacer_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
+            "pacer_head_logprobs_scratch_bytes", "pacer_head_logprobs"]
 
 
 def _model_cfg(s) -> ModelCfg:
@@ -480,6 +484,23 @@ def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, tempe
           teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
           out.data_ptr(), max(out.stride(0), z.shape[1]))
     return out
+
+
+def pacer_head_logprobs(hidden, head, tokens, bias_ids=None, bias: float = 0.0):
+    """pacer_logprobs of the rows hidden @ head.T without writing those logits: hidden bf16 [rows][d], head bf16 [vocab][d]
+    (rows of 16-byte multiples), tokens int32 [rows]; bias_ids int32 [rows]: tokens whose logit gets `bias` added.
+    Returns (logp [rows], entropy [rows], lse [rows])."""
+    h, w = _rows(hidden, "hidden"), _rows(head, "head")
+    assert h.dtype == w.dtype == torch.bfloat16 and h.device == w.device and h.shape[1] == w.shape[1], "bf16 [rows][d] and [vocab][d]"
+    tokens, bias_ids = _vec(tokens, "tokens", h, torch.int32), _vec(bias_ids, "bias_ids", h, torch.int32)
+    rows, d = h.shape
+    vocab = w.shape[0]
+    nbytes = _lib.pacer_head_logprobs_scratch_bytes(rows, vocab)
+    logp, entropy, lse = torch.empty(3, rows, dtype=torch.float32, device=h.device).unbind(0)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device)      # (torch aligns an allocation to 512 bytes)
+    _call("pacer_head_logprobs", h, h.data_ptr(), max(h.stride(0), d), w.data_ptr(), max(w.stride(0), d), rows, vocab, d, _ptr(tokens),
+          _ptr(bias_ids), bias, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), scratch.data_ptr(), nbytes)
+    return logp, entropy, lse
 
 
 def load_pair(ctx: Context, pair: dict):

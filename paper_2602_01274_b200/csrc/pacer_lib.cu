@@ -17,6 +17,7 @@
 #include "fwd_few.h"
 #include "fwd_kernel.cuh"
 #include "gemm.cuh"
+#include "head_score.h"
 #include "logits.h"
 #include "prefill.h"
 
@@ -1041,5 +1042,30 @@ extern "C" int pacer_distill_backward(const void *logits, int dtype, int64_t ld,
     REFUSE_IF(teacher_lse && !tail_lse, "teacher_lse without tail_lse");
     CK(lg::distill_backward({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, 1.f / temperature}, lse, tail_lse,
                             g_loss, dlogits, ld_dlogits, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+extern "C" size_t pacer_head_logprobs_scratch_bytes(int rows, int vocab) {
+    if (rows < 1 || rows > hs::MAX_ROWS || vocab < 1 || vocab > lg::MAX_VOCAB) return 0;
+    return hs::scratch_bytes(rows, vocab);
+}
+
+extern "C" int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
+                                   const int32_t *tokens, const int32_t *bias_ids, float bias, float *logp, float *entropy, float *lse,
+                                   void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_IF(rows < 0 || rows > hs::MAX_ROWS, "rows out of range");
+    REFUSE_IF(vocab < 1 || vocab > lg::MAX_VOCAB, "vocab out of range");
+    REFUSE_IF(d < 8 || d > hs::MAX_D || d % 8, "d out of range or not a multiple of 8");
+    REFUSE_IF(ld_hidden < d || ld_hidden % 8 || ld_hidden >> 38 || ld_head < d || ld_head % 8 || ld_head >> 38, "bad row stride");
+    if (!rows) return PACER_OK;
+    REFUSE_IF(!hidden || !head || !scratch, "hidden, head or scratch is null");
+    REFUSE_IF(((uintptr_t)hidden | (uintptr_t)head) & 15 || (uintptr_t)scratch & 255, "misaligned pointer");
+    REFUSE_IF(logp && !tokens, "logp without tokens");
+    if (scratch_bytes < hs::scratch_bytes(rows, vocab)) return fail(nullptr, PACER_ENOMEM, "pacer_head_logprobs: scratch too small");
+    bool no_maps = false;
+    CK(hs::run({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, logp, entropy, lse}, scratch, sm_count_or_default(),
+               (cudaStream_t)cuda_stream, &no_maps));
+    if (no_maps) return fail(nullptr, PACER_EUNSUPPORTED, "pacer_head_logprobs: the driver describes no tensor copies");
     return PACER_OK;
 }

@@ -85,3 +85,29 @@ def test_no_rows_is_no_work(lib):
     assert lib.pacer_logprobs_backward(*rows(z=None, rows=0), None, None, None, None, None, None, None, 100, None) == 0
     assert lib.pacer_distill(*rows(z=None, rows=0), None, None, 0, 4, None, 1.0, None, None, None, None, None, 0, None) == 0
     assert lib.pacer_distill_backward(*rows(z=None, rows=0), None, None, 0, 4, None, 1.0, None, None, None, None, 100, None) == 0
+
+
+@pytest.mark.parametrize("change,text,code", [
+    (dict(rows=-1), "rows out of range", -1), (dict(rows=(1 << 20) + 1), "rows out of range", -1), (dict(vocab=0), "vocab out of range", -1),
+    (dict(vocab=(1 << 21) + 1), "vocab out of range", -1), (dict(d=0), "d out of range", -1), (dict(d=12), "d out of range", -1),
+    (dict(d=1 << 17), "d out of range", -1), (dict(lh=56), "bad row stride", -1), (dict(lw=68), "bad row stride", -1),
+    (dict(h=None), "is null", -1), (dict(w=None), "is null", -1), (dict(s=None), "is null", -1), (dict(h=A + 2), "misaligned", -1),
+    (dict(w=A + 8), "misaligned", -1), (dict(s=X + 16), "misaligned", -1), (dict(tok=None), "logp without tokens", -1),
+    (dict(short=1), "scratch too small", -2),
+])
+def test_head_logprobs(lib, change, text, code):
+    a = dict(h=A, lh=64, w=B, lw=64, rows=4, vocab=100, d=64, tok=X, s=X, short=0)
+    a.update(change)
+    need = lib.pacer_head_logprobs_scratch_bytes(4, 100)
+    assert need > 0
+    rc = lib.pacer_head_logprobs(a["h"], a["lh"], a["w"], a["lw"], a["rows"], a["vocab"], a["d"], a["tok"], None, 0.0, X, X, X, a["s"],
+                                 need - a["short"], None)
+    assert rc == code and text in lib.pacer_last_error(None).decode()
+
+
+def test_head_scratch(lib):
+    n = lib.pacer_head_logprobs_scratch_bytes
+    assert n(0, 100) == n(1, 0) == n((1 << 20) + 1, 100) == n(1, (1 << 21) + 1) == 0
+    for rows, vocab in ((1, 1), (1, 32000), (25, 151936), (129, 32003), (2048, 32000)):
+        assert n(rows, vocab) >= rows * 4 + rows * 2 * -(-vocab // 256) * 16      # two parts of 16 bytes per tile of at most 256 tokens
+    assert lib.pacer_head_logprobs(None, 64, None, 64, 0, 100, 64, None, None, 0.0, None, None, None, None, 0, None) == 0
