@@ -17,7 +17,7 @@ namespace lg {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32, MAX_C = 8;
 constexpr int UNROLL = 4;                  // 16-byte loads in flight per thread
-constexpr int CAND = 1024;                 // candidates for the alternatives that a block collects at most
+constexpr int CAND = 1280;                 // candidates for the alternatives that a block collects at most
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_REF = -3.402823466e38f, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
@@ -27,18 +27,40 @@ constexpr float LSE_EXACT = 65536.f;       // beyond it an f32 log-sum-exp no lo
 
 template <class T> struct Vec;
 template <> struct Vec<float> {
-    static constexpr int E = 4;
+    static constexpr int E = 4, KEY_LOW = 0;             // KEY_LOW: low bits of a value as f32 that are always 0
+    static constexpr uint32_t NONE = 0xff800000u;        // -inf
+    __device__ static float max(const uint4 *v, int n) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(v[i].x)), fmaxf(__uint_as_float(v[i].y), __uint_as_float(v[i].z))), __uint_as_float(v[i].w));
+        return m;
+    }
     __device__ static void unpack(const uint4 &v, float (&f)[4]) {
         f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
     }
     __device__ static uint4 pack(const float (&f)[4]) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
+    __device__ static void hide(uint4 &v, uint32_t w) {                 // -inf in place of the elements whose bit is set
+        if (w & 1) v.x = NONE;
+        if (w & 2) v.y = NONE;
+        if (w & 4) v.z = NONE;
+        if (w & 8) v.w = NONE;
+    }
     __device__ static float to(float x) { return x; }
     __device__ static float from(float x) { return x; }
 };
 template <> struct Vec<__nv_bfloat16> {
-    static constexpr int E = 8;
+    static constexpr int E = 8, KEY_LOW = 16;
+    static constexpr uint32_t NONE = 0xff80ff80u;
+    __device__ static float max(const uint4 *v, int n) {                // (packed: two values an instruction; NaN is passed over)
+        const auto h = [](const uint32_t &u) { return *reinterpret_cast<const __nv_bfloat162 *>(&u); };
+        __nv_bfloat162 m = h(v[0].x);
+#pragma unroll
+        for (int i = 0; i < n; ++i) m = __hmax2(__hmax2(m, h(v[i].x)), __hmax2(__hmax2(h(v[i].y), h(v[i].z)), h(v[i].w)));
+        return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+    }
     __device__ static void two(uint32_t u, float &a, float &b) { a = __uint_as_float(u << 16); b = __uint_as_float(u & 0xffff0000u); }
     __device__ static void unpack(const uint4 &v, float (&f)[8]) {
         two(v.x, f[0], f[1]); two(v.y, f[2], f[3]); two(v.z, f[4], f[5]); two(v.w, f[6], f[7]);
@@ -48,11 +70,27 @@ template <> struct Vec<__nv_bfloat16> {
         return *reinterpret_cast<const uint32_t *>(&h);
     }
     __device__ static uint4 pack(const float (&f)[8]) { return make_uint4(one(f[0], f[1]), one(f[2], f[3]), one(f[4], f[5]), one(f[6], f[7])); }
+    __device__ static void hide(uint4 &v, uint32_t w) {
+        uint32_t *u = &v.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i, w >>= 2) {
+            if (w & 1) u[i] = (u[i] & 0xffff0000u) | (NONE & 0xffffu);
+            if (w & 2) u[i] = (u[i] & 0xffffu) | (NONE & 0xffff0000u);
+        }
+    }
     __device__ static float to(__nv_bfloat16 x) { return __bfloat162float(x); }
     __device__ static __nv_bfloat16 from(float x) { return __float2bfloat16_rn(x); }
 };
 template <> struct Vec<__half> {
-    static constexpr int E = 8;
+    static constexpr int E = 8, KEY_LOW = 13;
+    static constexpr uint32_t NONE = 0xfc00fc00u;
+    __device__ static float max(const uint4 *v, int n) {
+        const auto h = [](const uint32_t &u) { return *reinterpret_cast<const __half2 *>(&u); };
+        __half2 m = h(v[0].x);
+#pragma unroll
+        for (int i = 0; i < n; ++i) m = __hmax2(__hmax2(m, h(v[i].x)), __hmax2(__hmax2(h(v[i].y), h(v[i].z)), h(v[i].w)));
+        return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+    }
     __device__ static void two(uint32_t u, float &a, float &b) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u));
         a = f.x; b = f.y;
@@ -65,6 +103,14 @@ template <> struct Vec<__half> {
         return *reinterpret_cast<const uint32_t *>(&h);
     }
     __device__ static uint4 pack(const float (&f)[8]) { return make_uint4(one(f[0], f[1]), one(f[2], f[3]), one(f[4], f[5]), one(f[6], f[7])); }
+    __device__ static void hide(uint4 &v, uint32_t w) {
+        uint32_t *u = &v.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i, w >>= 2) {
+            if (w & 1) u[i] = (u[i] & 0xffff0000u) | (NONE & 0xffffu);
+            if (w & 2) u[i] = (u[i] & 0xffffu) | (NONE & 0xffff0000u);
+        }
+    }
     __device__ static float to(__half x) { return __half2float(x); }
     __device__ static __half from(float x) { return __float2half_rn(x); }
 };
@@ -99,6 +145,13 @@ __device__ __forceinline__ uint4 ld_row(const uint4 *p) {        // (not the rea
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
+// A thread's UNROLL vectors of a batch: j, j + THREADS, ..; past the block's share -inf.
+template <class T>
+__device__ __forceinline__ void ld_batch(const Share<T> &sh, int j, uint4 (&v)[UNROLL]) {
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+        v[u] = j + u * THREADS < sh.hi ? ld_row(sh.vecs() + j + u * THREADS) : make_uint4(Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE);
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -112,6 +165,30 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if eith
 
 // ------------------------------------------------------------------ softmax sums
 
+// Two fp32 values in one register pair: one instruction works on both.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 two(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void apart(f2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // S = sum 2^t, S2 = sum 2^t t with t = (z - m) scale.  A logit of -inf adds nothing; NaN and +inf make the sums NaN.
 struct Sums {
     float m = NO_REF, S = 0.f, S2 = 0.f;
@@ -121,15 +198,11 @@ struct Sums {
         S *= r;
         m = to;
     }
-    template <int E, bool ENTROPY>
-    __device__ void add(const float (&f)[E], float vmax, float scale, float slack) {
-        if (vmax > m + slack) raise(vmax, scale);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float t = max_nan((f[e] - m) * scale, FAR), x = ex2(t);
-            S += x;
-            if (ENTROPY) S2 = fmaf(x, t, S2);
-        }
+    __device__ void add(float z, float scale) {
+        if (z > m) raise(z, scale);
+        const float t = max_nan((z - m) * scale, FAR), x = ex2(t);
+        S += x;
+        S2 = fmaf(x, t, S2);
     }
     __device__ void join(float m2, float s, float s2, float scale) {   // with the sums of another share
         const float to = fmaxf(m, m2);
@@ -137,6 +210,43 @@ struct Sums {
         const float d = fmaxf((m2 - to) * scale, FAR), r = ex2(d);
         S = fmaf(r, s, S);
         S2 = fmaf(r, fmaf(s, d, s2), S2);
+    }
+};
+
+// A thread's sums while it reads its vectors: even and odd elements apart.
+template <bool ENTROPY>
+struct PairSums {
+    float m = NO_REF;
+    f2 S = 0, S2 = 0;
+    // `top`: the largest of the elements that come next
+    __device__ void reach(float top, float scale, float slack) {
+        if (top > m + slack) {
+            const float d = fmaxf((m - top) * scale, FAR), r = ex2(d);
+            if (ENTROPY) S2 = mul2(two(r, r), fma2(S, two(d, d), S2));
+            S = mul2(two(r, r), S);
+            m = top;
+        }
+    }
+    template <int E>
+    __device__ void add(const float (&f)[E], float scale) {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            f2 t = mul2(add2(two(f[e], f[e + 1]), two(-m, -m)), two(scale, scale));
+            float t0, t1;
+            apart(t, t0, t1);
+            if (ENTROPY) { t0 = max_nan(t0, FAR); t1 = max_nan(t1, FAR); t = two(t0, t1); }      // (0 * -inf; without the product 2^-inf does)
+            const f2 x = two(ex2(t0), ex2(t1));
+            S = add2(S, x);
+            if (ENTROPY) S2 = fma2(x, t, S2);
+        }
+    }
+    __device__ Sums sums() const {
+        Sums s;
+        float a, b;
+        s.m = m;
+        apart(S, a, b); s.S = a + b;
+        if (ENTROPY) { apart(S2, a, b); s.S2 = a + b; }
+        return s;
     }
 };
 
@@ -185,10 +295,7 @@ template <class T, class Skip>
 __device__ Sums whole_row(const T *z, int vocab, float scale, SumSlots &sl, Skip skip) {
     Sums s;
     for (int i = threadIdx.x; i < vocab; i += THREADS)
-        if (!skip(i)) {
-            const float f[1] = {Vec<T>::to(z[i])};
-            s.template add<1, false>(f, f[0], scale, SLACK / scale);
-        }
+        if (!skip(i)) s.add(Vec<T>::to(z[i]), scale);
     __syncwarp();
     return row_sums(s, sl, 0, 1, scale);
 }
@@ -203,75 +310,116 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 __device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k == 0u ? 0x7fffffffu : (k & 0x80000000u) ? k ^ 0x80000000u : ~k); }
 __device__ __forceinline__ uint64_t pair_key(float z, int idx) { return ((uint64_t)order_key(z) << 32) | (uint32_t)~idx; }
 
+constexpr int SEGS = 16, FLAGS = 1024;     // a thread's vectors in at most SEGS runs of whole batches; runs that are read again
+
 struct TopSlots {
+    float seg[SEGS][THREADS];              // largest value of each run
     uint32_t key[THREADS];
     int32_t vec[THREADS];
     uint64_t cand[CAND], best[MAX_TOP];
-    int32_t flagged[THREADS];
-    int32_t n_flag, n_cand, bound_idx;
+    uint16_t flagged[FLAGS];
+    int32_t n_flag, n_cand, bound_idx, ties;
     uint32_t bound;
     int32_t count[WARPS];
 };
 
 __device__ __forceinline__ int warp_count(int v) { return __reduce_add_sync(~0u, v); }
 
-// The `top` best elements of the block's share, in order, to best[] (with fewer elements: all, the rest 0).  Each thread brings
-// the largest value `bv` of its whole vectors lo + tid, lo + tid + THREADS, ... and the first vector that has it (-1: it had none).
-// The top-th best of those per-thread maxima bounds the top-th best element from below; only the vectors of the threads that
-// reach the bound are read again (out of L2).
+// The `top` best elements of the block's share, in order, to best[] (with fewer elements: all, the rest 0).  Thread tid has read the
+// whole vectors lo + tid, lo + tid + THREADS, .. in `segs` runs of `run` vectors, whose largest values are in seg[][tid].
+// The top-th best of the 256 per-thread maxima bounds the top-th best element from below; only the runs that reach the bound are
+// read again, out of L2 (2048 rows of 32 003 bf16, top 64: about 70 runs of four vectors of 4000, 74 candidates).
 template <class T>
-__device__ void block_top(const Share<T> &sh, float bv, int bj, bool has_nan, int top, TopSlots &s) {
-    constexpr int E = Vec<T>::E;
+__device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, int top, TopSlots &s) {
+    constexpr int E = Vec<T>::E, N = THREADS / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool mine = sh.lo + tid < sh.hi;
+    float bv = -INFINITY;
+    int bseg = 0;
+    for (int g = 0; g < segs; ++g) {
+        const float v = s.seg[g][tid];
+        if (v > bv) { bv = v; bseg = g; }
+    }
     // (a maximum that ignores NaN says nothing certain about a thread that saw only -inf: it then counts as lowest)
-    s.key[tid] = bj < 0 || (has_nan && bv == -INFINITY) ? 0u : order_key(bv);
-    s.vec[tid] = bj;
-    if (tid == 0) s.n_flag = s.n_cand = 0;
+    const uint32_t key = !mine || (has_nan && bv == -INFINITY) ? 0u : order_key(bv);
+    s.key[tid] = key;
+    if (tid == 0) { s.n_flag = s.n_cand = s.ties = 0; s.bound = 0; s.bound_idx = INT32_MAX; }
     __syncthreads();
-    if (warp == 0) {
-        uint32_t k[THREADS / 32];
-        int act = 0;
+    if (warp == 0 && min(sh.hi - sh.lo, THREADS) >= top) {
+        uint32_t k[N], hi = 0, lo = ~0u;
 #pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) { k[i] = s.key[i * 32 + lane]; act += s.vec[i * 32 + lane] >= 0; }
-        uint32_t bound = 0;
-        int idx = INT32_MAX;
-        if (warp_count(act) >= top) {
-            for (int b = 31; b >= 0; --b) {                            // the largest bound that `top` maxima reach
-                const uint32_t trial = bound | (1u << b);
-                int n = 0;
+        for (int i = 0; i < N; ++i) {
+            k[i] = s.key[i * 32 + lane];
+            if (i * 32 + lane < sh.hi - sh.lo) { hi = max(hi, k[i]); lo = min(lo, k[i]); }
+        }
+        hi = __reduce_max_sync(~0u, hi); lo = __reduce_min_sync(~0u, lo);
+        // a bound that at least `top` maxima reach, and few more unless they are equal: bit by bit below the bits they share
+        const int first = hi == lo ? 0 : 32 - __clz(hi ^ lo);
+        uint32_t bound = first == 32 ? 0u : hi >> first << first;
+        for (int b = first - 1; b >= Vec<T>::KEY_LOW; --b) {
+            const uint32_t trial = bound | (1u << b);
+            int n = 0;
 #pragma unroll
-                for (int i = 0; i < THREADS / 32; ++i) n += k[i] >= trial;
-                if (warp_count(n) >= top) bound = trial;
-            }
-            int above = 0, equal = 0;
-#pragma unroll
-            for (int i = 0; i < THREADS / 32; ++i) { above += k[i] > bound; equal += k[i] == bound; }
-            above = warp_count(above); equal = warp_count(equal);
-            if (above + equal > top && bound) {                        // of equal maxima only the first vectors are needed
-                int lim = 0;                                           // least vector number v with enough maxima at vectors < v
-                int v[THREADS / 32];
-#pragma unroll
-                for (int i = 0; i < THREADS / 32; ++i) v[i] = k[i] == bound ? s.vec[i * 32 + lane] : INT32_MAX;
-                for (int b = 30; b >= 0; --b) {
-                    const int trial = lim | (1 << b);
-                    int n = 0;
-#pragma unroll
-                    for (int i = 0; i < THREADS / 32; ++i) n += v[i] < trial;
-                    if (above + warp_count(n) < top) lim = trial;
-                }
-                idx = sh.end(lim) - 1;                                 // vectors up to `lim` hold enough
+            for (int i = 0; i < N; ++i) n += k[i] >= trial;
+            n = warp_count(n);
+            if (n >= top) {
+                bound = trial;
+                if (n <= top + 4 + top / 8) break;
             }
         }
-        if (lane == 0) { s.bound = bound; s.bound_idx = idx; }
+        if (hi == lo) bound = hi;
+        else if (bound && !(bound & 0x80000000u)) bound |= (1u << Vec<T>::KEY_LOW) - 1;      // a negative value's low bits are 1
+        int above = 0, equal = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) { above += k[i] > bound; equal += k[i] == bound; }
+        above = warp_count(above); equal = warp_count(equal);
+        if (above + equal < top) bound = 0;                            // (cannot be)
+        if (lane == 0) {
+            s.bound = bound;
+            s.ties = bound && above + equal > top + 32 ? top - above : 0;
+        }
     }
     __syncthreads();
     const uint32_t bound = s.bound;
+    if (s.ties > 0) {                                                  // of many equal maxima only the first vectors are needed
+        int at = INT32_MAX;
+        if (key == bound) {
+            const int j0 = sh.lo + tid + bseg * run * THREADS;
+            for (int i = 0; i < run && at == INT32_MAX && j0 + i * THREADS < sh.hi; ++i) {
+                const uint4 v = ld_row(sh.vecs() + j0 + i * THREADS);
+                if (Vec<T>::max(&v, 1) == bv) at = j0 + i * THREADS;
+            }
+        }
+        s.vec[tid] = at;
+        __syncthreads();
+        if (warp == 0) {
+            int v[N], lim = 0;                                         // least vector number with `ties` of them at most there
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = s.vec[i * 32 + lane];
+            for (int b = 31 - __clz(sh.hi); b >= 0; --b) {
+                const int trial = lim | (1 << b);
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) n += v[i] < trial;
+                if (warp_count(n) < s.ties) lim = trial;
+            }
+            if (lane == 0) s.bound_idx = sh.end(min(lim, sh.hi - 1)) - 1;
+        }
+        __syncthreads();
+    }
     const int bound_idx = s.bound_idx;
     const uint64_t least = ((uint64_t)bound << 32) | (uint32_t)~bound_idx;
-    if (bj >= 0 && ((has_nan && bv == -INFINITY) || order_key(bv) > bound || (order_key(bv) == bound && sh.begin(bj) <= bound_idx)))
-        s.flagged[atomicAdd(&s.n_flag, 1)] = tid;
+    if (mine)
+        for (int g = 0; g < segs; ++g) {
+            const float v = s.seg[g][tid];
+            const int j = sh.lo + tid + g * run * THREADS;
+            if (j < sh.hi && ((has_nan && v == -INFINITY) || order_key(v) > bound || (order_key(v) == bound && sh.begin(j) <= bound_idx))) {
+                const int at = atomicAdd(&s.n_flag, 1);
+                if (at < FLAGS) s.flagged[at] = (uint16_t)(g * THREADS + tid);
+            }
+        }
     __syncthreads();
-    const int nf = s.n_flag, per = (sh.hi - sh.lo + THREADS - 1) / THREADS;
+    const int nf = s.n_flag;
     auto test = [&](float z, int i) {
         const uint64_t k = pair_key(z, i);
         if (k >= least) {
@@ -279,23 +427,28 @@ __device__ void block_top(const Share<T> &sh, float bv, int bj, bool has_nan, in
             if (at < CAND) s.cand[at] = k;
         }
     };
-    for (int w = tid; w < nf * per; w += THREADS) {
-        const int j = sh.lo + s.flagged[w / per] + (w % per) * THREADS;
-        if (j < sh.hi) {
-            float f[E];
-            Vec<T>::unpack(ld_row(sh.vecs() + j), f);
+    if (nf <= FLAGS) {
+        for (int w = tid; w < nf * run; w += THREADS) {
+            const int f = s.flagged[w / run], j = sh.lo + f % THREADS + ((f / THREADS) * run + w % run) * THREADS;
+            if (j < sh.hi) {
+                const uint4 v = ld_row(sh.vecs() + j);
+                if (has_nan || order_key(Vec<T>::max(&v, 1)) >= bound) {
+                    float x[E];
+                    Vec<T>::unpack(v, x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) test(f[e], sh.begin(j) + e);
+                    for (int e = 0; e < E; ++e) test(x[e], sh.begin(j) + e);
+                }
+            }
         }
-    }
-    if (tid < 2) {
-        const int j = tid ? sh.last : sh.first;
-        if (j >= 0)
-            for (int i = sh.begin(j); i < sh.end(j); ++i) test(Vec<T>::to(sh.row[i]), i);
+        if (tid < 2) {
+            const int j = tid ? sh.last : sh.first;
+            if (j >= 0)
+                for (int i = sh.begin(j); i < sh.end(j); ++i) test(Vec<T>::to(sh.row[i]), i);
+        }
     }
     __syncthreads();
     int n = s.n_cand;
-    if (n > CAND) {                                                    // (many elements of few threads, or NaN): bit by bit
+    if (n > CAND || nf > FLAGS) {                                      // (many elements of few threads, or NaN): bit by bit
         uint64_t bar = 0;
         __syncthreads();
         for (int b = 63; b >= 0; --b) {
@@ -321,11 +474,15 @@ __device__ void block_top(const Share<T> &sh, float bv, int bj, bool has_nan, in
     }
     for (int i = tid; i < top; i += THREADS)
         if (i >= n) s.best[i] = 0;
-    for (int i = tid; i < n; i += THREADS) {
-        const uint64_t k = s.cand[i];
+    for (int i0 = 0; i0 < n; i0 += THREADS / 4) {                      // a candidate's place: those above it, by four lanes
+        const int i = i0 + tid / 4;
+        const uint64_t k = i < n ? s.cand[i] : 0;
         int above = 0;
-        for (int q = 0; q < n; ++q) above += s.cand[q] > k;
-        if (above < top) s.best[above] = k;
+        if (i < n)
+            for (int q = tid % 4; q < n; q += 4) above += s.cand[q] > k;
+        above += __shfl_xor_sync(~0u, above, 1);
+        above += __shfl_xor_sync(~0u, above, 2);
+        if (i < n && tid % 4 == 0 && above < top) s.best[above] = k;
     }
     __syncthreads();
 }
@@ -354,34 +511,31 @@ __global__ void __launch_bounds__(THREADS, 4) k_logprobs(const ScoreArgs a) {
     const Share<T> sh(z, a.r.vocab, rank, C);
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (peers run before their memory is written)
 
-    Sums s;
-    float bv = -INFINITY;
-    int bj = -1;
-    auto take = [&](const uint4 &v, int j) {
-        float f[E];
-        Vec<T>::unpack(v, f);
-        float m = f[0];
-#pragma unroll
-        for (int e = 1; e < E; ++e) m = fmaxf(m, f[e]);
-        s.template add<E, true>(f, m, LOG2E, SLACK * LN2);
-        if (TOP && (m > bv || bj < 0)) { bv = m > bv ? m : bv; bj = j; }
-    };
-    int j = sh.lo + tid;
-    for (; j + (UNROLL - 1) * THREADS < sh.hi; j += UNROLL * THREADS) {
+    TopSlots &ts = *reinterpret_cast<TopSlots *>(dyn);
+    const int batches = (sh.hi - sh.lo + UNROLL * THREADS - 1) / (UNROLL * THREADS), per = (batches + SEGS - 1) / SEGS;      // a run: `per` batches
+    PairSums<true> ps;
+    float most = -INFINITY;
+    for (int n = 0, left = per, g = 0; n < batches; ++n) {
         uint4 v[UNROLL];
+        ld_batch(sh, sh.lo + tid + n * UNROLL * THREADS, v);
+        const float m = Vec<T>::max(v, UNROLL);
+        ps.reach(m, LOG2E, SLACK * LN2);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) take(v[u], j + u * THREADS);
+        for (int u = 0; u < UNROLL; ++u) {
+            float f[E];
+            Vec<T>::unpack(v[u], f);
+            ps.add(f, LOG2E);
+        }
+        if (TOP) {
+            most = fmaxf(most, m);
+            if (--left == 0 || n == batches - 1) { ts.seg[g++][tid] = most; most = -INFINITY; left = per; }
+        }
     }
-    for (; j < sh.hi; j += THREADS) take(ld_row(sh.vecs() + j), j);
+    Sums s = ps.sums();
     if (tid < 2) {
         const int p = tid ? sh.last : sh.first;
         if (p >= 0)
-            for (int i = sh.begin(p); i < sh.end(p); ++i) {
-                const float f[1] = {Vec<T>::to(z[i])};
-                s.template add<1, true>(f, f[0], LOG2E, SLACK * LN2);
-            }
+            for (int i = sh.begin(p); i < sh.end(p); ++i) s.add(Vec<T>::to(z[i]), LOG2E);
     }
     __syncwarp();
     if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -394,10 +548,9 @@ __global__ void __launch_bounds__(THREADS, 4) k_logprobs(const ScoreArgs a) {
         if (a.out.logp) a.out.logp[row] = token >= 0 && token < a.r.vocab ? logp(Vec<T>::to(z[token])) : 0.f;
     }
     if (!TOP) return;
-    TopSlots &ts = *reinterpret_cast<TopSlots *>(dyn);
     uint64_t *lists = reinterpret_cast<uint64_t *>(dyn + sizeof(TopSlots));            // rank 0: the blocks' lists
     const int top = a.out.top;
-    block_top<T>(sh, bv, bj, isnan(t.S), top, ts);
+    block_top<T>(sh, per ? (batches + per - 1) / per : 0, per * UNROLL, isnan(t.S), top, ts);
     const uint64_t *list = ts.best;
     int n = top;
     if (C > 1) {
@@ -473,31 +626,39 @@ __global__ void __launch_bounds__(THREADS) k_logprobs_back(const BackArgs a) {
         ref = s.m; rest = log2f(s.S) * LN2;
         if (C > 1) barrier_cluster();                                  // the gradient may go where the logits are
     }
+    const float c = none ? 0.f : 1.f, A1 = c * A, G1 = -c * gh, at_token = c * gl;
     auto grad = [&](float x) {
         const float l = max_nan((x - ref) - rest, FAR), p = ex2(l * LOG2E);
-        return none ? 0.f : ENTROPY ? p * fmaf(-gh, l + H, A) : p * A;
+        return none ? 0.f : ENTROPY ? p * fmaf(G1, l + H, A1) : p * A1;
     };
-    const float at_token = none ? 0.f : gl;
-    auto put = [&](const uint4 &v, int j) {
-        float f[E], d[E];
-        Vec<T>::unpack(v, f);
-        const int i0 = j * E - sh.off;
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = grad(f[e]);
-        if ((uint32_t)(token - i0) < (uint32_t)E)
-#pragma unroll
-            for (int e = 0; e < E; ++e) d[e] += i0 + e == token ? at_token : 0.f;
-        st_grad<T>(out, same, j, sh.off, d);
-    };
-    int j = sh.lo + tid;
-    for (; j + (UNROLL - 1) * THREADS < sh.hi; j += UNROLL * THREADS) {
+    for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
         uint4 v[UNROLL];
+        ld_batch(sh, j, v);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
+        for (int u = 0; u < UNROLL; ++u) {
+            if (j + u * THREADS >= sh.hi) break;
+            float f[E], d[E];
+            Vec<T>::unpack(v[u], f);
+            const int i0 = (j + u * THREADS) * E - sh.off;
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) put(v[u], j + u * THREADS);
+            for (int e = 0; e < E; e += 2) {
+                f2 l = add2(add2(two(f[e], f[e + 1]), two(-ref, -ref)), two(-rest, -rest));
+                float l0, l1;
+                if (ENTROPY) { apart(l, l0, l1); l = two(max_nan(l0, FAR), max_nan(l1, FAR)); }
+                apart(mul2(l, two(LOG2E, LOG2E)), l0, l1);
+                const f2 p = two(ex2(l0), ex2(l1));
+                const f2 g = ENTROPY ? fma2(two(G1, G1), add2(l, two(H, H)), two(A1, A1)) : two(A1, A1);
+                apart(mul2(p, g), d[e], d[e + 1]);
+            }
+            if (none)
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] = 0.f;
+            if ((uint32_t)(token - i0) < (uint32_t)E)
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] += i0 + e == token ? at_token : 0.f;
+            st_grad<T>(out, same, j + u * THREADS, sh.off, d);
+        }
     }
-    for (; j < sh.hi; j += THREADS) put(ld_row(sh.vecs() + j), j);
     if (tid < 2) {
         const int p = tid ? sh.last : sh.first;
         if (p >= 0)
@@ -637,40 +798,32 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(const DistillArgs a) {
             if (C > 1) barrier_cluster();                              // the gradient may go where the logits are
         }
     } else {
-        Sums s;
-        auto take = [&](const uint4 &v, int j) {
-            float f[E];
-            Vec<T>::unpack(v, f);
-            if (TAIL) {
-                const int o = j * E - sh.off - from;
-                const uint32_t w = __funnelshift_r(marks[o >> 5], marks[(o >> 5) + 1], o & 31) & ((1u << E) - 1);
-                if (w)
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (w >> e & 1) f[e] = -INFINITY;
-            }
-            float m = f[0];
-#pragma unroll
-            for (int e = 1; e < E; ++e) m = fmaxf(m, f[e]);
-            s.template add<E, false>(f, m, scale, slack);
-        };
-        int j = sh.lo + tid;
-        for (; j + (UNROLL - 1) * THREADS < sh.hi; j += UNROLL * THREADS) {
+        PairSums<false> ps;
+        for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
             uint4 v[UNROLL];
+            ld_batch(sh, j, v);
+            if (TAIL)
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
+                for (int u = 0; u < UNROLL; ++u) {
+                    if (j + u * THREADS >= sh.hi) break;
+                    const int o = (j + u * THREADS) * E - sh.off - from;
+                    const uint32_t w = __funnelshift_r(marks[o >> 5], marks[(o >> 5) + 1], o & 31) & ((1u << E) - 1);
+                    if (w) Vec<T>::hide(v[u], w);
+                }
+            ps.reach(Vec<T>::max(v, UNROLL), scale, slack);
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) take(v[u], j + u * THREADS);
+            for (int u = 0; u < UNROLL; ++u) {
+                float f[E];
+                Vec<T>::unpack(v[u], f);
+                ps.add(f, scale);
+            }
         }
-        for (; j < sh.hi; j += THREADS) take(ld_row(sh.vecs() + j), j);
+        Sums s = ps.sums();
         if (tid < 2) {
             const int p = tid ? sh.last : sh.first;
             if (p >= 0)
-                for (int i = sh.begin(p); i < sh.end(p); ++i) {
-                    if (TAIL && (marks[(i - from) >> 5] >> ((i - from) & 31) & 1)) continue;
-                    const float f[1] = {Vec<T>::to(z[i])};
-                    s.template add<1, false>(f, f[0], scale, slack);
-                }
+                for (int i = sh.begin(p); i < sh.end(p); ++i)
+                    if (!TAIL || !(marks[(i - from) >> 5] >> ((i - from) & 31) & 1)) s.add(Vec<T>::to(z[i]), scale);
         }
         __syncwarp();
         if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -691,23 +844,28 @@ __global__ void __launch_bounds__(THREADS, 4) k_distill(const DistillArgs a) {
     const float g = a.weight[row] * it;
     const bool others = !none && tail != -INFINITY;
     const float coef = !others ? 0.f : g * (TAIL ? Q * ex2(max_nan(((tref - ref) * it + tail - all) * LOG2E, FAR)) - qt : Q), off = others ? tail : 0.f;
-    auto grad = [&](float x) { return others ? coef * ex2(max_nan(((x - tref) * it - off) * LOG2E, FAR)) : 0.f; };
-    auto put = [&](const uint4 &v, int j) {
-        float f[E], d[E];
-        Vec<T>::unpack(v, f);
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = grad(f[e]);
-        st_grad<T>(out, same, j, sh.off, d);
-    };
-    int j = sh.lo + tid;
-    for (; j + (UNROLL - 1) * THREADS < sh.hi; j += UNROLL * THREADS) {
+    auto grad = [&](float x) { return others ? coef * ex2(((x - tref) * it - off) * LOG2E) : 0.f; };
+    const float c1 = it * LOG2E, c2 = -off * LOG2E;
+    for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
         uint4 v[UNROLL];
+        ld_batch(sh, j, v);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
+        for (int u = 0; u < UNROLL; ++u) {
+            if (j + u * THREADS >= sh.hi) break;
+            float f[E], d[E];
+            Vec<T>::unpack(v[u], f);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) put(v[u], j + u * THREADS);
+            for (int e = 0; e < E; e += 2) {
+                float t0, t1;
+                apart(fma2(add2(two(f[e], f[e + 1]), two(-tref, -tref)), two(c1, c1), two(c2, c2)), t0, t1);
+                apart(mul2(two(ex2(t0), ex2(t1)), two(coef, coef)), d[e], d[e + 1]);
+            }
+            if (!others)
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] = 0.f;
+            st_grad<T>(out, same, j + u * THREADS, sh.off, d);
+        }
     }
-    for (; j < sh.hi; j += THREADS) put(ld_row(sh.vecs() + j), j);
     if (tid < 2) {
         const int p = tid ? sh.last : sh.first;
         if (p >= 0)
