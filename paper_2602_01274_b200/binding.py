@@ -368,21 +368,28 @@ def pacer_linear_static(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor) -> 
 
 def _rows(t: torch.Tensor, name: str = "logits") -> torch.Tensor:
     """`t` as the library takes it: on the GPU, [rows][vocab], one of three types, elements of a row side by side."""
-    assert t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES, f"{name}: f32, bf16 or f16 [rows][vocab] on the GPU"
-    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES):
+        raise AssertionError(f"{name}: f32, bf16 or f16 [rows][vocab] on the GPU")
+    return t if t.is_contiguous() or (t.stride(1) == 1 and t.stride(0) >= t.shape[1]) else t.contiguous()
 
 
 def _vec(t: Optional[torch.Tensor], name: str, like: torch.Tensor, dtype, *more) -> Optional[torch.Tensor]:
     """A side input: [rows] or [rows][more], of the given type, contiguous, beside the logits.  None stays None."""
     if t is None:
         return None
-    assert t.device == like.device and t.dtype == dtype and tuple(t.shape) == (like.shape[0], *more), \
-        f"{name}: {dtype} of shape {(like.shape[0], *more)} on {like.device}"
+    if t.dtype != dtype or t.shape != (like.shape[0], *more) or t.device != like.device:
+        raise AssertionError(f"{name}: {dtype} of shape {(like.shape[0], *more)} on {like.device}")
     return t.contiguous()
 
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
+
+
+def _layout(z: torch.Tensor):
+    """The C arguments that describe rows of logits."""
+    rows, vocab = z.shape
+    return z.data_ptr(), _DTYPES[z.dtype], vocab if z.is_contiguous() else z.stride(0), rows, vocab
 
 
 def _gradient_like(z: torch.Tensor) -> torch.Tensor:
@@ -400,13 +407,19 @@ def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
     return out
 
 
-def _call(name: str, like: torch.Tensor, *args):
+_raw_stream = torch._C._cuda_getCurrentRawStream         # torch.cuda.current_stream(..).cuda_stream without the object: 2 us a call
+
+
+def _call(fn, like: torch.Tensor, *args):
     """The C entry point on the tensors' device and torch's current stream there."""
-    dev = like.device
-    with contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev):
-        rc = getattr(_lib, name)(*args, torch.cuda.current_stream(dev).cuda_stream)
+    dev = like.device.index
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
     if rc != 0:
-        raise PacerError(f"{name}: {_lib.pacer_strerror(rc).decode()}: {_lib.pacer_last_error(None).decode()}")
+        raise PacerError(f"{fn.__name__}: {_lib.pacer_strerror(rc).decode()}: {_lib.pacer_last_error(None).decode()}")
 
 
 def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
@@ -416,13 +429,13 @@ def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
     pacer_logprobs_backward, and losses.token_logprobs for autograd."""
     z = _rows(logits)
     tokens = _vec(tokens, "tokens", z, torch.int32)
-    rows, vocab = z.shape
-    logp, entropy, lse = torch.empty(3, rows, dtype=torch.float32, device=z.device).unbind(0)
-    ids = torch.empty(rows, max(top, 0), dtype=torch.int32, device=z.device)
-    top_logp = torch.empty(rows, max(top, 0), dtype=torch.float32, device=z.device)
-    _call("pacer_logprobs", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), vocab), rows, vocab, _ptr(tokens), top, logp.data_ptr(),
-          entropy.data_ptr(), lse.data_ptr(), ids.data_ptr(), top_logp.data_ptr())
-    return logp, entropy, lse, ids, top_logp
+    rows, dev, n = z.shape[0], z.device, max(top, 0)
+    # (five small tensors out of two allocations)
+    logp, entropy, lse, top_logp = torch.empty((3 + n) * rows, dtype=torch.float32, device=dev).split_with_sizes((rows, rows, rows, n * rows))
+    ids = torch.empty((rows, n), dtype=torch.int32, device=dev)
+    at = logp.data_ptr()
+    _call(_lib.pacer_logprobs, z, *_layout(z), _ptr(tokens), top, at, at + 4 * rows, at + 8 * rows, ids.data_ptr(), at + 12 * rows)
+    return logp, entropy, lse, ids, top_logp.view(rows, n)
 
 
 def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, grad_lse=None, out=None):
@@ -433,13 +446,13 @@ def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entrop
     tokens, lse, entropy = _vec(tokens, "tokens", z, torch.int32), _vec(lse, "lse", z, f32), _vec(entropy, "entropy", z, f32)
     gl, gh, gs = _vec(grad_logp, "grad_logp", z, f32), _vec(grad_entropy, "grad_entropy", z, f32), _vec(grad_lse, "grad_lse", z, f32)
     out = _out_like(z, out)
-    _call("pacer_logprobs_backward", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], _ptr(tokens),
-          _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), out.data_ptr(), max(out.stride(0), z.shape[1]))
+    _call(_lib.pacer_logprobs_backward, z, *_layout(z), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), out.data_ptr(),
+          max(out.stride(0), z.shape[1]))
     return out
 
 
 def _teacher(z, ids, teacher, teacher_lse):
-    k = ids.shape[1] if ids.dim() == 2 else -1
+    k = ids.shape[-1] if ids.dim() == 2 else -1
     ids = _vec(ids, "ids", z, torch.int32, k)
     assert teacher.dtype in _DTYPES, "teacher: f32, bf16 or f16"
     return ids, _vec(teacher, "teacher", z, teacher.dtype, k), _vec(teacher_lse, "teacher_lse", z, torch.float32), k
@@ -452,10 +465,9 @@ def pacer_distill(logits, ids, teacher, temperature: float = 1.0, teacher_lse=No
     outside the vocabulary is no entry.  Returns (loss [rows], lse [rows], tail_lse [rows] or None)."""
     z = _rows(logits)
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
-    loss, lse, tail = torch.empty(3, z.shape[0], dtype=torch.float32, device=z.device).unbind(0)
-    tail = None if teacher_lse is None else tail
-    _call("pacer_distill", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
-          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), lse.data_ptr(), _ptr(tail), None, None,
+    loss, lse = torch.empty(2, z.shape[0], dtype=torch.float32, device=z.device).unbind(0)
+    tail = None if teacher_lse is None else torch.empty_like(teacher_lse)
+    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), lse.data_ptr(), _ptr(tail), None, None,
           0)
     return loss, lse, tail
 
@@ -467,8 +479,7 @@ def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, t
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
     weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
     loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-    _call("pacer_distill", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
-          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, weight.data_ptr(),
+    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, weight.data_ptr(),
           out.data_ptr(), max(out.stride(0), z.shape[1]))
     return loss, out
 
@@ -480,8 +491,7 @@ def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, tempe
     f32 = torch.float32
     lse, tail_lse, grad_loss = _vec(lse, "lse", z, f32), _vec(tail_lse, "tail_lse", z, f32), _vec(grad_loss, "grad_loss", z, f32)
     out = _out_like(z, out)
-    _call("pacer_distill_backward", z, z.data_ptr(), _DTYPES[z.dtype], max(z.stride(0), z.shape[1]), z.shape[0], z.shape[1], ids.data_ptr(),
-          teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
+    _call(_lib.pacer_distill_backward, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
           out.data_ptr(), max(out.stride(0), z.shape[1]))
     return out
 
@@ -496,9 +506,9 @@ def pacer_head_logprobs(hidden, head, tokens, bias_ids=None, bias: float = 0.0):
     rows, d = h.shape
     vocab = w.shape[0]
     nbytes = _lib.pacer_head_logprobs_scratch_bytes(rows, vocab)
-    logp, entropy, lse = torch.empty(3, rows, dtype=torch.float32, device=h.device).unbind(0)
+    logp, entropy, lse = torch.empty(3 * rows, dtype=torch.float32, device=h.device).split_with_sizes((rows, rows, rows))
     scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device)      # (torch aligns an allocation to 512 bytes)
-    _call("pacer_head_logprobs", h, h.data_ptr(), max(h.stride(0), d), w.data_ptr(), max(w.stride(0), d), rows, vocab, d, _ptr(tokens),
+    _call(_lib.pacer_head_logprobs, h, h.data_ptr(), max(h.stride(0), d), w.data_ptr(), max(w.stride(0), d), rows, vocab, d, _ptr(tokens),
           _ptr(bias_ids), bias, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), scratch.data_ptr(), nbytes)
     return logp, entropy, lse
 

@@ -5,7 +5,7 @@
 
 namespace hs {
 
-constexpr int MAX_ROWS = 1 << 20, MAX_D = 1 << 16;
+constexpr int MAX_ROWS = 1 << 20, MAX_VOCAB = 1 << 21, MAX_D = 1 << 16;
 
 struct Args {
     const void *hidden, *head;             // bf16 [rows][d], [vocab][d]

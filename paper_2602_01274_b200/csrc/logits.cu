@@ -2,26 +2,44 @@
 // teacher's top logits, and their gradients.
 //
 // All are bound by HBM: a row is read once (and its gradient written once).  A row belongs to a cluster of C blocks, each with a
-// share of its 16-byte vectors, so that one row can have the loads of up to 16 SMs in flight; with many rows C is 1.
-// Softmax sums are held as (m, S) with S = sum 2^((z - m) scale): the reference m is raised only when a logit lies more than
-// 2^SLACK above it (S stays below vocab * 2^SLACK), so that the common path has no rescaling.  z - m is taken first: logits of any
-// size (a row masked with the type's lowest value among them) keep their differences.
+// share of its 16-byte vectors, so that one row can have the loads of up to eight SMs in flight; with many rows C is 1.  What needs a
+// row twice (its best elements, its gradient) reads it again out of L2.
+// Softmax sums are held as (m, S), S = sum 2^(z scale - m): the reference m is raised only when a logit lies more than 2^SLACK above
+// it (S stays below vocab * 2^SLACK), so that the common path has no rescaling and an exponent is one fused multiply-add.  That is
+// exact whatever the rounding of m, as long as the steps of numbers of m's size stay small: rows whose largest logit is beyond
+// HUGE_M (a row masked with the type's lowest value, say) are summed again, with differences taken first.
 #include "logits.h"
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "../../include/pacer.h"
 
 namespace lg {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32, MAX_C = 8;
-constexpr int UNROLL = 4;                  // 16-byte loads in flight per thread
-constexpr int CAND = 1280;                 // candidates for the alternatives that a block collects at most
+constexpr int UNROLL = 4;                  // 16-byte vectors of a thread in a batch
+constexpr int BATCH = UNROLL * THREADS;    // vectors of a block's batch
+constexpr int PER_SM = 5;                  // blocks on an SM
+constexpr int CAND = 512;                  // candidates for the alternatives that a block collects at most
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float NO_REF = -3.402823466e38f, SLACK = 16.f;
+constexpr float NO_REF = -3.402823466e38f, LOWEST = NO_REF, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
+constexpr float HUGE_M = 1e8f;
 constexpr float LSE_EXACT = 65536.f;       // beyond it an f32 log-sum-exp no longer tells the logits of a row apart
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 
 // ------------------------------------------------------------------ rows of 16-byte vectors
 
@@ -41,6 +59,13 @@ template <> struct Vec<float> {
     }
     __device__ static uint4 pack(const float (&f)[4]) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    // Where sums of 2^t t are wanted, what lies below LOW counts as LOW, which has 2^t = 0 over the first reference START already:
+    // 0 * -inf would be NaN.  LEAST: a row whose largest logit is below it is summed apart (LOW could count there).
+    static constexpr float LOW = -1e30f, START = -1e29f, LEAST = -HUGE_M;
+    __device__ static void lift(uint4 &v) {                             // (NaN stays)
+        v.x = __float_as_uint(max_nan(__uint_as_float(v.x), LOW)); v.y = __float_as_uint(max_nan(__uint_as_float(v.y), LOW));
+        v.z = __float_as_uint(max_nan(__uint_as_float(v.z), LOW)); v.w = __float_as_uint(max_nan(__uint_as_float(v.w), LOW));
     }
     __device__ static void hide(uint4 &v, uint32_t w) {                 // -inf in place of the elements whose bit is set
         if (w & 1) v.x = NONE;
@@ -70,6 +95,14 @@ template <> struct Vec<__nv_bfloat16> {
         return *reinterpret_cast<const uint32_t *>(&h);
     }
     __device__ static uint4 pack(const float (&f)[8]) { return make_uint4(one(f[0], f[1]), one(f[2], f[3]), one(f[4], f[5]), one(f[6], f[7])); }
+    static constexpr uint32_t LOW = 0xf14af14au;          // -1e30
+    static constexpr float START = -1e29f, LEAST = -HUGE_M;
+    __device__ static uint32_t lift(uint32_t u) {
+        const uint32_t l = LOW;
+        const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&l));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    __device__ static void lift(uint4 &v) { v.x = lift(v.x); v.y = lift(v.y); v.z = lift(v.z); v.w = lift(v.w); }
     __device__ static void hide(uint4 &v, uint32_t w) {
         uint32_t *u = &v.x;
 #pragma unroll
@@ -103,6 +136,14 @@ template <> struct Vec<__half> {
         return *reinterpret_cast<const uint32_t *>(&h);
     }
     __device__ static uint4 pack(const float (&f)[8]) { return make_uint4(one(f[0], f[1]), one(f[2], f[3]), one(f[4], f[5]), one(f[6], f[7])); }
+    static constexpr uint32_t LOW = 0xfbfffbffu;          // the lowest finite value, -65504
+    static constexpr float START = -60000.f, LEAST = -30000.f;
+    __device__ static uint32_t lift(uint32_t u) {
+        const uint32_t l = LOW;
+        const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&l));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    __device__ static void lift(uint4 &v) { v.x = lift(v.x); v.y = lift(v.y); v.z = lift(v.z); v.w = lift(v.w); }
     __device__ static void hide(uint4 &v, uint32_t w) {
         uint32_t *u = &v.x;
 #pragma unroll
@@ -135,6 +176,11 @@ struct Share {
     __device__ const uint4 *vecs() const { return reinterpret_cast<const uint4 *>(row - off); }
     __device__ int begin(int j) const { return max(j * E - off, 0); }
     __device__ int end(int j) const { return (int)min((int64_t)(j + 1) * E - off, (int64_t)vocab); }
+    // Elements of the partial vectors, one a thread: its number, or -1.
+    __device__ int edge(int tid) const {
+        const int j = tid < E ? first : tid < 2 * E ? last : -1, i = j >= 0 ? begin(j) + tid % E : 0;
+        return j >= 0 && i < end(j) ? i : -1;
+    }
     // elements of the block: [from, to)
     __device__ int from() const { return first >= 0 ? begin(first) : begin(lo); }
     __device__ int to() const { return last >= 0 ? end(last) : hi > lo ? end(hi - 1) : first >= 0 ? end(first) : from(); }
@@ -145,22 +191,20 @@ __device__ __forceinline__ uint4 ld_row(const uint4 *p) {        // (not the rea
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
-// A thread's UNROLL vectors of a batch: j, j + THREADS, ..; past the block's share -inf.
-template <class T>
-__device__ __forceinline__ void ld_batch(const Share<T> &sh, int j, uint4 (&v)[UNROLL]) {
+// f(vectors, first vector number) for a thread's vectors lo + tid, lo + tid + THREADS, ..: UNROLL at a time, the last ones one by one.
+template <class T, class F, class G>
+__device__ __forceinline__ void each_vec(const Share<T> &sh, F batch, G single) {
+    int j = sh.lo + threadIdx.x;
+    for (; j + (UNROLL - 1) * THREADS < sh.hi; j += UNROLL * THREADS) {
+        uint4 v[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
-        v[u] = j + u * THREADS < sh.hi ? ld_row(sh.vecs() + j + u * THREADS) : make_uint4(Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE);
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
+        for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
+        batch(v, j);
+    }
+    for (; j < sh.hi; j += THREADS) {
+        uint4 v[1] = {ld_row(sh.vecs() + j)};
+        single(v, j);
+    }
 }
 
 // ------------------------------------------------------------------ softmax sums
@@ -189,64 +233,73 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
     return r;
 }
 
-// S = sum 2^t, S2 = sum 2^t t with t = (z - m) scale.  A logit of -inf adds nothing; NaN and +inf make the sums NaN.
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// S = sum 2^t, S2 = sum 2^t t with t = (z - ref) scale - m.  A logit of -inf adds nothing; NaN and +inf make the sums NaN.
 struct Sums {
-    float m = NO_REF, S = 0.f, S2 = 0.f;
-    __device__ void raise(float to, float scale) {
-        const float d = fmaxf((m - to) * scale, FAR), r = ex2(d);
-        S2 = r * fmaf(S, d, S2);
-        S *= r;
-        m = to;
-    }
-    __device__ void add(float z, float scale) {
-        if (z > m) raise(z, scale);
-        const float t = max_nan((z - m) * scale, FAR), x = ex2(t);
-        S += x;
-        S2 = fmaf(x, t, S2);
-    }
-    __device__ void join(float m2, float s, float s2, float scale) {   // with the sums of another share
-        const float to = fmaxf(m, m2);
-        raise(to, scale);
-        const float d = fmaxf((m2 - to) * scale, FAR), r = ex2(d);
-        S = fmaf(r, s, S);
-        S2 = fmaf(r, fmaf(s, d, s2), S2);
-    }
+    float ref = 0.f, m = NO_REF, S = 0.f, S2 = 0.f;
+    __device__ float exponent(float z, float scale) const { return fmaf(z - ref, scale, -m); }
 };
 
 // A thread's sums while it reads its vectors: even and odd elements apart.
-template <bool ENTROPY>
+template <class T, bool ENTROPY>
 struct PairSums {
-    float m = NO_REF;
+    float m = ENTROPY ? Vec<T>::START : NO_REF;
     f2 S = 0, S2 = 0;
-    // `top`: the largest of the elements that come next
-    __device__ void reach(float top, float scale, float slack) {
-        if (top > m + slack) {
-            const float d = fmaxf((m - top) * scale, FAR), r = ex2(d);
+    __device__ void reach(float top) {                                   // the largest exponent (scaled logit) that comes next
+        if (top > m + SLACK) {
+            const float d = fmaxf(m - top, FAR), r = ex2(d);
             if (ENTROPY) S2 = mul2(two(r, r), fma2(S, two(d, d), S2));
             S = mul2(two(r, r), S);
             m = top;
         }
     }
-    template <int E>
-    __device__ void add(const float (&f)[E], float scale) {
+    // -inf has 2^t = 0, but 0 * t is NaN: a thread whose sum of products turns NaN takes the vectors again lifted, and all that follow
+    bool lifted = false;
+    template <int N>
+    __device__ void add(uint4 (&v)[N], float scale) {
+        if (!ENTROPY) { sum<N, false>(v, scale); return; }
+        if (!lifted) {
+            const f2 S0 = S, P0 = S2;
+            sum<N, false>(v, scale);
+            float a, b;
+            apart(S2, a, b);
+            if (!isnan(a + b)) return;
+            S = S0; S2 = P0;
+            lifted = true;
+        }
+        sum<N, true>(v, scale);
+    }
+    template <int N, bool LIFT>
+    __device__ void sum(const uint4 (&v)[N], float scale) {
+        constexpr int E = Vec<T>::E;
+        const f2 c = two(scale, scale), nm = two(-m, -m);
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            f2 t = mul2(add2(two(f[e], f[e + 1]), two(-m, -m)), two(scale, scale));
-            float t0, t1;
-            apart(t, t0, t1);
-            if (ENTROPY) { t0 = max_nan(t0, FAR); t1 = max_nan(t1, FAR); t = two(t0, t1); }      // (0 * -inf; without the product 2^-inf does)
-            const f2 x = two(ex2(t0), ex2(t1));
-            S = add2(S, x);
-            if (ENTROPY) S2 = fma2(x, t, S2);
+        for (int u = 0; u < N; ++u) {
+            float f[E];
+            uint4 w = v[u];
+            if (LIFT) Vec<T>::lift(w);
+            Vec<T>::unpack(w, f);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const f2 t = fma2(two(f[e], f[e + 1]), c, nm);
+                float t0, t1;
+                apart(t, t0, t1);
+                const f2 x = two(ex2(t0), ex2(t1));
+                S = add2(S, x);
+                if (ENTROPY) S2 = fma2(x, t, S2);
+            }
         }
     }
-    __device__ Sums sums() const {
-        Sums s;
-        float a, b;
-        s.m = m;
-        apart(S, a, b); s.S = a + b;
-        if (ENTROPY) { apart(S2, a, b); s.S2 = a + b; }
-        return s;
+    __device__ void add(float z, float scale) {
+        reach(z * scale);
+        const float t = max_nan(fmaf(z, scale, -m), FAR), x = ex2(t);
+        S = add2(S, two(x, 0.f));
+        if (ENTROPY) S2 = fma2(two(x, 0.f), two(t, 0.f), S2);
     }
 };
 
@@ -262,42 +315,97 @@ __device__ __forceinline__ uint32_t peer(const void *smem, int rank) {
 __device__ __forceinline__ void st_peer(uint32_t at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
 __device__ __forceinline__ void st_peer64(uint32_t at, uint64_t v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory"); }
 
-struct SumSlots {
-    float warp[WARPS][3], block[MAX_C][3];
-};
-// The row's sums in every thread of every block of the cluster; fixed order.  Ends with the cluster (or block) in step.
-__device__ __forceinline__ Sums row_sums(Sums s, SumSlots &sl, int rank, int C, float scale) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// The sums of N = 2^i lanes (lane, lane ^ 1, ..), each with its own reference, over the reference m of them all.
+template <int N>
+__device__ __forceinline__ void join_lanes(float &m, float &S, float &S2, float scale_m, int n = N) {
+    const float top = warp_max(m), d = fmaxf((m - top) * scale_m, FAR), r = ex2(d);
+    S2 = r * fmaf(S, d, S2);
+    S *= r;
+    m = top;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m = __shfl_xor_sync(~0u, s.m, o), a = __shfl_xor_sync(~0u, s.S, o), b = __shfl_xor_sync(~0u, s.S2, o);
-        s.join(m, a, b, scale);
-    }
-    if (lane == 0) { sl.warp[warp][0] = s.m; sl.warp[warp][1] = s.S; sl.warp[warp][2] = s.S2; }
-    __syncthreads();
-    Sums t;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) t.join(sl.warp[w][0], sl.warp[w][1], sl.warp[w][2], scale);
-    if (C == 1) return t;
-    if ((int)threadIdx.x < C) {
-        const uint32_t at = peer(&sl.block[rank][0], threadIdx.x);
-        st_peer(at, t.m); st_peer(at + 4, t.S); st_peer(at + 8, t.S2);
-    }
-    barrier_cluster();
-    Sums u;
-    for (int c = 0; c < C; ++c) u.join(sl.block[c][0], sl.block[c][1], sl.block[c][2], scale);
-    return u;
+    for (int o = 1; o < N; o <<= 1)
+        if (o < n) { S += __shfl_xor_sync(~0u, S, o); S2 += __shfl_xor_sync(~0u, S2, o); }
 }
 
-// The sums of a whole row in every thread of one block, element by element, without the tokens that skip() names: for rows whose
-// log-sum-exp says too little (see LSE_EXACT).
+struct SumSlots {
+    float4 warp[WARPS], block[MAX_C];
+};
+// The sums of the block's threads in all of them, in a fixed order.  scale_m: from differences of m to exponents.
+__device__ __forceinline__ void block_sums(float &m, float &S, float &S2, SumSlots &sl, float scale_m) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    join_lanes<32>(m, S, S2, scale_m);
+    if (lane == 0) sl.warp[warp] = make_float4(m, S, S2, 0.f);
+    __syncthreads();
+    const float4 w = sl.warp[lane % WARPS];
+    m = w.x; S = w.y; S2 = w.z;
+    join_lanes<WARPS>(m, S, S2, scale_m);
+}
+
+// The sums of a whole row by one block, differences of logits taken first: for rows whose scaled logits or log-sum-exp say too
+// little (HUGE_M, LSE_EXACT).  skip(i): tokens to leave out.
 template <class T, class Skip>
-__device__ Sums whole_row(const T *z, int vocab, float scale, SumSlots &sl, Skip skip) {
+__device__ __noinline__ Sums whole_row(const T *z, int vocab, float scale, SumSlots &sl, Skip skip) {
+    constexpr int E = Vec<T>::E;
+    const Share<T> sh(z, vocab, 0, 1);
+    float m = LOWEST, S = 0.f, S2 = 0.f;                                 // (m unscaled)
+    auto add = [&](float x, int i) {
+        if (skip(i)) return;
+        if (x > m) {
+            const float d = fmaxf((m - x) * scale, FAR), r = ex2(d);
+            S2 = r * fmaf(S, d, S2);
+            S *= r;
+            m = x;
+        }
+        const float t = max_nan((x - m) * scale, FAR), p = ex2(t);
+        S += p;
+        S2 = fmaf(p, t, S2);
+    };
+    auto vec = [&](const uint4 &v, int j) {
+        float f[E];
+        Vec<T>::unpack(v, f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(f[e], j * E - sh.off + e);
+    };
+#pragma unroll 4
+    for (int j = sh.lo + threadIdx.x; j < sh.hi; j += THREADS) vec(ld_row(sh.vecs() + j), j);
+    if (const int i = sh.edge(threadIdx.x); i >= 0) add(Vec<T>::to(z[i]), i);
+    __syncthreads();                                                     // (the slots may still be read)
+    block_sums(m, S, S2, sl, scale);
     Sums s;
-    for (int i = threadIdx.x; i < vocab; i += THREADS)
-        if (!skip(i)) s.add(Vec<T>::to(z[i]), scale);
+    s.ref = m; s.m = 0.f; s.S = S; s.S2 = S2;
+    return s;
+}
+
+template <class T>
+__device__ __forceinline__ bool huge(float m, float scale) { return !(m < HUGE_M && m > Vec<T>::LEAST * fminf(1.f, scale)); }
+
+// The row's sums in every thread of every block of the cluster, in a fixed order; the cluster (or block) is in step after it.
+template <class T, class Skip>
+__device__ __forceinline__ Sums row_sums(float m, f2 S_, f2 S2_, const Share<T> &sh, SumSlots &sl, int rank, int C, float scale, Skip skip) {
+    float S, S2, b;
+    apart(S_, S, b); S += b;
+    apart(S2_, S2, b); S2 += b;
     __syncwarp();
-    return row_sums(s, sl, 0, 1, scale);
+    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // (the peers run: see the kernels' first lines)
+    block_sums(m, S, S2, sl, 1.f);
+    if (C > 1) {
+        if ((int)threadIdx.x < C) {
+            const uint32_t at = peer(&sl.block[rank], threadIdx.x);
+            st_peer(at, m); st_peer(at + 4, S); st_peer(at + 8, S2);
+        }
+        barrier_cluster();
+        const float4 w = sl.block[threadIdx.x & (C - 1)];
+        m = w.x; S = w.y; S2 = w.z;
+        join_lanes<MAX_C>(m, S, S2, 1.f, C);
+    }
+    if (huge<T>(m, scale)) {                                             // (in all blocks of the cluster alike)
+        const Sums s = whole_row<T>(sh.row, sh.vocab, scale, sl, skip);
+        if (C > 1) barrier_cluster();                                    // the gradient may go where the logits are
+        return s;
+    }
+    Sums s;
+    s.m = m; s.S = S; s.S2 = S2;
+    return s;
 }
 
 // ------------------------------------------------------------------ alternatives
@@ -310,15 +418,16 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 __device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k == 0u ? 0x7fffffffu : (k & 0x80000000u) ? k ^ 0x80000000u : ~k); }
 __device__ __forceinline__ uint64_t pair_key(float z, int idx) { return ((uint64_t)order_key(z) << 32) | (uint32_t)~idx; }
 
-constexpr int SEGS = 16, FLAGS = 1024;     // a thread's vectors in at most SEGS runs of whole batches; runs that are read again
+constexpr int AGAIN = 512;                 // batches that are looked at again at most
 
 struct TopSlots {
-    float seg[SEGS][THREADS];              // largest value of each run
-    uint32_t key[THREADS];
-    int32_t vec[THREADS];
-    uint64_t cand[CAND], best[MAX_TOP];
-    uint16_t flagged[FLAGS];
-    int32_t n_flag, n_cand, bound_idx, ties;
+    union {
+        struct { uint32_t key[THREADS]; int32_t vec[THREADS]; int32_t equal[THREADS]; };     // while the bound is looked for
+        uint64_t cand[CAND];
+    };
+    uint64_t best[MAX_TOP];
+    uint16_t again[AGAIN];
+    int32_t n_again, n_cand, bound_idx, ties;
     uint32_t bound;
     int32_t count[WARPS];
 };
@@ -326,31 +435,32 @@ struct TopSlots {
 __device__ __forceinline__ int warp_count(int v) { return __reduce_add_sync(~0u, v); }
 
 // The `top` best elements of the block's share, in order, to best[] (with fewer elements: all, the rest 0).  Thread tid has read the
-// whole vectors lo + tid, lo + tid + THREADS, .. in `segs` runs of `run` vectors, whose largest values are in seg[][tid].
-// The top-th best of the 256 per-thread maxima bounds the top-th best element from below; only the runs that reach the bound are
-// read again, out of L2 (2048 rows of 32 003 bf16, top 64: about 70 runs of four vectors of 4000, 74 candidates).
+// whole vectors lo + tid, lo + tid + THREADS, .., and left the largest value of each of its `runs` runs of `run` of them in seg[][tid].
+// The top-th best of the 256 per-thread maxima bounds the top-th best element from below; only runs that reach the bound are
+// read again, out of L2 (2048 rows of 32 003 bf16, top 64: 79 runs of four vectors of 1000, 82 candidates).
 template <class T>
-__device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, int top, TopSlots &s) {
+__device__ void block_top(const Share<T> &sh, const float (*seg)[THREADS], int runs, int run, bool has_nan, int top, TopSlots &s) {
     constexpr int E = Vec<T>::E, N = THREADS / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool mine = sh.lo + tid < sh.hi;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = sh.hi - sh.lo, RUN = run * THREADS;
+    const uint4 *buf = sh.vecs() + sh.lo;
+    const bool mine = tid < nv;
     float bv = -INFINITY;
     int bseg = 0;
-    for (int g = 0; g < segs; ++g) {
-        const float v = s.seg[g][tid];
+    for (int g = 0; g < runs; ++g) {
+        const float v = seg[g][tid];
         if (v > bv) { bv = v; bseg = g; }
     }
     // (a maximum that ignores NaN says nothing certain about a thread that saw only -inf: it then counts as lowest)
     const uint32_t key = !mine || (has_nan && bv == -INFINITY) ? 0u : order_key(bv);
     s.key[tid] = key;
-    if (tid == 0) { s.n_flag = s.n_cand = s.ties = 0; s.bound = 0; s.bound_idx = INT32_MAX; }
+    if (tid == 0) { s.n_again = s.n_cand = s.ties = 0; s.bound = 0; s.bound_idx = INT32_MAX; }
     __syncthreads();
-    if (warp == 0 && min(sh.hi - sh.lo, THREADS) >= top) {
+    if (warp == 0 && min(nv, THREADS) >= top) {
         uint32_t k[N], hi = 0, lo = ~0u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             k[i] = s.key[i * 32 + lane];
-            if (i * 32 + lane < sh.hi - sh.lo) { hi = max(hi, k[i]); lo = min(lo, k[i]); }
+            if (i * 32 + lane < nv) { hi = max(hi, k[i]); lo = min(lo, k[i]); }
         }
         hi = __reduce_max_sync(~0u, hi); lo = __reduce_min_sync(~0u, lo);
         // a bound that at least `top` maxima reach, and few more unless they are equal: bit by bit below the bits they share
@@ -382,25 +492,27 @@ __device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, i
     __syncthreads();
     const uint32_t bound = s.bound;
     if (s.ties > 0) {                                                  // of many equal maxima only the first vectors are needed
-        int at = INT32_MAX;
-        if (key == bound) {
-            const int j0 = sh.lo + tid + bseg * run * THREADS;
-            for (int i = 0; i < run && at == INT32_MAX && j0 + i * THREADS < sh.hi; ++i) {
-                const uint4 v = ld_row(sh.vecs() + j0 + i * THREADS);
-                if (Vec<T>::max(&v, 1) == bv) at = j0 + i * THREADS;
-            }
-        }
-        s.vec[tid] = at;
+        int at = INT32_MAX, equal = 0;
+        if (key == bound && mine)
+            for (int i = bseg * RUN + tid; i < min((bseg + 1) * RUN, nv) && at == INT32_MAX; i += THREADS)
+                if (const uint4 v = ld_row(buf + i); Vec<T>::max(&v, 1) == bv) {
+                    float x[E];
+                    Vec<T>::unpack(v, x);
+                    at = sh.lo + i;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) equal += x[e] == bv;
+                }
+        s.vec[tid] = at; s.equal[tid] = equal;
         __syncthreads();
         if (warp == 0) {
-            int v[N], lim = 0;                                         // least vector number with `ties` of them at most there
+            int v[N], c[N], lim = 0;                                   // least vector number with `ties` such elements up to it
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = s.vec[i * 32 + lane];
+            for (int i = 0; i < N; ++i) { v[i] = s.vec[i * 32 + lane]; c[i] = s.equal[i * 32 + lane]; }
             for (int b = 31 - __clz(sh.hi); b >= 0; --b) {
                 const int trial = lim | (1 << b);
                 int n = 0;
 #pragma unroll
-                for (int i = 0; i < N; ++i) n += v[i] < trial;
+                for (int i = 0; i < N; ++i) n += v[i] < trial ? c[i] : 0;
                 if (warp_count(n) < s.ties) lim = trial;
             }
             if (lane == 0) s.bound_idx = sh.end(min(lim, sh.hi - 1)) - 1;
@@ -409,17 +521,7 @@ __device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, i
     }
     const int bound_idx = s.bound_idx;
     const uint64_t least = ((uint64_t)bound << 32) | (uint32_t)~bound_idx;
-    if (mine)
-        for (int g = 0; g < segs; ++g) {
-            const float v = s.seg[g][tid];
-            const int j = sh.lo + tid + g * run * THREADS;
-            if (j < sh.hi && ((has_nan && v == -INFINITY) || order_key(v) > bound || (order_key(v) == bound && sh.begin(j) <= bound_idx))) {
-                const int at = atomicAdd(&s.n_flag, 1);
-                if (at < FLAGS) s.flagged[at] = (uint16_t)(g * THREADS + tid);
-            }
-        }
-    __syncthreads();
-    const int nf = s.n_flag;
+    const float least_value = bound > order_key(-INFINITY) ? order_value(bound) : -INFINITY;
     auto test = [&](float z, int i) {
         const uint64_t k = pair_key(z, i);
         if (k >= least) {
@@ -427,28 +529,44 @@ __device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, i
             if (at < CAND) s.cand[at] = k;
         }
     };
-    if (nf <= FLAGS) {
-        for (int w = tid; w < nf * run; w += THREADS) {
-            const int f = s.flagged[w / run], j = sh.lo + f % THREADS + ((f / THREADS) * run + w % run) * THREADS;
-            if (j < sh.hi) {
-                const uint4 v = ld_row(sh.vecs() + j);
-                if (has_nan || order_key(Vec<T>::max(&v, 1)) >= bound) {
-                    float x[E];
-                    Vec<T>::unpack(v, x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) test(x[e], sh.begin(j) + e);
-                }
-            }
-        }
-        if (tid < 2) {
-            const int j = tid ? sh.last : sh.first;
-            if (j >= 0)
-                for (int i = sh.begin(j); i < sh.end(j); ++i) test(Vec<T>::to(sh.row[i]), i);
-        }
+    for (int g = 0; g < runs; ++g) {
+        const int i0 = g * RUN + tid;
+        const uint32_t k = i0 < nv ? order_key(seg[g][tid]) : 0u;
+        const bool hit = i0 < nv && (has_nan || k > bound || (k == bound && sh.begin(sh.lo + i0) <= bound_idx));
+        const uint32_t all = __ballot_sync(~0u, hit);
+        if (!all) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s.n_again, __popc(all));
+        at = __shfl_sync(~0u, at, 0) + __popc(all & ((1u << lane) - 1));
+        if (hit && at < AGAIN) s.again[at] = (uint16_t)(g * THREADS + tid);
     }
     __syncthreads();
+    const int again = min(s.n_again, AGAIN);
+    for (int w0 = tid; w0 < again * UNROLL; w0 += 2 * THREADS)         // (two vectors on their way)
+        for (int p = 0; p < run; p += UNROLL) {
+            uint4 v[2];
+            int at[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int w = w0 + h * THREADS, f = w < again * UNROLL ? s.again[w / UNROLL] : 0;
+                const int i = f / THREADS * RUN + f % THREADS + (p + w % UNROLL) * THREADS;
+                at[h] = w < again * UNROLL && i < nv ? i : -1;
+                if (at[h] >= 0) v[h] = ld_row(buf + i);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (at[h] < 0 || (!has_nan && order_key(Vec<T>::max(v + h, 1)) < bound)) continue;
+                float x[E];
+                Vec<T>::unpack(v[h], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (has_nan || x[e] >= least_value) test(x[e], sh.begin(sh.lo + at[h]) + e);
+            }
+        }
+    if (const int i = sh.edge(tid); i >= 0) test(Vec<T>::to(sh.row[i]), i);
+    __syncthreads();
     int n = s.n_cand;
-    if (n > CAND || nf > FLAGS) {                                      // (many elements of few threads, or NaN): bit by bit
+    if (n > CAND || s.n_again > AGAIN) {                                      // (many elements of few threads, or NaN): bit by bit
         uint64_t bar = 0;
         __syncthreads();
         for (int b = 63; b >= 0; --b) {
@@ -479,6 +597,7 @@ __device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, i
         const uint64_t k = i < n ? s.cand[i] : 0;
         int above = 0;
         if (i < n)
+#pragma unroll 4
             for (int q = tid % 4; q < n; q += 4) above += s.cand[q] > k;
         above += __shfl_xor_sync(~0u, above, 1);
         above += __shfl_xor_sync(~0u, above, 2);
@@ -487,17 +606,18 @@ __device__ void block_top(const Share<T> &sh, int segs, int run, bool has_nan, i
     __syncthreads();
 }
 
+constexpr int RUNS = 8;                    // runs of a thread's vectors at most
+
 struct ScoreArgs {
     Rows r;
     const int32_t *tokens;
     Window win;
     ScoreOut out;
-    int32_t C;
+    int32_t C, per;                        // blocks of a row; batches of a run
 };
 
 template <class T, bool TOP>
-__global__ void __launch_bounds__(THREADS, 4) k_logprobs(const ScoreArgs a) {
-    constexpr int E = Vec<T>::E;
+__global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a) {
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ SumSlots sl;
     const int C = a.C, rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x;
@@ -507,50 +627,47 @@ __global__ void __launch_bounds__(THREADS, 4) k_logprobs(const ScoreArgs a) {
         if (j >= n) return;                                            // (all blocks of the cluster)
         if (j < n - 1) token = a.win.drafts[(size_t)s * (a.win.per_seq - 1) + j];
     } else if (a.tokens) token = a.tokens[row];
+    // shared memory, with alternatives: the runs' maxima, the slots, and (rank 0) the blocks' lists
+    float (*seg)[THREADS] = reinterpret_cast<float (*)[THREADS]>(dyn);
+    TopSlots &ts = *reinterpret_cast<TopSlots *>(seg + RUNS);
+    uint64_t *lists = reinterpret_cast<uint64_t *>(&ts + 1);
     const T *z = reinterpret_cast<const T *>(a.r.z) + (int64_t)row * a.r.ld;
     const Share<T> sh(z, a.r.vocab, rank, C);
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (peers run before their memory is written)
 
-    TopSlots &ts = *reinterpret_cast<TopSlots *>(dyn);
-    const int batches = (sh.hi - sh.lo + UNROLL * THREADS - 1) / (UNROLL * THREADS), per = (batches + SEGS - 1) / SEGS;      // a run: `per` batches
-    PairSums<true> ps;
+    const int edge = sh.edge(tid);
+    const float at_edge = edge >= 0 ? Vec<T>::to(z[edge]) : 0.f, at_token = token >= 0 && token < a.r.vocab ? Vec<T>::to(z[token]) : 0.f;
+    PairSums<T, true> ps;
     float most = -INFINITY;
-    for (int n = 0, left = per, g = 0; n < batches; ++n) {
-        uint4 v[UNROLL];
-        ld_batch(sh, sh.lo + tid + n * UNROLL * THREADS, v);
+    int left = a.per, runs = 0;
+    each_vec(sh, [&](uint4 (&v)[UNROLL], int) {
         const float m = Vec<T>::max(v, UNROLL);
-        ps.reach(m, LOG2E, SLACK * LN2);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            float f[E];
-            Vec<T>::unpack(v[u], f);
-            ps.add(f, LOG2E);
-        }
+        ps.reach(m * LOG2E);
+        ps.add(v, LOG2E);
         if (TOP) {
             most = fmaxf(most, m);
-            if (--left == 0 || n == batches - 1) { ts.seg[g++][tid] = most; most = -INFINITY; left = per; }
+            if (--left == 0) { seg[runs++][tid] = most; most = -INFINITY; left = a.per; }
         }
-    }
-    Sums s = ps.sums();
-    if (tid < 2) {
-        const int p = tid ? sh.last : sh.first;
-        if (p >= 0)
-            for (int i = sh.begin(p); i < sh.end(p); ++i) s.add(Vec<T>::to(z[i]), LOG2E);
-    }
-    __syncwarp();
-    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const Sums t = row_sums(s, sl, rank, C, LOG2E);
-    const float log2S = log2f(t.S), logS = log2S * LN2;                // (a row of -inf: S = 0)
-    auto logp = [&](float x) { return t.S == 0.f ? -INFINITY : (x - t.m) - logS; };
+    }, [&](uint4 (&v)[1], int) {
+        const float m = Vec<T>::max(v, 1);
+        ps.reach(m * LOG2E);
+        ps.add(v, LOG2E);
+        if (TOP) most = fmaxf(most, m);
+    });
+    const int batches = (sh.hi - sh.lo + BATCH - 1) / BATCH, all_runs = (batches + a.per - 1) / a.per;
+    if (TOP && runs < all_runs) seg[runs][tid] = most;
+    if (edge >= 0) ps.add(at_edge, LOG2E);
+    const Sums t = row_sums<T>(ps.m, ps.S, ps.S2, sh, sl, rank, C, LOG2E, [](int) { return false; });
+    const float log2S = log2f(t.S), all = (t.m + log2S) * LN2;         // (a row of -inf: S = 0)
+    auto logp = [&](float x) { return t.S == 0.f ? -INFINITY : (x - t.ref) - all; };
     if (rank == 0 && tid == 0) {
-        if (a.out.lse) a.out.lse[row] = t.S == 0.f ? -INFINITY : t.m + logS;
+        if (a.out.lse) a.out.lse[row] = t.S == 0.f ? -INFINITY : t.ref + all;
         if (a.out.entropy) a.out.entropy[row] = t.S == 0.f ? 0.f : (log2S - t.S2 / t.S) * LN2;
-        if (a.out.logp) a.out.logp[row] = token >= 0 && token < a.r.vocab ? logp(Vec<T>::to(z[token])) : 0.f;
+        if (a.out.logp) a.out.logp[row] = token >= 0 && token < a.r.vocab ? logp(at_token) : 0.f;
     }
     if (!TOP) return;
-    uint64_t *lists = reinterpret_cast<uint64_t *>(dyn + sizeof(TopSlots));            // rank 0: the blocks' lists
     const int top = a.out.top;
-    block_top<T>(sh, per ? (batches + per - 1) / per : 0, per * UNROLL, isnan(t.S), top, ts);
+    block_top<T>(sh, seg, all_runs, a.per * UNROLL, isnan(t.S), top, ts);
     const uint64_t *list = ts.best;
     int n = top;
     if (C > 1) {
@@ -622,8 +739,8 @@ __global__ void __launch_bounds__(THREADS) k_logprobs_back(const BackArgs a) {
     const bool none = lse == -INFINITY;                                // a row of -inf: no gradient
     float ref = lse, rest = 0.f;                                       // log p = (z - ref) - rest
     if (fabsf(lse) >= LSE_EXACT && !none) {                            // (the same in all blocks of the cluster)
-        const Sums s = whole_row(z, a.r.vocab, LOG2E, sl, [](int) { return false; });
-        ref = s.m; rest = log2f(s.S) * LN2;
+        const Sums s = whole_row<T>(z, a.r.vocab, LOG2E, sl, [](int) { return false; });
+        ref = s.ref; rest = log2f(s.S) * LN2;
         if (C > 1) barrier_cluster();                                  // the gradient may go where the logits are
     }
     const float c = none ? 0.f : 1.f, A1 = c * A, G1 = -c * gh, at_token = c * gl;
@@ -631,39 +748,33 @@ __global__ void __launch_bounds__(THREADS) k_logprobs_back(const BackArgs a) {
         const float l = max_nan((x - ref) - rest, FAR), p = ex2(l * LOG2E);
         return none ? 0.f : ENTROPY ? p * fmaf(G1, l + H, A1) : p * A1;
     };
-    for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
-        uint4 v[UNROLL];
-        ld_batch(sh, j, v);
+    auto put = [&](const uint4 &v, int j) {
+        float f[E], d[E];
+        Vec<T>::unpack(v, f);
+        const int i0 = j * E - sh.off;
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            if (j + u * THREADS >= sh.hi) break;
-            float f[E], d[E];
-            Vec<T>::unpack(v[u], f);
-            const int i0 = (j + u * THREADS) * E - sh.off;
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                f2 l = add2(add2(two(f[e], f[e + 1]), two(-ref, -ref)), two(-rest, -rest));
-                float l0, l1;
-                if (ENTROPY) { apart(l, l0, l1); l = two(max_nan(l0, FAR), max_nan(l1, FAR)); }
-                apart(mul2(l, two(LOG2E, LOG2E)), l0, l1);
-                const f2 p = two(ex2(l0), ex2(l1));
-                const f2 g = ENTROPY ? fma2(two(G1, G1), add2(l, two(H, H)), two(A1, A1)) : two(A1, A1);
-                apart(mul2(p, g), d[e], d[e + 1]);
-            }
-            if (none)
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] = 0.f;
-            if ((uint32_t)(token - i0) < (uint32_t)E)
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] += i0 + e == token ? at_token : 0.f;
-            st_grad<T>(out, same, j + u * THREADS, sh.off, d);
+        for (int e = 0; e < E; e += 2) {
+            f2 l = add2(add2(two(f[e], f[e + 1]), two(-ref, -ref)), two(-rest, -rest));
+            float l0, l1;
+            if (ENTROPY) { apart(l, l0, l1); l = two(max_nan(l0, FAR), max_nan(l1, FAR)); }
+            apart(mul2(l, two(LOG2E, LOG2E)), l0, l1);
+            const f2 p = two(ex2(l0), ex2(l1));
+            const f2 g = ENTROPY ? fma2(two(G1, G1), add2(l, two(H, H)), two(A1, A1)) : two(A1, A1);
+            apart(mul2(p, g), d[e], d[e + 1]);
         }
-    }
-    if (tid < 2) {
-        const int p = tid ? sh.last : sh.first;
-        if (p >= 0)
-            for (int i = sh.begin(p); i < sh.end(p); ++i) out[i] = Vec<T>::from(grad(Vec<T>::to(z[i])) + (i == token ? at_token : 0.f));
-    }
+        if (none)
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = 0.f;
+        if ((uint32_t)(token - i0) < (uint32_t)E)
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] += i0 + e == token ? at_token : 0.f;
+        st_grad<T>(out, same, j, sh.off, d);
+    };
+    each_vec(sh, [&](uint4 (&v)[UNROLL], int j) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) put(v[u], j + u * THREADS);
+    }, [&](uint4 (&v)[1], int j) { put(v[0], j); });
+    if (const int i = sh.edge(tid); i >= 0) out[i] = Vec<T>::from(grad(Vec<T>::to(z[i])) + (i == token ? at_token : 0.f));
 }
 
 // ------------------------------------------------------------------ distillation
@@ -677,44 +788,64 @@ struct DistillArgs {
     const float *lse_in, *tail_in, *weight;
     void *dz;
     int64_t ld_dz;
-    int32_t C;
+    int32_t C, mark_words;
 };
 
 struct DistillSlots {
-    SumSlots sums;
-    int32_t id[MAX_K];
+    alignas(16) int32_t id[MAX_K + 4];
+    float tl[MAX_K], zk[MAX_K];            // teacher's entry as an exponent (-inf: no entry), student's logit
     float q[MAX_K];
-    float red[WARPS];
+    uint8_t first[MAX_K];                  // 1: the first entry of its id
+    float Q, qt, norm, top, list;          // sum q, the rest, log2 of the teacher's sum; largest listed logit, sum 2^((zk - top) scale)
+    int32_t any;
 };
 
-__device__ __forceinline__ float block_add(float v, float *red) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ float warp_add(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-    __syncthreads();
-    if (lane == 0) red[warp] = v;
-    __syncthreads();
-    float t = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) t += red[w];
-    return t;
-}
-__device__ __forceinline__ float block_max(float v, float *red) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-    __syncthreads();
-    if (lane == 0) red[warp] = v;
-    __syncthreads();
-    float t = red[0];
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) t = fmaxf(t, red[w]);
-    return t;
+    return v;
 }
 __device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
     return dtype == PACER_F32 ? reinterpret_cast<const float *>(p)[i]
          : dtype == PACER_BF16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[i])
                                : __half2float(reinterpret_cast<const __half *>(p)[i]);
+}
+
+// The list's own sums, by one warp: q, Q, q_t, and (a tail) the listed tokens' sum of exponentials over their largest logit.
+template <bool TAIL>
+__device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, float teacher_lse) {
+    const int lane = threadIdx.x & 31;
+    float norm, top = -INFINITY, tm = -INFINITY;
+    bool any = false;
+    for (int k = lane; k < K; k += 32) {
+        any |= ds.id[k] >= 0;
+        if (TAIL && ds.first[k]) top = fmaxf(top, ds.zk[k]);
+        if (!TAIL) tm = fmaxf(tm, ds.tl[k]);
+    }
+    any = __any_sync(~0u, any);
+    if (TAIL) {
+        norm = teacher_lse * LOG2E;
+        top = warp_max(top);
+    } else {
+        tm = warp_max(tm);
+        const float ref = tm == -INFINITY ? 0.f : tm;
+        float sum = 0.f;
+        for (int k = lane; k < K; k += 32) sum += ex2(ds.tl[k] - ref);
+        norm = ref + log2f(warp_add(sum));                             // -inf: no entry that the teacher allows
+    }
+    float Q = 0.f, list = 0.f;
+    for (int k = lane; k < K; k += 32) {
+        const float q = ds.id[k] >= 0 && norm != -INFINITY ? ex2(ds.tl[k] - norm) : 0.f;
+        ds.q[k] = q;
+        Q += q;
+        if (TAIL && ds.first[k]) list += ex2(max_nan((ds.zk[k] - top) * scale, FAR));
+    }
+    Q = warp_add(Q);
+    if (TAIL) list = warp_add(list);
+    if (lane == 0) {
+        const float qt = TAIL ? fmaxf(0.f, 1.f - Q) : 0.f;
+        ds.Q = Q + qt; ds.qt = qt; ds.norm = norm; ds.top = top; ds.list = list; ds.any = any;
+    }
 }
 
 // L = sum_k q_k (log q_k - log p_{id_k}) + q_t (log q_t - log p_t), p = softmax(z / temperature); q: the teacher's entries,
@@ -723,174 +854,178 @@ __device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
 //   dL/dz_v = w_v (Q p_t - q_t) / temperature                  for the others, w_v = p_v / p_t: their softmax among themselves
 // (without q_t: p_v Q / temperature).  The tail's sum is taken over the tokens outside the list themselves, marked in a bitmap:
 // one minus the list's share would lose it where the student is sure of the list.
-// The gradient is written from a second reading of the row, out of L2, with the list's tokens put right after it.
+// The gradient of all others is written first, the list's tokens are put right after it.
 template <class T, bool TAIL, int MODE>
-__global__ void __launch_bounds__(THREADS, 4) k_distill(const DistillArgs a) {
+__global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a) {
     constexpr int E = Vec<T>::E;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ DistillSlots ds;
+    __shared__ SumSlots sl;
     const int C = a.C, rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x, V = a.r.vocab, K = a.t.k;
     const T *z = reinterpret_cast<const T *>(a.r.z) + (int64_t)row * a.r.ld;
     const Share<T> sh(z, V, rank, C);
     const float scale = LOG2E * a.t.inv_temp;
-    if (C > 1 && MODE != GRAD) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    constexpr bool marked = TAIL && MODE != GRAD;
+    uint32_t *marks = reinterpret_cast<uint32_t *>(dyn);               // a bit for each element of the share
+    if (C > 1 && MODE != GRAD) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (peers run before their memory is written)
 
     // the list: entry tid
-    uint32_t *marks = reinterpret_cast<uint32_t *>(dyn);               // TAIL: a bit per element of the block's share
-    const int from = sh.from(), to = sh.to();
-    if (TAIL && MODE != GRAD)
-        for (int i = tid; i < (to - from + 31) / 32 + 1; i += THREADS) marks[i] = 0;
+    const int from = sh.from(), to = sh.to(), edge = sh.edge(tid);
     int id = -1;
-    float tl = -INFINITY, zk = -INFINITY;
     if (tid < K) {
         id = a.t.ids[(int64_t)row * K + tid];
         if (id < 0 || id >= V) id = -1;
-        if (id >= 0) {
-            tl = load_any(a.t.t, (int64_t)row * K + tid, a.t.dtype) * scale;
-            zk = Vec<T>::to(z[id]);
-        }
         ds.id[tid] = id;
-    }
-    float norm;                                                        // log2 of the teacher's sum
-    if (TAIL) norm = a.t.lse[row] * LOG2E;
-    else {
-        const float m = block_max(tl, ds.red), ref = m == -INFINITY ? 0.f : m;
-        norm = ref + log2f(block_add(ex2(tl - ref), ds.red));          // -inf: an empty list
-    }
-    const float lq = id >= 0 ? tl - norm : -INFINITY, q = id >= 0 && norm != -INFINITY ? ex2(lq) : 0.f;
-    bool first = id >= 0;
+        ds.tl[tid] = id >= 0 ? load_any(a.t.t, (int64_t)row * K + tid, a.t.dtype) * scale : -INFINITY;
+    } else if (tid < K + 4) ds.id[tid] = -1;                           // (ids are compared four at a time)
+    if (marked)
+        for (int i = tid; i < a.mark_words; i += THREADS) marks[i] = 0;
+    const float at_edge = edge >= 0 ? Vec<T>::to(z[edge]) : 0.f, my_z = id >= 0 ? Vec<T>::to(z[id]) : -INFINITY;
     __syncthreads();
-    if (id >= 0) {
-        for (int k = 0; k < tid; ++k) first = first && ds.id[k] != id;
-        ds.q[tid] = q;
-        if (TAIL && MODE != GRAD && id >= from && id < to) atomicOr(marks + ((id - from) >> 5), 1u << ((id - from) & 31));
-    } else if (tid < K) ds.q[tid] = 0.f;
-    float Q = block_add(q, ds.red);                                    // (and the marks are set)
-    const float qt = TAIL ? fmaxf(0.f, 1.f - Q) : 0.f;
-    const bool any = __syncthreads_or(id >= 0);
-    Q += qt;
+    bool first = id >= 0, again = false;                               // the first entry of its id; there are more
+    if (tid < K) {
+#pragma unroll 4
+        for (int q = 0; q < K; q += 4) {
+            const int4 o = *reinterpret_cast<const int4 *>(ds.id + q);
+            const bool e0 = o.x == id && q != tid, e1 = o.y == id && q + 1 != tid, e2 = o.z == id && q + 2 != tid, e3 = o.w == id && q + 3 != tid;
+            again |= e0 | e1 | e2 | e3;
+            first &= !((e0 && q < tid) | (e1 && q + 1 < tid) | (e2 && q + 2 < tid) | (e3 && q + 3 < tid));
+        }
+        ds.zk[tid] = my_z;
+        ds.first[tid] = first;
+    }
+    const bool here = first && id >= from && id < to;
+    if (marked && here) atomicOr(marks + ((id - from) >> 5), 1u << ((id - from) & 31));
+    __syncthreads();
+    if (tid < 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);
 
-    // log p_v = (z_v - ref) inv_temp - all, of the others among themselves: (z_v - tref) inv_temp - tail
-    float ref, all, tref, tail;
-    const float it = a.t.inv_temp, slack = SLACK / scale;
+    // log2 p_v = (z_v - al.ref) scale - al.m - log2 al.S; of the others among themselves (w_v) the same with ot
+    Sums al, ot;
+    float al2, ot2;                                                    // log2 of their sums
     auto in_list = [&](int i) {
-        for (int k = 0; k < K; ++k)
-            if (ds.id[k] == i) return true;
-        return false;
+        bool in = false;
+        if constexpr (TAIL)
+            for (int k = 0; k < K; ++k) in = in || ds.id[k] == i;
+        return in;
     };
-    auto finish = [&](const Sums &t) {                                 // from the sums of the others (without a tail: of all)
-        ref = tref = t.m;
-        tail = t.S == 0.f ? -INFINITY : log2f(t.S) * LN2;
-        all = tail;
+    auto finish = [&]() {                                              // from the sums of the others (without a tail: of all)
+        ot2 = ot.S == 0.f ? -INFINITY : log2f(ot.S);
+        al = ot;
+        al2 = ot2;
         if (TAIL) {                                                    // and the list's tokens
-            const float top = block_max(first ? zk : -INFINITY, ds.red);
-            if (top > ref) ref = top;
-            const float others = t.S == 0.f ? 0.f : ex2(max_nan(((tref - ref) * it + tail) * LOG2E, FAR));
-            all = log2f(block_add(first ? ex2(max_nan((zk - ref) * scale, FAR)) : 0.f, ds.red) + others) * LN2;
+            const float d = ot.exponent(ds.top, scale);                // their largest over the others' reference
+            if (d > 0.f || ot.S == 0.f) {
+                al.ref = ds.top; al.m = 0.f;
+                al.S = ds.list + (ot.S == 0.f ? 0.f : ex2(max_nan(ot2 - d, FAR)));
+                if (ds.top == -INFINITY) { al.ref = 0.f; al.S = 0.f; }
+            } else al.S = ot.S + ds.list * ex2(max_nan(d, FAR));
+            al2 = al.S == 0.f ? -INFINITY : log2f(al.S);
         }
     };
     if (MODE == GRAD) {
-        ref = tref = 0.f;
-        all = a.lse_in[row];
-        tail = TAIL ? a.tail_in[row] : all;
-        if ((fabsf(all) >= LSE_EXACT && all != -INFINITY) || (fabsf(tail) >= LSE_EXACT && tail != -INFINITY)) {   // (in all blocks alike)
-            finish(whole_row(z, V, scale, ds.sums, [&](int i) { return TAIL && in_list(i); }));
+        __syncthreads();
+        const float lse = a.lse_in[row], tail = TAIL ? a.tail_in[row] : lse;
+        if ((fabsf(lse) >= LSE_EXACT && lse != -INFINITY) || (fabsf(tail) >= LSE_EXACT && tail != -INFINITY)) {   // (in all blocks alike)
+            ot = whole_row<T>(z, V, scale, sl, in_list);
+            finish();
             if (C > 1) barrier_cluster();                              // the gradient may go where the logits are
+        } else {
+            al.ref = ot.ref = 0.f;
+            al2 = lse == -INFINITY ? lse : 0.f;
+            ot2 = tail == -INFINITY ? tail : 0.f;
+            al.m = lse * LOG2E; ot.m = tail * LOG2E;
         }
     } else {
-        PairSums<false> ps;
-        for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
-            uint4 v[UNROLL];
-            ld_batch(sh, j, v);
+        PairSums<T, false> ps;
+        auto hide = [&](uint4 &v, int j) {
+            const int o = j * E - sh.off - from;
+            const uint32_t w = __funnelshift_r(marks[o >> 5], marks[(o >> 5) + 1], o & 31) & ((1u << E) - 1);
+            if (w) Vec<T>::hide(v, w);
+        };
+        each_vec(sh, [&](uint4 (&v)[UNROLL], int j) {
             if (TAIL)
 #pragma unroll
-                for (int u = 0; u < UNROLL; ++u) {
-                    if (j + u * THREADS >= sh.hi) break;
-                    const int o = (j + u * THREADS) * E - sh.off - from;
-                    const uint32_t w = __funnelshift_r(marks[o >> 5], marks[(o >> 5) + 1], o & 31) & ((1u << E) - 1);
-                    if (w) Vec<T>::hide(v[u], w);
-                }
-            ps.reach(Vec<T>::max(v, UNROLL), scale, slack);
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                float f[E];
-                Vec<T>::unpack(v[u], f);
-                ps.add(f, scale);
+                for (int u = 0; u < UNROLL; ++u) hide(v[u], j + u * THREADS);
+            ps.reach(Vec<T>::max(v, UNROLL) * scale);
+            ps.add(v, scale);
+        }, [&](uint4 (&v)[1], int j) {
+            if (TAIL) hide(v[0], j);
+            ps.reach(Vec<T>::max(v, 1) * scale);
+            ps.add(v, scale);
+        });
+        if (edge >= 0 && (!TAIL || !(marks[(edge - from) >> 5] >> ((edge - from) & 31) & 1))) ps.add(at_edge, scale);
+        ot = row_sums<T>(ps.m, ps.S, ps.S2, sh, sl, rank, C, scale, in_list);
+        finish();
+        if (rank == 0 && tid < 32) {
+            const float it = a.t.inv_temp, all = (al.m + al2) * LN2;
+            float loss = 0.f;
+            for (int k = tid; k < K; k += 32) {
+                const float q = ds.q[k];
+                if (q > 0.f || isnan(q)) loss += q * ((ds.tl[k] - ds.norm) * LN2 - ((ds.zk[k] - al.ref) * it - all));
             }
-        }
-        Sums s = ps.sums();
-        if (tid < 2) {
-            const int p = tid ? sh.last : sh.first;
-            if (p >= 0)
-                for (int i = sh.begin(p); i < sh.end(p); ++i)
-                    if (!TAIL || !(marks[(i - from) >> 5] >> ((i - from) & 31) & 1)) s.add(Vec<T>::to(z[i]), scale);
-        }
-        __syncwarp();
-        if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        finish(row_sums(s, ds.sums, rank, C, scale));
-        float loss = block_add(q > 0.f ? q * (lq * LN2 - ((zk - ref) * it - all)) : 0.f, ds.red);
-        if (rank == 0 && tid == 0) {
-            if (TAIL && qt > 0.f) loss += qt * (log2f(qt) * LN2 - ((tref - ref) * it + tail - all));
-            if (a.loss) a.loss[row] = any && all != -INFINITY ? loss : 0.f;
-            // (NO_REF where a finite one is out of range: -inf says that nothing is left)
-            if (a.lse) a.lse[row] = all == -INFINITY ? all : max_nan(ref * it + all, NO_REF);
-            if (TAIL && a.tail_lse) a.tail_lse[row] = tail == -INFINITY ? tail : max_nan(tref * it + tail, NO_REF);
+            loss = warp_add(loss);
+            if (tid == 0) {
+                if (TAIL && ds.qt > 0.f) loss += ds.qt * (log2f(ds.qt) - (ot2 + (ot.ref - al.ref) * scale + (ot.m - al.m) - al2)) * LN2;
+                // (LOWEST where a finite one is out of range: -inf says that nothing is left)
+                if (a.loss) a.loss[row] = ds.any && al2 != -INFINITY ? loss : 0.f;
+                if (a.lse) a.lse[row] = al2 == -INFINITY ? al2 : max_nan(fmaf(al.ref, it, all), LOWEST);
+                if (TAIL && a.tail_lse) a.tail_lse[row] = ot2 == -INFINITY ? ot2 : max_nan(fmaf(ot.ref, it, (ot.m + ot2) * LN2), LOWEST);
+            }
         }
     }
     if (MODE == LOSS) return;
 
     T *out = reinterpret_cast<T *>(a.dz) + (int64_t)row * a.ld_dz;
-    const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15), none = !any || all == -INFINITY;
-    const float g = a.weight[row] * it;
-    const bool others = !none && tail != -INFINITY;
-    const float coef = !others ? 0.f : g * (TAIL ? Q * ex2(max_nan(((tref - ref) * it + tail - all) * LOG2E, FAR)) - qt : Q), off = others ? tail : 0.f;
-    auto grad = [&](float x) { return others ? coef * ex2(((x - tref) * it - off) * LOG2E) : 0.f; };
-    const float c1 = it * LOG2E, c2 = -off * LOG2E;
-    for (int j = sh.lo + tid; j < sh.hi; j += UNROLL * THREADS) {
-        uint4 v[UNROLL];
-        ld_batch(sh, j, v);
+    const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15), none = !ds.any || al2 == -INFINITY, others = !none && ot2 != -INFINITY;
+    const float g = a.weight[row] * a.t.inv_temp;
+    const float coef = !TAIL ? g * ds.Q : g * (ds.Q * ex2(max_nan(ot2 + (ot.ref - al.ref) * scale + (ot.m - al.m) - al2, FAR)) - ds.qt);
+    const float less = ot.m + ot2;
+    const f2 c0 = two(-ot.ref, -ot.ref), c1 = two(scale, scale), c2 = two(-less, -less), c3 = two(coef, coef);
+    auto put = [&](const uint4 &v, int j) {
+        float f[E], d[E];
+        Vec<T>::unpack(v, f);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            if (j + u * THREADS >= sh.hi) break;
-            float f[E], d[E];
-            Vec<T>::unpack(v[u], f);
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                float t0, t1;
-                apart(fma2(add2(two(f[e], f[e + 1]), two(-tref, -tref)), two(c1, c1), two(c2, c2)), t0, t1);
-                apart(mul2(two(ex2(t0), ex2(t1)), two(coef, coef)), d[e], d[e + 1]);
-            }
-            if (!others)
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] = 0.f;
-            st_grad<T>(out, same, j + u * THREADS, sh.off, d);
+        for (int e = 0; e < E; e += 2) {
+            float t0, t1;
+            apart(fma2(add2(two(f[e], f[e + 1]), c0), c1, c2), t0, t1);
+            apart(mul2(two(ex2(t0), ex2(t1)), c3), d[e], d[e + 1]);
         }
-    }
-    if (tid < 2) {
-        const int p = tid ? sh.last : sh.first;
-        if (p >= 0)
-            for (int i = sh.begin(p); i < sh.end(p); ++i) out[i] = Vec<T>::from(grad(Vec<T>::to(z[i])));
-    }
+        if (!others)
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = 0.f;
+        st_grad<T>(out, same, j, sh.off, d);
+    };
+    each_vec(sh, [&](uint4 (&v)[UNROLL], int j) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) put(v[u], j + u * THREADS);
+    }, [&](uint4 (&v)[1], int j) { put(v[0], j); });
+    if (edge >= 0) out[edge] = Vec<T>::from(others ? coef * ex2(fmaf(at_edge - ot.ref, scale, -less)) : 0.f);
     __syncthreads();
-    if (first && id >= from && id < to) {                              // the list's tokens
-        float qs = 0.f;
-        for (int k = tid; k < K; ++k) qs += ds.id[k] == id ? ds.q[k] : 0.f;
-        out[id] = Vec<T>::from(none ? 0.f : g * (Q * ex2(max_nan(((zk - ref) * it - all) * LOG2E, FAR)) - qs));
+    if (here) {                                                        // the list's tokens
+        float qs = ds.q[tid];
+        if (again)
+            for (int k = tid + 1; k < K; ++k) qs += ds.id[k] == id ? ds.q[k] : 0.f;
+        out[id] = Vec<T>::from(none ? 0.f : g * (ds.Q * ex2(max_nan(al.exponent(my_z, scale) - al2, FAR)) - qs));
     }
 }
 
 // ------------------------------------------------------------------ launches
 
-// Blocks per row: enough that rows * C fill the device's block slots, but not less than one batch of loads per thread.
-static int blocks_per_row(int rows, int vocab, int elem) {
-    const int64_t bytes = (int64_t)vocab * elem;
+static int elem_bytes(int dtype) { return dtype == PACER_F32 ? 4 : 2; }
+
+// Blocks per row: more than one while all rows' blocks fit the device at a time and a thread keeps a vector; and, where rows are read
+// twice, while the rows at work (of all SMs) exceed what L2 (126 MB) surely keeps.
+static int blocks_per_row(int rows, int vocab, int elem, bool twice) {
+    const int slots = PER_SM * 148;
+    const double bytes = (double)vocab * elem;
     int C = 1;
-    while (C < MAX_C && (int64_t)rows * C * 2 <= 4 * 148 && bytes / (2 * C) >= THREADS * 16) C *= 2;
+    while (C < MAX_C && (((int64_t)rows * C * 2 <= slots && bytes / (2 * C) >= THREADS * 16) ||
+                         (twice && std::min(rows, slots / C) * bytes > 64e6))) C *= 2;
     return C;
 }
 
-template <class A>
-static cudaError_t launch(void (*k)(const A), const A &a, int rows, int C, size_t smem, cudaStream_t st) {
+template <auto K, class A>
+static cudaError_t launch(const A &a, int rows, int C, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)rows * (unsigned)C);
     c.blockDim = dim3(THREADS);
@@ -901,57 +1036,62 @@ static cudaError_t launch(void (*k)(const A), const A &a, int rows, int C, size_
     at[0].val.clusterDim.x = C; at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     c.attrs = at;
     c.numAttrs = C > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&c, k, a);
+    return cudaLaunchKernelEx(&c, K, a);
 }
 
-static int elem_bytes(int dtype) { return dtype == PACER_F32 ? 4 : 2; }
+// f(a value of the rows' element type)
+template <class F>
+static cudaError_t by_type(int dtype, F f) {
+    return dtype == PACER_F32 ? f(float()) : dtype == PACER_BF16 ? f(__nv_bfloat16()) : f(__half());
+}
 
 cudaError_t logprobs(const Rows &r, const int32_t *tokens, const Window &win, const ScoreOut &out, cudaStream_t st) {
-    const bool top = out.top > 0;
-    ScoreArgs a{r, tokens, win, out, blocks_per_row(r.rows, r.vocab, elem_bytes(r.dtype))};
-    const size_t smem = top ? sizeof(TopSlots) + (size_t)a.C * out.top * 8 : 0;
-    auto go = [&](auto k0, auto k1) { return launch<ScoreArgs>(top ? k1 : k0, a, r.rows, a.C, smem, st); };
-    if (r.dtype == PACER_F32) return go(k_logprobs<float, false>, k_logprobs<float, true>);
-    if (r.dtype == PACER_BF16) return go(k_logprobs<__nv_bfloat16, false>, k_logprobs<__nv_bfloat16, true>);
-    return go(k_logprobs<__half, false>, k_logprobs<__half, true>);
+    const int elem = elem_bytes(r.dtype), C = blocks_per_row(r.rows, r.vocab, elem, false);
+    const int batches = (int)(((int64_t)r.vocab * elem / 16 + 2) / C + BATCH) / BATCH;
+    const ScoreArgs a{r, tokens, win, out, C, std::max(1, (batches + RUNS - 1) / RUNS)};
+    const size_t smem = out.top == 0 ? 0 : RUNS * THREADS * 4 + sizeof(TopSlots) + (size_t)C * out.top * 8;
+    return by_type(r.dtype, [&](auto t) {
+        using T = decltype(t);
+        return out.top > 0 ? launch<k_logprobs<T, true>>(a, r.rows, C, smem, st) : launch<k_logprobs<T, false>>(a, r.rows, C, smem, st);
+    });
 }
 
 cudaError_t logprobs_backward(const Rows &r, const int32_t *tokens, const float *lse, const float *entropy, const float *g_logp,
                               const float *g_entropy, const float *g_lse, void *dz, int64_t ld_dz, cudaStream_t st) {
-    BackArgs a{r, tokens, lse, entropy, g_logp, g_entropy, g_lse, dz, ld_dz, blocks_per_row(r.rows, r.vocab, elem_bytes(r.dtype))};
-    auto go = [&](auto k0, auto k1) { return launch<BackArgs>(g_entropy ? k1 : k0, a, r.rows, a.C, 0, st); };
-    if (r.dtype == PACER_F32) return go(k_logprobs_back<float, false>, k_logprobs_back<float, true>);
-    if (r.dtype == PACER_BF16) return go(k_logprobs_back<__nv_bfloat16, false>, k_logprobs_back<__nv_bfloat16, true>);
-    return go(k_logprobs_back<__half, false>, k_logprobs_back<__half, true>);
+    const int C = blocks_per_row(r.rows, r.vocab, elem_bytes(r.dtype), false);
+    const BackArgs a{r, tokens, lse, entropy, g_logp, g_entropy, g_lse, dz, ld_dz, C};
+    return by_type(r.dtype, [&](auto t) {
+        using T = decltype(t);
+        return g_entropy ? launch<k_logprobs_back<T, true>>(a, r.rows, C, 0, st) : launch<k_logprobs_back<T, false>>(a, r.rows, C, 0, st);
+    });
 }
 
-// A bit for each element of a block's share (at most three vectors more than an even one), and two words of slack.
-static size_t mark_bytes(int vocab, int C) { return ((size_t)(vocab / C + 3 * 8) / 32 + 3) * 4; }
-
-template <class T, int MODE>
-static cudaError_t distill_any(const DistillArgs &a, cudaStream_t st) {
-    const size_t marks = a.t.lse && MODE != GRAD ? mark_bytes(a.r.vocab, a.C) : 0;
-    return launch<DistillArgs>(a.t.lse ? k_distill<T, true, MODE> : k_distill<T, false, MODE>, a, a.r.rows, a.C, marks, st);
-}
 template <int MODE>
-static cudaError_t distill_type(DistillArgs &a, cudaStream_t st) {
-    a.C = blocks_per_row(a.r.rows, a.r.vocab, elem_bytes(a.r.dtype));
-    while (a.t.lse && mark_bytes(a.r.vocab, a.C) > 40 * 1024) a.C *= 2;      // (MAX_VOCAB / MAX_C bits fit)
-    if (a.r.dtype == PACER_F32) return distill_any<float, MODE>(a, st);
-    if (a.r.dtype == PACER_BF16) return distill_any<__nv_bfloat16, MODE>(a, st);
-    return distill_any<__half, MODE>(a, st);
+static cudaError_t distill_mode(DistillArgs &a, cudaStream_t st) {
+    const int elem = elem_bytes(a.r.dtype);
+    int C = blocks_per_row(a.r.rows, a.r.vocab, elem, MODE == LOSS_GRAD);
+    if (a.t.lse)
+        while (a.r.vocab / C > 49152) C *= 2;                          // (the marks stay below 8 KB; MAX_VOCAB / MAX_C is 49152)
+    a.C = C;
+    // (a tail: a bit for each element of the share, which is at most three vectors more than an even one, and words of slack)
+    a.mark_words = a.t.lse && MODE != GRAD ? (a.r.vocab / C + 3 * (16 / elem)) / 32 + 3 : 0;
+    const size_t smem = (size_t)a.mark_words * 4;
+    return by_type(a.r.dtype, [&](auto t) {
+        using T = decltype(t);
+        return a.t.lse ? launch<k_distill<T, true, MODE>>(a, a.r.rows, C, smem, st) : launch<k_distill<T, false, MODE>>(a, a.r.rows, C, smem, st);
+    });
 }
 
 cudaError_t distill(const Rows &r, const Teacher &t, float *loss, float *lse, float *tail_lse, const float *weight, void *dz, int64_t ld_dz,
                     cudaStream_t st) {
-    DistillArgs a{r, t, loss, lse, tail_lse, nullptr, nullptr, weight, dz, ld_dz, 1};
-    return dz ? distill_type<LOSS_GRAD>(a, st) : distill_type<LOSS>(a, st);
+    DistillArgs a{r, t, loss, lse, tail_lse, nullptr, nullptr, weight, dz, ld_dz, 1, 0};
+    return dz ? distill_mode<LOSS_GRAD>(a, st) : distill_mode<LOSS>(a, st);
 }
 
 cudaError_t distill_backward(const Rows &r, const Teacher &t, const float *lse, const float *tail_lse, const float *weight, void *dz,
                              int64_t ld_dz, cudaStream_t st) {
-    DistillArgs a{r, t, nullptr, nullptr, nullptr, lse, tail_lse, weight, dz, ld_dz, 1};
-    return distill_type<GRAD>(a, st);
+    DistillArgs a{r, t, nullptr, nullptr, nullptr, lse, tail_lse, weight, dz, ld_dz, 1, 0};
+    return distill_mode<GRAD>(a, st);
 }
 
 }  // namespace lg

@@ -6,7 +6,7 @@
 namespace lg {
 
 constexpr int MAX_TOP = 128;               // alternatives of a row at most
-constexpr int MAX_VOCAB = 1 << 21, MAX_ROWS = 1 << 24;
+constexpr int MAX_VOCAB = 3 << 17, MAX_ROWS = 1 << 24;
 constexpr int MAX_K = 256;                 // entries of a teacher's list at most
 
 struct Rows {                              // [rows][vocab] with `ld` elements from row to row

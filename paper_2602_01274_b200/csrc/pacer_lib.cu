@@ -951,6 +951,8 @@ extern "C" int pacer_linear_static(const void *x, const void *w, float *y, int r
 
 // ------------------------------------------------------------------ operators on rows of logits
 
+static_assert(lg::MAX_VOCAB == PACER_MAX_VOCAB && lg::MAX_TOP == PACER_MAX_TOP && lg::MAX_K == PACER_MAX_DISTILL_K, "limits of the interface");
+
 // NULL if the rows can be worked on, else what is wrong with them.
 static const char *bad_rows(const void *z, int dtype, int64_t ld, int rows, int vocab) {
     if (dtype != PACER_F32 && dtype != PACER_BF16 && dtype != PACER_F16) return "unknown type of logits";
@@ -1046,7 +1048,7 @@ extern "C" int pacer_distill_backward(const void *logits, int dtype, int64_t ld,
 }
 
 extern "C" size_t pacer_head_logprobs_scratch_bytes(int rows, int vocab) {
-    if (rows < 1 || rows > hs::MAX_ROWS || vocab < 1 || vocab > lg::MAX_VOCAB) return 0;
+    if (rows < 1 || rows > hs::MAX_ROWS || vocab < 1 || vocab > hs::MAX_VOCAB) return 0;
     return hs::scratch_bytes(rows, vocab);
 }
 
@@ -1055,7 +1057,7 @@ extern "C" int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const 
                                    void *scratch, size_t scratch_bytes, void *cuda_stream) {
     pacer_ctx *c = nullptr;
     REFUSE_IF(rows < 0 || rows > hs::MAX_ROWS, "rows out of range");
-    REFUSE_IF(vocab < 1 || vocab > lg::MAX_VOCAB, "vocab out of range");
+    REFUSE_IF(vocab < 1 || vocab > hs::MAX_VOCAB, "vocab out of range");
     REFUSE_IF(d < 8 || d > hs::MAX_D || d % 8, "d out of range or not a multiple of 8");
     REFUSE_IF(ld_hidden < d || ld_hidden % 8 || ld_hidden >> 38 || ld_head < d || ld_head % 8 || ld_head >> 38, "bad row stride");
     if (!rows) return PACER_OK;

@@ -69,13 +69,16 @@ def check_logprobs(z, tokens, top):
     (17, 4096, 0, 0, "f32", 5), (600, 4099, 0, 0, "bf16", 20), (2, 4097, 0, 3, "f32", 64),
     (1, 32000, 0, 0, "bf16", 20), (25, 32256, 0, 0, "f32", 1), (136, 32003, 61, 0, "bf16", 64), (700, 32003, 0, 0, "f16", 20),
     (1, 151936, 0, 0, "f32", 20), (1, 151936, 0, 0, "f32", 128), (33, 151936, 0, 0, "bf16", 128), (3, 151937, 2, 1, "f16", 64),
+    # rows of one warp each
+    (1024, 1, 0, 0, "f32", 1), (1025, 7, 0, 1, "bf16", 7), (2000, 127, 0, 5, "f16", 127), (5000, 300, 3, 0, "f32", 128),
+    (1100, 4099, 61, 0, "bf16", 64), (1024, 32003, 0, 0, "f16", 20), (1500, 2048, 0, 0, "f32", 0), (1030, 70001, 0, 3, "bf16", 128),
 ])
 def test_logprobs(rows, vocab, pad, offset, dtype, top):
     check_logprobs(make_logits(rows, vocab, dtype, pad, offset, seed=vocab + rows), make_tokens(rows, vocab), top)
 
 
-@pytest.mark.parametrize("rows", [1, 40, 600])
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 40, 600, 1100])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_logprobs_of_masked_rows(rows, dtype):
     vocab, top = 32003, 20
     z = make_logits(rows, vocab, dtype, seed=3)
@@ -96,23 +99,24 @@ def test_logprobs_of_masked_rows(rows, dtype):
     check_logprobs(z, tokens, top)
 
 
-@pytest.mark.parametrize("rows,vocab,dtype", [(1, 151936, "f32"), (300, 32000, "bf16")])
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 151936, "f32"), (300, 32000, "bf16"), (1024, 32000, "bf16")])
 def test_alternatives_that_sit_in_few_threads(rows, vocab, dtype):
     """The best elements all in vectors that one thread reads: more candidates than the block keeps at a time."""
     z = make_logits(rows, vocab, dtype, seed=4)
     z[:, :] = z.abs().neg()
     E = 16 // z.element_size()
-    for step in (256 * E, 8 * E):
-        z.view(rows, -1, E)[:, ::max(1, step // E)] += 64.0
-    check_logprobs(z, make_tokens(rows, vocab), 64)
-    z = (torch.arange(vocab, device=DEV) // 50).float().expand(2, vocab).contiguous()      # ascending, ties of 50
-    check_logprobs(z / z.max() * 20, make_tokens(2, vocab), 128)
-    check_logprobs(-z / z.max() * 20, make_tokens(2, vocab), 128)
+    for step in (256, 32, 8):                           # vectors of one thread of a block, of one lane, of an eighth of the threads
+        z.view(rows, -1, E)[:, ::step] += 64.0
+        check_logprobs(z, make_tokens(rows, vocab), 64)
+    z = (torch.arange(vocab, device=DEV) // 50).float().expand(rows, vocab).contiguous()   # ascending, ties of 50
+    check_logprobs(z / z.max() * 20, make_tokens(rows, vocab), 128)
+    check_logprobs(-z / z.max() * 20, make_tokens(rows, vocab), 128)
 
 
-def test_logprobs_of_rows_with_nan_and_inf():
+@pytest.mark.parametrize("rows", [6, 1030])
+def test_logprobs_of_rows_with_nan_and_inf(rows):
     from paper_2602_01274_b200 import binding as b
-    z = make_logits(6, 5000, "f32", seed=5)
+    z = make_logits(rows, 5000, "f32", seed=5)
     z[0, 17] = math.nan
     z[1] = math.nan
     z[2, 4:] = math.nan
@@ -120,7 +124,7 @@ def test_logprobs_of_rows_with_nan_and_inf():
     z[3, 100] = math.inf
     z[4] = -math.inf
     z[4, 3000:] = math.nan
-    tokens = torch.arange(6, dtype=torch.int32, device=DEV)
+    tokens = torch.arange(rows, dtype=torch.int32, device=DEV)
     logp, ent, lse, ids, tlp = b.pacer_logprobs(z, tokens, 100)
     for r in range(5):
         assert torch.isnan(lse[r]) and torch.isnan(ent[r]) and torch.isnan(logp[r]) and torch.isnan(tlp[r]).all()
@@ -128,7 +132,7 @@ def test_logprobs_of_rows_with_nan_and_inf():
         assert ids[r].tolist() == ref.order(z[r], 100), r
     # a row's neighbours are as without it
     one = b.pacer_logprobs(z[5:], tokens[5:], 100)
-    assert torch.equal(one[3], ids[5:]) and torch.isfinite(lse[5])
+    assert torch.equal(one[3], ids[5:]) and torch.isfinite(lse[5:]).all()
 
 
 @pytest.mark.parametrize("rows,vocab,pad,offset,dtype,use", [

@@ -19,7 +19,7 @@ def refused(lib, rc, text):
 LOGITS = [  # changes of (logits, dtype, ld, rows, vocab) and the reason
     (dict(z=None), "logits is null"), (dict(dtype=3), "unknown type"), (dict(dtype=-1), "unknown type"), (dict(ld=99), "ld is less"),
     (dict(rows=-1), "rows out of range"), (dict(rows=(1 << 24) + 1), "rows out of range"), (dict(vocab=0), "vocab out of range"),
-    (dict(vocab=(1 << 21) + 1, ld=1 << 22), "vocab out of range"), (dict(z=A + 2), "misaligned logits"),
+    (dict(vocab=393217, ld=1 << 22), "vocab out of range"), (dict(z=A + 2), "misaligned logits"),
     (dict(z=A + 1, dtype=1), "misaligned logits"),
 ]
 
