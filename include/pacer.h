@@ -312,6 +312,13 @@ enum { PACER_F32 = 0, PACER_BF16 = 1, PACER_F16 = 2 };
 int pacer_logprobs(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens, int top, float *logp,
                    float *entropy, float *lse, int32_t *top_ids, float *top_logp, void *cuda_stream);
 
+/* The same of the verify forward just enqueued (between pacer_verify and the next stage call; else PACER_ESTATE), on the
+ * context's stream, without copying its logits to the host: row j of a sequence holds the target's distribution behind
+ * [last accepted token, y_1 .. y_j], and its token is the draft y_{j+1}; the row behind the last draft has no token (logp 0).
+ * logp, entropy: device f32 [batch][gamma_cap + 1]; top_ids int32, top_logp f32 [batch][gamma_cap + 1][top]; each may be NULL.
+ * Rows past a sequence's window, and sequences that have finished, are left as they were. */
+int pacer_verify_logprobs(pacer_ctx *ctx, int top, float *logp, float *entropy, int32_t *top_ids, float *top_logp);
+
 /* Gradient of the above: dlogits[r][v] = g_logp[r] ([v = token] - p_v) + g_lse[r] p_v - g_entropy[r] p_v (log p_v + entropy[r]),
  * in the logits' type.  lse and entropy: as pacer_logprobs left them.  Each of g_logp, g_entropy, g_lse may be NULL, not all
  * three; tokens may be NULL where g_logp is, entropy where g_entropy is.  A row whose token names nothing has no g_logp term.

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import math
 import os
 import threading
 import weakref
@@ -98,6 +99,7 @@ _lib.pacer_linear_static.argtypes = [_P, _P, _P, C.c_int, C.c_int, C.c_int, _P]
 PACER_LINEAR_STATIC_BYTES = 4 << 20
 _I, _L, _F = C.c_int, C.c_int64, C.c_float
 _lib.pacer_logprobs.argtypes = [_P, _I, _L, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P]
+_lib.pacer_verify_logprobs.argtypes = [_P, _I, _P, _P, _P, _P]
 _lib.pacer_logprobs_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _L, _P]
 _lib.pacer_distill.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P]
 _lib.pacer_distill_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _L, _P]
@@ -119,7 +121,7 @@ def exported_symbols():
             "pacer_accept_rollback", "pacer_read_state", "pacer_read_buffer", "pacer_generate", "pacer_generate_sched",
             "pacer_generate_ar", "pacer_debug_set_device_status",
             "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
-            "pacer_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
+            "pacer_logprobs", "pacer_verify_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
             "pacer_head_logprobs_scratch_bytes", "pacer_head_logprobs"]
 
 
@@ -180,6 +182,7 @@ class Context:
             rc = _lib.pacer_create(C.byref(cfg), self._ws_ptr, nbytes, self.stream.cuda_stream, C.byref(h))
         self._h = h
         self._keep = []
+        self._batch = 1                                             # sequences of the run that pacer_prefill began
         self._check(rc)
 
     def _check(self, rc):
@@ -221,6 +224,7 @@ class Context:
         with torch.cuda.device(self.device):
             self._check(_lib.pacer_prefill(self._h, p.ctypes.data, p.shape[0], p.shape[1], max_new, gamma_max,
                                            threshold, mode, seed))
+        self._batch = p.shape[0]
 
     def pacer_draft_step(self):
         with torch.cuda.device(self.device):
@@ -233,6 +237,21 @@ class Context:
     def pacer_verify(self):
         with torch.cuda.device(self.device):
             self._check(_lib.pacer_verify(self._h))
+
+    def pacer_verify_logprobs(self, top: int = 0):
+        """Between pacer_verify and the next stage call: (logp, entropy f32 [batch][gamma_cap + 1], top_ids int32 and top_logp f32
+        [batch][gamma_cap + 1][top]) of the target's distributions behind every row of the window, on the device.  Row j's token
+        is draft j + 1; rows past a sequence's window are NaN (ids -1)."""
+        rows = (self._batch, self.cfg.gamma_cap + 1)
+        with torch.cuda.device(self.device):
+            logp, entropy = (torch.full(rows, math.nan, device=self.device) for _ in range(2))
+            ids = torch.full((*rows, max(top, 0)), -1, dtype=torch.int32, device=self.device)
+            top_logp = torch.full((*rows, max(top, 0)), math.nan, device=self.device)
+            current = torch.cuda.current_stream(self.device)
+            self.stream.wait_stream(current)                        # the outputs are being filled there
+            self._check(_lib.pacer_verify_logprobs(self._h, top, logp.data_ptr(), entropy.data_ptr(), ids.data_ptr(), top_logp.data_ptr()))
+            current.wait_stream(self.stream)
+        return logp, entropy, ids, top_logp
 
     def pacer_accept_rollback(self):
         with torch.cuda.device(self.device):

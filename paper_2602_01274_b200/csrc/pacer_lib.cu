@@ -39,6 +39,7 @@ struct pacer_ctx {
     int batch;                 // sequences of the current run
     int mode;                  // PACER_GREEDY / PACER_SAMPLE of the current run
     int prefilled;
+    int verified;              // the verify logits and drafts are those of a pacer_verify call just before
     int64_t launches;
     cudaEvent_t ev[4];
     // one draft-and-verify step of Algorithm 1 (every draft forward and pre-verification call of the window, the
@@ -567,6 +568,7 @@ static int start_run(pacer_ctx *c, const int32_t *prompt, int batch, int n_promp
     if (draft_rows < 2) return fail(c, PACER_EINVAL, "prescribed windows: batch too large");
     set_geoms(c, batch, draft_rows);
     c->mode = mode;
+    c->verified = 0;
     std::vector<SeqState> hs(k.max_batch);
     memset(hs.data(), 0, sizeof(SeqState) * hs.size());
     for (int s = 0; s < batch; ++s) {
@@ -641,24 +643,30 @@ extern "C" int pacer_prefill(pacer_ctx *c, const int32_t *prompt, int batch, int
 extern "C" int pacer_draft_step(pacer_ctx *c) {
     int rc = need_ready(c, true);
     if (rc) return rc;
+    c->verified = 0;
     return run_forward(c, PACER_DRAFT, c->g_draft, KIND_DRAFT, 0, true);
 }
 
 extern "C" int pacer_preverify(pacer_ctx *c) {
     int rc = need_ready(c, true);
     if (rc) return rc;
+    c->verified = 0;
     return run_forward(c, PACER_PREVERIFY, c->g_mb, KIND_MB, 0, false);
 }
 
 extern "C" int pacer_verify(pacer_ctx *c) {
     int rc = need_ready(c, true);
     if (rc) return rc;
-    return run_forward(c, PACER_TARGET, c->g_verify, KIND_VERIFY, 0, true);
+    c->verified = 0;
+    if ((rc = run_forward(c, PACER_TARGET, c->g_verify, KIND_VERIFY, 0, true))) return rc;
+    c->verified = 1;
+    return PACER_OK;
 }
 
 extern "C" int pacer_accept_rollback(pacer_ctx *c) {
     int rc = need_ready(c, true);
     if (rc) return rc;
+    c->verified = 0;
     if (c->mode == PACER_SAMPLE) {
         k_lse_parts<<<dim3(2 * c->cfg.gamma_cap + 1, LSE_PARTS, c->batch), LSE_THREADS, 0, c->stream>>>(c->d, c->acc, c->cfg.target.vocab);
         LAUNCH_CHECK();
@@ -987,6 +995,20 @@ extern "C" int pacer_logprobs(const void *logits, int dtype, int64_t ld, int row
     if (!rows) return PACER_OK;
     if (!top_ids && !top_logp) top = 0;
     CK(lg::logprobs({logits, dtype, ld, rows, vocab}, tokens, {}, {logp, entropy, lse, top, top_ids, top_logp}, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+extern "C" int pacer_verify_logprobs(pacer_ctx *c, int top, float *logp, float *entropy, int32_t *top_ids, float *top_logp) {
+    int rc = need_ready(c, true);
+    if (rc) return rc;
+    if (!c->verified) return fail(c, PACER_ESTATE, "pacer_verify_logprobs: not directly after pacer_verify");
+    const int vocab = c->cfg.target.vocab, per = c->cfg.gamma_cap + 1;
+    if (top < 0 || top > PACER_MAX_TOP || top > vocab) return fail(c, PACER_EINVAL, "pacer_verify_logprobs: top out of range");
+    if (vocab > lg::MAX_VOCAB) return fail(c, PACER_EUNSUPPORTED, "pacer_verify_logprobs: vocab exceeds PACER_MAX_VOCAB");
+    if (!top_ids && !top_logp) top = 0;
+    CK(lg::logprobs({c->d.verify_logits, PACER_F32, vocab, c->batch * per, vocab}, nullptr, {c->d.n_rows, c->d.y, per},
+                    {logp, entropy, nullptr, top, top_ids, top_logp}, c->stream));
+    c->launches++;
     return PACER_OK;
 }
 
