@@ -164,18 +164,19 @@ struct Share {
     const T *row;
     int32_t vocab, off, lo, hi, first, last;             // first / last: a partial vector of this block, or -1
 
-    __device__ Share(const T *row_, int vocab_, int rank, int C) : row(row_), vocab(vocab_) {
+    // (2^shift blocks; a division of 64-bit numbers here would cost as much as a quarter of a thread's work on a row)
+    __device__ Share(const T *row_, int vocab_, int rank, int shift) : row(row_), vocab(vocab_) {
         off = (int)(((uintptr_t)row & 15) / sizeof(T));
-        const int nv = (int)(((int64_t)off + vocab + E - 1) / E);
-        lo = (int)((int64_t)nv * rank / C);
-        hi = (int)((int64_t)nv * (rank + 1) / C);
+        const uint32_t ends = (uint32_t)off + (uint32_t)vocab, nv = (ends + E - 1) / E;
+        lo = (int)(nv * (uint32_t)rank >> shift);
+        hi = (int)(nv * (uint32_t)(rank + 1) >> shift);
         first = last = -1;
         if (lo < hi && lo == 0 && (off || vocab < E)) first = lo++;
-        if (lo < hi && hi == nv && ((int64_t)off + vocab) % E) last = --hi;
+        if (lo < hi && hi == (int)nv && ends % E) last = --hi;
     }
     __device__ const uint4 *vecs() const { return reinterpret_cast<const uint4 *>(row - off); }
     __device__ int begin(int j) const { return max(j * E - off, 0); }
-    __device__ int end(int j) const { return (int)min((int64_t)(j + 1) * E - off, (int64_t)vocab); }
+    __device__ int end(int j) const { return min((j + 1) * E - off, vocab); }
     // Elements of the partial vectors, one a thread: its number, or -1.
     __device__ int edge(int tid) const {
         const int j = tid < E ? first : tid < 2 * E ? last : -1, i = j >= 0 ? begin(j) + tid % E : 0;
@@ -191,7 +192,9 @@ __device__ __forceinline__ uint4 ld_row(const uint4 *p) {        // (not the rea
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
-// f(vectors, first vector number) for a thread's vectors lo + tid, lo + tid + THREADS, ..: UNROLL at a time, the last ones one by one.
+// A thread's vectors lo + tid, lo + tid + THREADS, ..: batch(vectors, first number) for UNROLL at a time, single(vector, number) for
+// the last ones, which are loaded together too (one after the other they cost a memory latency each: 263 against 246 us for the
+// loss and gradient of 997 rows of 151 936 f32 with a tail).
 template <class T, class F, class G>
 __device__ __forceinline__ void each_vec(const Share<T> &sh, F batch, G single) {
     int j = sh.lo + threadIdx.x;
@@ -201,10 +204,13 @@ __device__ __forceinline__ void each_vec(const Share<T> &sh, F batch, G single) 
         for (int u = 0; u < UNROLL; ++u) v[u] = ld_row(sh.vecs() + j + u * THREADS);
         batch(v, j);
     }
-    for (; j < sh.hi; j += THREADS) {
-        uint4 v[1] = {ld_row(sh.vecs() + j)};
-        single(v, j);
-    }
+    uint4 v[UNROLL - 1][1];
+#pragma unroll
+    for (int u = 0; u < UNROLL - 1; ++u)
+        if (j + u * THREADS < sh.hi) v[u][0] = ld_row(sh.vecs() + j + u * THREADS);
+#pragma unroll
+    for (int u = 0; u < UNROLL - 1; ++u)
+        if (j + u * THREADS < sh.hi) single(v[u], j + u * THREADS);
 }
 
 // ------------------------------------------------------------------ softmax sums
@@ -346,7 +352,7 @@ __device__ __forceinline__ void block_sums(float &m, float &S, float &S2, SumSlo
 template <class T, class Skip>
 __device__ __noinline__ Sums whole_row(const T *z, int vocab, float scale, SumSlots &sl, Skip skip) {
     constexpr int E = Vec<T>::E;
-    const Share<T> sh(z, vocab, 0, 1);
+    const Share<T> sh(z, vocab, 0, 0);
     float m = LOWEST, S = 0.f, S2 = 0.f;                                 // (m unscaled)
     auto add = [&](float x, int i) {
         if (skip(i)) return;
@@ -613,14 +619,14 @@ struct ScoreArgs {
     const int32_t *tokens;
     Window win;
     ScoreOut out;
-    int32_t C, per;                        // blocks of a row; batches of a run
+    int32_t shift, per;                    // 2^shift blocks of a row; batches of a run
 };
 
 template <class T, bool TOP>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a) {
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ SumSlots sl;
-    const int C = a.C, rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x;
+    const int C = 1 << a.shift, rank = blockIdx.x & (C - 1), row = blockIdx.x >> a.shift, tid = threadIdx.x;
     int token = -1;
     if (a.win.n_rows) {
         const int s = row / a.win.per_seq, j = row - s * a.win.per_seq, n = a.win.n_rows[s];
@@ -632,7 +638,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a)
     TopSlots &ts = *reinterpret_cast<TopSlots *>(seg + RUNS);
     uint64_t *lists = reinterpret_cast<uint64_t *>(&ts + 1);
     const T *z = reinterpret_cast<const T *>(a.r.z) + (int64_t)row * a.r.ld;
-    const Share<T> sh(z, a.r.vocab, rank, C);
+    const Share<T> sh(z, a.r.vocab, rank, a.shift);
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (peers run before their memory is written)
 
     const int edge = sh.edge(tid);
@@ -706,7 +712,7 @@ struct BackArgs {
     const float *lse, *entropy, *g_logp, *g_entropy, *g_lse;
     void *dz;
     int64_t ld_dz;
-    int32_t C;
+    int32_t shift;
 };
 
 // The vector's gradient goes where its logits were, or to a row of another alignment element by element.
@@ -727,10 +733,10 @@ template <class T, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS) k_logprobs_back(const BackArgs a) {
     constexpr int E = Vec<T>::E;
     __shared__ SumSlots sl;
-    const int C = a.C, rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x;
+    const int C = 1 << a.shift, rank = blockIdx.x & (C - 1), row = blockIdx.x >> a.shift, tid = threadIdx.x;
     const T *z = reinterpret_cast<const T *>(a.r.z) + (int64_t)row * a.r.ld;
     T *out = reinterpret_cast<T *>(a.dz) + (int64_t)row * a.ld_dz;
-    const Share<T> sh(z, a.r.vocab, rank, C);
+    const Share<T> sh(z, a.r.vocab, rank, a.shift);
     const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15);
     int token = a.tokens && a.g_logp ? a.tokens[row] : -1;
     if (token >= a.r.vocab) token = -1;
@@ -788,7 +794,7 @@ struct DistillArgs {
     const float *lse_in, *tail_in, *weight;
     void *dz;
     int64_t ld_dz;
-    int32_t C, mark_words;
+    int32_t shift;
 };
 
 struct DistillSlots {
@@ -796,6 +802,7 @@ struct DistillSlots {
     float tl[MAX_K], zk[MAX_K];            // teacher's entry as an exponent (-inf: no entry), student's logit
     float q[MAX_K];
     uint8_t first[MAX_K];                  // 1: the first entry of its id
+    unsigned long long listed[THREADS];    // a tail: which of a thread's vectors hold listed tokens
     float Q, qt, norm, top, list;          // sum q, the rest, log2 of the teacher's sum; largest listed logit, sum 2^((zk - top) scale)
     int32_t any;
 };
@@ -852,21 +859,19 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
 // renormalised (no q_t), or with the teacher's own log-sum-exp, q_t = 1 - sum q then being one class of all other tokens.
 //   dL/dz_v = (p_v Q - sum_{k: id_k = v} q_k) / temperature   for the list's tokens, Q = sum q + q_t
 //   dL/dz_v = w_v (Q p_t - q_t) / temperature                  for the others, w_v = p_v / p_t: their softmax among themselves
-// (without q_t: p_v Q / temperature).  The tail's sum is taken over the tokens outside the list themselves, marked in a bitmap:
-// one minus the list's share would lose it where the student is sure of the list.
+// (without q_t: p_v Q / temperature).  The tail's sum is taken over the tokens outside the list themselves (a thread knows its
+// vectors with listed tokens): one minus the list's share would lose it where the student is sure of the list.
 // The gradient of all others is written first, the list's tokens are put right after it.
 template <class T, bool TAIL, int MODE>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a) {
     constexpr int E = Vec<T>::E;
-    extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ DistillSlots ds;
     __shared__ SumSlots sl;
-    const int C = a.C, rank = blockIdx.x % C, row = blockIdx.x / C, tid = threadIdx.x, V = a.r.vocab, K = a.t.k;
+    const int C = 1 << a.shift, rank = blockIdx.x & (C - 1), row = blockIdx.x >> a.shift, tid = threadIdx.x, V = a.r.vocab, K = a.t.k;
     const T *z = reinterpret_cast<const T *>(a.r.z) + (int64_t)row * a.r.ld;
-    const Share<T> sh(z, V, rank, C);
+    const Share<T> sh(z, V, rank, a.shift);
     const float scale = LOG2E * a.t.inv_temp;
     constexpr bool marked = TAIL && MODE != GRAD;
-    uint32_t *marks = reinterpret_cast<uint32_t *>(dyn);               // a bit for each element of the share
     if (C > 1 && MODE != GRAD) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // (peers run before their memory is written)
 
     // the list: entry tid
@@ -878,8 +883,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         ds.id[tid] = id;
         ds.tl[tid] = id >= 0 ? load_any(a.t.t, (int64_t)row * K + tid, a.t.dtype) * scale : -INFINITY;
     } else if (tid < K + 4) ds.id[tid] = -1;                           // (ids are compared four at a time)
-    if (marked)
-        for (int i = tid; i < a.mark_words; i += THREADS) marks[i] = 0;
+    if (marked) ds.listed[tid] = 0;
     const float at_edge = edge >= 0 ? Vec<T>::to(z[edge]) : 0.f, my_z = id >= 0 ? Vec<T>::to(z[id]) : -INFINITY;
     __syncthreads();
     bool first = id >= 0, again = false;                               // the first entry of its id; there are more
@@ -895,7 +899,10 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         ds.first[tid] = first;
     }
     const bool here = first && id >= from && id < to;
-    if (marked && here) atomicOr(marks + ((id - from) >> 5), 1u << ((id - from) & 31));
+    if (marked && here) {
+        const int i = (id + sh.off) / E - sh.lo;                       // its vector of the share
+        if (i >= 0 && i < sh.hi - sh.lo) atomicOr(ds.listed + i % THREADS, 1ull << i / THREADS);
+    }
     __syncthreads();
     if (tid < 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);
 
@@ -937,23 +944,37 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         }
     } else {
         PairSums<T, false> ps;
-        auto hide = [&](uint4 &v, int j) {
-            const int o = j * E - sh.off - from;
-            const uint32_t w = __funnelshift_r(marks[o >> 5], marks[(o >> 5) + 1], o & 31) & ((1u << E) - 1);
-            if (w) Vec<T>::hide(v, w);
+        auto which = [&](int i0, int n) {                              // a bit for each listed token of i0 .. i0 + n - 1
+            uint32_t w = 0;
+            for (int q = 0; q < K; q += 4) {
+                const int4 o = *reinterpret_cast<const int4 *>(ds.id + q);
+                w |= (uint32_t)(o.x - i0) < (uint32_t)n ? 1u << (o.x - i0) : 0u;
+                w |= (uint32_t)(o.y - i0) < (uint32_t)n ? 1u << (o.y - i0) : 0u;
+                w |= (uint32_t)(o.z - i0) < (uint32_t)n ? 1u << (o.z - i0) : 0u;
+                w |= (uint32_t)(o.w - i0) < (uint32_t)n ? 1u << (o.w - i0) : 0u;
+            }
+            return w;
         };
+        unsigned long long listed = TAIL ? ds.listed[tid] : 0;
         each_vec(sh, [&](uint4 (&v)[UNROLL], int j) {
-            if (TAIL)
+            if (TAIL) {
+                if (listed & ((1u << UNROLL) - 1))
 #pragma unroll
-                for (int u = 0; u < UNROLL; ++u) hide(v[u], j + u * THREADS);
+                    for (int u = 0; u < UNROLL; ++u)
+                        if (listed >> u & 1) Vec<T>::hide(v[u], which((j + u * THREADS) * E - sh.off, E));
+                listed >>= UNROLL;
+            }
             ps.reach(Vec<T>::max(v, UNROLL) * scale);
             ps.add(v, scale);
         }, [&](uint4 (&v)[1], int j) {
-            if (TAIL) hide(v[0], j);
+            if (TAIL) {
+                if (listed & 1) Vec<T>::hide(v[0], which(j * E - sh.off, E));
+                listed >>= 1;
+            }
             ps.reach(Vec<T>::max(v, 1) * scale);
             ps.add(v, scale);
         });
-        if (edge >= 0 && (!TAIL || !(marks[(edge - from) >> 5] >> ((edge - from) & 31) & 1))) ps.add(at_edge, scale);
+        if (edge >= 0 && (!TAIL || !which(edge, 1))) ps.add(at_edge, scale);
         ot = row_sums<T>(ps.m, ps.S, ps.S2, sh, sl, rank, C, scale, in_list);
         finish();
         if (rank == 0 && tid < 32) {
@@ -1014,20 +1035,22 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
 static int elem_bytes(int dtype) { return dtype == PACER_F32 ? 4 : 2; }
 
 // Blocks per row: more than one while all rows' blocks fit the device at a time and a thread keeps a vector; and, where rows are read
-// twice, while the rows at work (of all SMs) exceed what L2 (126 MB) surely keeps.
-static int blocks_per_row(int rows, int vocab, int elem, bool twice) {
+// twice, while the rows at work (of all SMs) exceed what L2 (126 MB) surely keeps: 997 rows of 151 936 f32, loss and gradient, took
+// 257 us with eight blocks a row (56 MB at work), 288 us with four (112 MB).
+static int blocks_per_row_log2(int rows, int vocab, int elem, bool twice) {
     const int slots = PER_SM * 148;
     const double bytes = (double)vocab * elem;
-    int C = 1;
-    while (C < MAX_C && (((int64_t)rows * C * 2 <= slots && bytes / (2 * C) >= THREADS * 16) ||
-                         (twice && std::min(rows, slots / C) * bytes > 64e6))) C *= 2;
-    return C;
+    int shift = 0;
+    while (1 << shift < MAX_C && (((int64_t)rows << (shift + 1) <= slots && bytes / (2 << shift) >= THREADS * 16) ||
+                                  (twice && std::min(rows, slots >> shift) * bytes > 64e6))) ++shift;
+    return shift;
 }
 
 template <auto K, class A>
-static cudaError_t launch(const A &a, int rows, int C, size_t smem, cudaStream_t st) {
+static cudaError_t launch(const A &a, size_t smem, cudaStream_t st) {
+    const int C = 1 << a.shift;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3((unsigned)rows * (unsigned)C);
+    c.gridDim = dim3((unsigned)a.r.rows * (unsigned)C);
     c.blockDim = dim3(THREADS);
     c.dynamicSmemBytes = smem;
     c.stream = st;
@@ -1046,51 +1069,46 @@ static cudaError_t by_type(int dtype, F f) {
 }
 
 cudaError_t logprobs(const Rows &r, const int32_t *tokens, const Window &win, const ScoreOut &out, cudaStream_t st) {
-    const int elem = elem_bytes(r.dtype), C = blocks_per_row(r.rows, r.vocab, elem, false);
-    const int batches = (int)(((int64_t)r.vocab * elem / 16 + 2) / C + BATCH) / BATCH;
-    const ScoreArgs a{r, tokens, win, out, C, std::max(1, (batches + RUNS - 1) / RUNS)};
-    const size_t smem = out.top == 0 ? 0 : RUNS * THREADS * 4 + sizeof(TopSlots) + (size_t)C * out.top * 8;
+    const int elem = elem_bytes(r.dtype), shift = blocks_per_row_log2(r.rows, r.vocab, elem, false);
+    const int batches = ((r.vocab * elem / 16 + 2 >> shift) + BATCH) / BATCH;
+    const ScoreArgs a{r, tokens, win, out, shift, std::max(1, (batches + RUNS - 1) / RUNS)};
+    const size_t smem = out.top == 0 ? 0 : RUNS * THREADS * 4 + sizeof(TopSlots) + ((size_t)out.top * 8 << shift);
     return by_type(r.dtype, [&](auto t) {
         using T = decltype(t);
-        return out.top > 0 ? launch<k_logprobs<T, true>>(a, r.rows, C, smem, st) : launch<k_logprobs<T, false>>(a, r.rows, C, smem, st);
+        return out.top > 0 ? launch<k_logprobs<T, true>>(a, smem, st) : launch<k_logprobs<T, false>>(a, smem, st);
     });
 }
 
 cudaError_t logprobs_backward(const Rows &r, const int32_t *tokens, const float *lse, const float *entropy, const float *g_logp,
                               const float *g_entropy, const float *g_lse, void *dz, int64_t ld_dz, cudaStream_t st) {
-    const int C = blocks_per_row(r.rows, r.vocab, elem_bytes(r.dtype), false);
-    const BackArgs a{r, tokens, lse, entropy, g_logp, g_entropy, g_lse, dz, ld_dz, C};
+    const BackArgs a{r, tokens, lse, entropy, g_logp, g_entropy, g_lse, dz, ld_dz, blocks_per_row_log2(r.rows, r.vocab, elem_bytes(r.dtype), false)};
     return by_type(r.dtype, [&](auto t) {
         using T = decltype(t);
-        return g_entropy ? launch<k_logprobs_back<T, true>>(a, r.rows, C, 0, st) : launch<k_logprobs_back<T, false>>(a, r.rows, C, 0, st);
+        return g_entropy ? launch<k_logprobs_back<T, true>>(a, 0, st) : launch<k_logprobs_back<T, false>>(a, 0, st);
     });
 }
 
 template <int MODE>
 static cudaError_t distill_mode(DistillArgs &a, cudaStream_t st) {
     const int elem = elem_bytes(a.r.dtype);
-    int C = blocks_per_row(a.r.rows, a.r.vocab, elem, MODE == LOSS_GRAD);
-    if (a.t.lse)
-        while (a.r.vocab / C > 49152) C *= 2;                          // (the marks stay below 8 KB; MAX_VOCAB / MAX_C is 49152)
-    a.C = C;
-    // (a tail: a bit for each element of the share, which is at most three vectors more than an even one, and words of slack)
-    a.mark_words = a.t.lse && MODE != GRAD ? (a.r.vocab / C + 3 * (16 / elem)) / 32 + 3 : 0;
-    const size_t smem = (size_t)a.mark_words * 4;
+    a.shift = blocks_per_row_log2(a.r.rows, a.r.vocab, elem, MODE == LOSS_GRAD);
+    // (a tail: a thread has a bit for each of its vectors, 64 at most; MAX_VOCAB f32 over MAX_C blocks are 48)
+    while (a.t.lse && (a.r.vocab * elem / 16 + 2 >> a.shift) + 1 > 64 * THREADS) ++a.shift;
     return by_type(a.r.dtype, [&](auto t) {
         using T = decltype(t);
-        return a.t.lse ? launch<k_distill<T, true, MODE>>(a, a.r.rows, C, smem, st) : launch<k_distill<T, false, MODE>>(a, a.r.rows, C, smem, st);
+        return a.t.lse ? launch<k_distill<T, true, MODE>>(a, 0, st) : launch<k_distill<T, false, MODE>>(a, 0, st);
     });
 }
 
 cudaError_t distill(const Rows &r, const Teacher &t, float *loss, float *lse, float *tail_lse, const float *weight, void *dz, int64_t ld_dz,
                     cudaStream_t st) {
-    DistillArgs a{r, t, loss, lse, tail_lse, nullptr, nullptr, weight, dz, ld_dz, 1, 0};
+    DistillArgs a{r, t, loss, lse, tail_lse, nullptr, nullptr, weight, dz, ld_dz, 0};
     return dz ? distill_mode<LOSS_GRAD>(a, st) : distill_mode<LOSS>(a, st);
 }
 
 cudaError_t distill_backward(const Rows &r, const Teacher &t, const float *lse, const float *tail_lse, const float *weight, void *dz,
                              int64_t ld_dz, cudaStream_t st) {
-    DistillArgs a{r, t, nullptr, nullptr, nullptr, lse, tail_lse, weight, dz, ld_dz, 1, 0};
+    DistillArgs a{r, t, nullptr, nullptr, nullptr, lse, tail_lse, weight, dz, ld_dz, 0};
     return distill_mode<GRAD>(a, st);
 }
 
