@@ -2,10 +2,10 @@
 // the logit of one token.  The logits are never written: [rows][vocab] f32 would be 262 MB for 2048 rows of 32 000.
 //
 // Many rows are bound by the tensor cores (2 rows vocab d operations), few by reading the head once.  One kernel does both: tiles
-// of 128 rows x up to 256 tokens on tcgen05, operands by tensor copies in the 128-byte swizzle, four stages of 48 KB, two accumulators
-// so that a tile's epilogue runs under the next tile's products.  With few rows the 128-row operand is mostly unused, but the
-// tensor cores are not what bounds: a 256-token tile takes 64 cycles per 16 columns and 8 KB of weights, 128 bytes a cycle and
-// SM, five times what HBM delivers.
+// of 128 rows (256 by a pair of blocks) x up to 256 tokens on tcgen05, operands by tensor copies in the 128-byte swizzle, 192 KB of
+// stages, two accumulators so that a tile's epilogue runs under the next tile's products.  With few rows the 128-row operand is
+// mostly unused, but the tensor cores are not what bounds: a 256-token tile takes 128 cycles per 16 columns and 8 KB of weights, 64
+// bytes a cycle and SM, nearly three times what HBM delivers (25 rows x 32 256 x 7168: 76 us, 92 % of the measured copy rate).
 // The tensor cores truncate when they add to an accumulator: the products over 512 columns are taken out and added in ordinary
 // fp32 (registers of the epilogue's threads) while the next 512 run into the other accumulator.  With one accumulator over all of
 // 7168 columns the results were 2.3e-6 off a 64-bit product's, relative, and 1.2e-7 with segments.
@@ -23,9 +23,14 @@ namespace hs {
 
 using namespace fwd;
 
-constexpr int TM = 128, TN = 256, STAGES_H = 4, A_BYTES = TM * 128, B_BYTES = TN * 128, STAGE = A_BYTES + B_BYTES;
+constexpr int TM = 128, TN = 256, A_BYTES = TM * 128;
+// PAIR: two blocks of a cluster work on 256 rows, each with its 128 of them and half of the tile's tokens in shared memory.
+template <bool PAIR> struct Cfg {
+    static constexpr int B_BYTES = (PAIR ? TN / 2 : TN) * 128, STAGE = A_BYTES + B_BYTES, STAGES = PAIR ? 6 : 4;
+};
 constexpr int SEG = 8;                     // k blocks of 64 columns accumulated inside the tensor cores
-constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = STAGES_H * STAGE + 1024;
+constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = 192 * 1024 + 1024;
+static_assert(Cfg<true>::STAGE * Cfg<true>::STAGES == 192 * 1024 && Cfg<false>::STAGE * Cfg<false>::STAGES == 192 * 1024, "the stages");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_REF = -3.402823466e38f, SLACK = 11.f, FAR = -1000.f;
 constexpr float OUTSIDE = -1e30f;          // a logit past the vocabulary: 2^t is 0, and t finite
@@ -45,9 +50,35 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar, uint64_t policy) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
-                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)), "l"(policy) : "memory");
+// bar: a shared::cluster address; with PAIR that of the pair's first block.
+template <bool PAIR>
+__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar, uint64_t policy) {
+    if (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint32_t first_block(const void *smem) {      // the address of the pair's first block
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(smem)), "r"(0));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// As umma_if and umma_commit_if for both blocks' operands, accumulators and barriers; issued by the first block.
+__device__ __forceinline__ void umma2_if(uint32_t on, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
+}
+__device__ __forceinline__ void umma2_commit_if(uint32_t on, uint64_t *bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
+                 ::"r"(smem_u32(bar)), "r"(on), "h"((uint16_t)3) : "memory");
 }
 // Bounded wait; one that runs out ends the block's work (its rows become NaN).
 __device__ __forceinline__ bool wait_h(volatile int32_t *gave_up, uint64_t *bar, uint32_t parity) {
@@ -76,27 +107,36 @@ struct Run {                               // a thread's running sums
 // Persistent: block b computes the tiles b, b + grid, ...; row tiles vary fastest, so that the blocks that run together share
 // their weights in L2.  Warps 0..7 epilogues (warp w reads accumulator lanes 32 (w % 4) .., the first or second half of the
 // tile's tokens), warp 8 copies, warp 9 tensor cores.
+template <bool PAIR>
 __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                              const KArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ uint64_t full[STAGES_H], empty[STAGES_H], acc_full[2], acc_empty[2];
+    constexpr int STAGES = Cfg<PAIR>::STAGES, STAGE = Cfg<PAIR>::STAGE;
+    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int32_t gave_up;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    unsigned char *smem = smem_raw + (-(int)smem_u32(smem_raw) & 1023);
+    unsigned char *smem = smem_raw + (-(int)smem_u32(smem_raw) & 1023);      // (the same in both blocks of a pair)
+    const int rank = PAIR ? blockIdx.x & 1 : 0, worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (int i = 0; i < STAGES_H; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, EPI_WARPS); }
+        for (int i = 0; i < STAGES; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, PAIR ? 2 * EPI_WARPS : EPI_WARPS); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async();
     }
     if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     tc_fence_before();
     __syncthreads();
+    if (PAIR) cluster_sync();                                          // (both blocks' barriers are set up)
     tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = tmem_slot;
@@ -110,54 +150,60 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
             else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(stream));
             int n = 0;
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-                const int r0 = (t % a.mt) * TM, n0 = (t / a.mt) * a.bn;
+            for (int t = worker; t < tiles && ok; t += workers) {
+                const int r0 = (t % a.mt) * (PAIR ? 2 * TM : TM) + rank * TM, n0 = (t / a.mt) * a.bn + (PAIR ? rank * (a.bn >> 1) : 0);
                 for (int kb = 0; kb < a.nkb; ++kb, ++n) {
-                    const int slot = n % STAGES_H;
-                    ok = wait_h(&gave_up, empty + slot, (((uint32_t)(n / STAGES_H)) & 1u) ^ 1u);
+                    const int slot = n % STAGES;
+                    ok = wait_h(&gave_up, empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
                     if (!ok) break;
                     unsigned char *st = smem + slot * STAGE;
-                    mbar_expect_tx(full + slot, (uint32_t)(a.a_rows + a.bn) * 128u);
-                    tma_2d(st, &map_a, kb * 64, r0, full + slot, keep);
-                    tma_2d(st + A_BYTES, &map_b, kb * 64, n0, full + slot, stream);
+                    if (rank == 0) mbar_expect_tx(full + slot, (uint32_t)(PAIR ? 2 * a.a_rows + a.bn : a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
+                    const uint32_t bar = PAIR ? first_block(full + slot) : smem_u32(full + slot);
+                    tma_2d<PAIR>(st, &map_a, kb * 64, r0, bar, keep);
+                    tma_2d<PAIR>(st + A_BYTES, &map_b, kb * 64, n0, bar, stream);
                 }
             }
-            for (int j = max(0, n - STAGES_H); j < n; ++j)            // no copy may be in flight when the block ends
-                for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(full + j % STAGES_H, ((uint32_t)(j / STAGES_H)) & 1u); ++it) {}
+            // no copy may be in flight when the block ends (a pair's arrive at its first block's barriers; the second ends after it)
+            for (int j = max(0, n - STAGES); j < n && rank == 0; ++j)
+                for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
         }
     } else if (warp == 9) {
-        const uint32_t on = elect_lane(), idesc = umma_idesc(a.bn);  // (all lanes wait, one issues)
+        // (all lanes wait, one issues; of a pair the first block's)
+        const uint32_t on = elect_lane(), idesc = PAIR ? (umma_idesc(a.bn) & ~(31u << 24)) | (256u >> 4) << 24 : umma_idesc(a.bn);
         int n = 0, i = 0;
         bool ok = true;
-        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++i) {
+        for (int t = worker; t < tiles && ok && rank == 0; t += workers, ++i) {
             for (int kb = 0; kb < a.nkb; ++kb, ++n) {
                 if (kb % SEG == 0) {
-                    if (kb) { umma_commit_if(on, acc_full + (i & 1)); ++i; }
+                    if (kb) { PAIR ? umma2_commit_if(on, acc_full + (i & 1)) : umma_commit_if(on, acc_full + (i & 1)); ++i; }
                     ok = __all_sync(0xffffffffu, wait_h(&gave_up, acc_empty + (i & 1), (((uint32_t)(i >> 1)) & 1u) ^ 1u));
                     if (!ok) break;
                 }
                 const uint32_t acc = tmem + (uint32_t)(i & 1) * 256u;
-                const int slot = n % STAGES_H;
-                ok = __all_sync(0xffffffffu, wait_h(&gave_up, full + slot, ((uint32_t)(n / STAGES_H)) & 1u));
+                const int slot = n % STAGES;
+                ok = __all_sync(0xffffffffu, wait_h(&gave_up, full + slot, ((uint32_t)(n / STAGES)) & 1u));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t a0 = smem_u32(smem + slot * STAGE), b0 = a0 + A_BYTES;
 #pragma unroll
-                for (int k16 = 0; k16 < 4; ++k16)
-                    umma_if(on, acc, umma_desc(a0 + k16 * 32), umma_desc(b0 + k16 * 32), idesc, (kb % SEG > 0 || k16 > 0) ? 1u : 0u);
-                umma_commit_if(on, empty + slot);
+                for (int k16 = 0; k16 < 4; ++k16) {
+                    const uint64_t da = umma_desc(a0 + k16 * 32), db = umma_desc(b0 + k16 * 32);
+                    const uint32_t add = (kb % SEG > 0 || k16 > 0) ? 1u : 0u;
+                    PAIR ? umma2_if(on, acc, da, db, idesc, add) : umma_if(on, acc, da, db, idesc, add);
+                }
+                PAIR ? umma2_commit_if(on, empty + slot) : umma_commit_if(on, empty + slot);
             }
-            if (ok) umma_commit_if(on, acc_full + (i & 1));
+            if (ok) PAIR ? umma2_commit_if(on, acc_full + (i & 1)) : umma_commit_if(on, acc_full + (i & 1));
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;
         const int chunks = (a.bn + 31) >> 5, c0 = half ? (chunks + 1) >> 1 : 0, c1 = half ? chunks : (chunks + 1) >> 1;
         int i = 0;                                                    // segments so far
         bool ok = true;                                               // (once a wait has given up, the tiles left become NaN)
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+        for (int t = worker; t < tiles; t += workers) {
             const int m = t % a.mt, nti = t / a.mt, n0 = nti * a.bn, width = min(a.bn, a.vocab - n0);
-            const int r = m * TM + quad * 32 + lane;
-            const bool live = r < a.rows, reads = m * TM + quad * 32 < a.rows;      // (a warp without rows has nothing to read)
+            const int rq = m * (PAIR ? 2 * TM : TM) + rank * TM + quad * 32, r = rq + lane;
+            const bool live = r < a.rows, reads = rq < a.rows;      // (a warp without rows has nothing to read)
             const int tok = live && a.tokens ? a.tokens[r] - n0 : -1, bid = live && a.bias_ids ? a.bias_ids[r] - n0 : -1;
             float z[4][32];                                           // this thread's logits: row r, tokens n0 + 32 (c0 + ..)
             for (int kb = 0; kb < a.nkb && ok; kb += SEG, ++i) {
@@ -175,7 +221,10 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                         }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty + (i & 1));      // the next products may overwrite the accumulator
+                if (lane == 0) {                                      // the next products may overwrite the accumulator
+                    if (PAIR) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(acc_empty + (i & 1))) : "memory");
+                    else mbar_arrive(acc_empty + (i & 1));
+                }
             }
             Run s;
             if (ok && reads)
@@ -219,7 +268,11 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (PAIR) cluster_sync();                                          // (nothing of one block is in use by the other)
+    if (warp == 9) {
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
 }
 
 // One warp per row joins its parts.
@@ -250,21 +303,25 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
 }
 
 // Tokens of a tile: the width with the least waves x (time of a tile), counted in tokens; a tile has a fixed cost of about 16.
-static int tile_width(int mt, int vocab, int n_sm) {
+static int tile_width(int mt, int vocab, int n_sm, int step) {
     int best = TN;
     int64_t best_cost = INT64_MAX;
-    for (int w = TN; w >= 32; w -= 16) {
+    for (int w = TN; w >= 32; w -= step) {
         const int64_t tiles = (int64_t)mt * ((vocab + w - 1) / w), cost = (tiles + n_sm - 1) / n_sm * (w + 16);
         if (cost < best_cost) { best_cost = cost; best = w; }
     }
     return best;
 }
 
-struct Tiles { int mt, bn, nt; };
+struct Tiles { int pair, mt, bn, nt; };
+// Pairs of blocks where that leaves few rows empty: they read a third less out of L2, and the power cap leaves them a higher clock
+// for it (2048 rows x 32 000 x 4096: 4.9 GB and 415 us, tensor pipe 91 % active; by single blocks 7.1 GB and 474 us).
 static Tiles tiles_of(int rows, int vocab) {
     Tiles t;
-    t.mt = (rows + TM - 1) / TM;
-    t.bn = tile_width(t.mt, vocab, 148);
+    const int m128 = (rows + TM - 1) / TM;
+    t.pair = m128 % 2 == 0 || m128 >= 9;
+    t.mt = t.pair ? (m128 + 1) / 2 : m128;
+    t.bn = tile_width(t.mt, vocab, t.pair ? 74 : 148, t.pair ? 32 : 16);      // (a pair's product takes tokens by 32)
     t.nt = (vocab + t.bn - 1) / t.bn;
     return t;
 }
@@ -300,7 +357,8 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
         encode = reinterpret_cast<EncodeFn>(fn);
     }
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-        e = cudaFuncSetAttribute(k_head_score, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        e = cudaFuncSetAttribute(k_head_score<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
@@ -312,12 +370,21 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     k.part = reinterpret_cast<Part *>(scratch);
     k.ztok = reinterpret_cast<float *>(k.part + (size_t)a.rows * (2 * t.nt));
     CUtensorMap ma, mb;
-    if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, k.a_rows) || !make_map(encode, &mb, a.head, a.ld_head, a.vocab, a.d, t.bn)) {
+    if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, k.a_rows) || !make_map(encode, &mb, a.head, a.ld_head, a.vocab, a.d, t.pair ? t.bn / 2 : t.bn)) {
         *no_maps = true;
         return cudaSuccess;
     }
-    k_head_score<<<std::min((int64_t)n_sm, (int64_t)t.mt * t.nt), THREADS_H, SMEM_H, st>>>(ma, mb, k);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t m = {};
+    m.gridDim = dim3((unsigned)std::min((int64_t)(t.pair ? n_sm / 2 : n_sm), (int64_t)t.mt * t.nt) * (t.pair ? 2 : 1));
+    m.blockDim = dim3(THREADS_H);
+    m.dynamicSmemBytes = SMEM_H;
+    m.stream = st;
+    cudaLaunchAttribute two[1];
+    two[0].id = cudaLaunchAttributeClusterDimension;
+    two[0].val.clusterDim.x = 2; two[0].val.clusterDim.y = two[0].val.clusterDim.z = 1;
+    m.attrs = two;
+    m.numAttrs = t.pair ? 1 : 0;
+    e = t.pair ? cudaLaunchKernelEx(&m, k_head_score<true>, ma, mb, k) : cudaLaunchKernelEx(&m, k_head_score<false>, ma, mb, k);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)((a.rows + 3) / 4));
