@@ -293,7 +293,7 @@ int pacer_linear_static(const void *x, const void *w, float *y, int rows, int N,
 
 /* Operators on rows of logits: what a server returns beside the tokens, what a scoring program needs, and the loss that
  * trains a draft model towards its target.  logits: device, [rows][vocab] of type dtype (PACER_F32 / _BF16 / _F16) with ld >=
- * vocab elements from row to row (any ld and any element-aligned address; whole 16-byte pieces are moved at a time where rows of
+ * vocab elements from row to row (any ld below 2^36 and any element-aligned address; whole 16-byte pieces are moved at a time where rows of
  * input and output lie alike modulo 16 bytes).  rows <= 2^24, vocab <= PACER_MAX_VOCAB; rows = 0 does nothing.  All other arrays are device,
  * contiguous, f32 or int32 as declared.  Sums and statistics are fp32.  A logit of -inf has probability 0; a row of -inf only has lse -inf,
  * every log probability -inf, entropy 0 and gradient 0; a NaN or +inf logit makes the results of its row NaN.  The calls enqueue
@@ -322,7 +322,7 @@ int pacer_verify_logprobs(pacer_ctx *ctx, int top, float *logp, float *entropy, 
 /* Gradient of the above: dlogits[r][v] = g_logp[r] ([v = token] - p_v) + g_lse[r] p_v - g_entropy[r] p_v (log p_v + entropy[r]),
  * in the logits' type.  lse and entropy: as pacer_logprobs left them.  Each of g_logp, g_entropy, g_lse may be NULL, not all
  * three; tokens may be NULL where g_logp is, entropy where g_entropy is.  A row whose token names nothing has no g_logp term.
- * dlogits may be the logits themselves (same ld). */
+ * dlogits may be the logits themselves (same address and ld), else the two must not overlap. */
 int pacer_logprobs_backward(const void *logits, int dtype, int64_t ld, int rows, int vocab, const int32_t *tokens, const float *lse,
                             const float *entropy, const float *g_logp, const float *g_entropy, const float *g_lse, void *dlogits,
                             int64_t ld_dlogits, void *cuda_stream);

@@ -107,6 +107,7 @@ _lib.pacer_head_logprobs_scratch_bytes.restype = C.c_size_t
 _lib.pacer_head_logprobs_scratch_bytes.argtypes = [_I, _I]
 _lib.pacer_head_logprobs.argtypes = [_P, _L, _P, _L, _I, _I, _I, _P, _P, _F, _P, _P, _P, _P, C.c_size_t, _P]
 PACER_F32, PACER_BF16, PACER_F16 = 0, 1, 2
+PACER_MAX_VOCAB = 393216
 _DTYPES = {torch.float32: PACER_F32, torch.bfloat16: PACER_BF16, torch.float16: PACER_F16}
 
 
@@ -422,7 +423,8 @@ def _gradient_like(z: torch.Tensor) -> torch.Tensor:
 def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
     if out is None:
         return _gradient_like(z)
-    assert out.device == z.device and out.dtype == z.dtype and out.shape == z.shape and out.stride(1) == 1, "out: like the logits"
+    assert out.device == z.device and out.dtype == z.dtype and out.shape == z.shape and out.stride(1) == 1 and \
+        (out.shape[0] <= 1 or out.stride(0) >= out.shape[1]), "out: like the logits, rows apart"
     return out
 
 
@@ -498,7 +500,7 @@ def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, t
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
     weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
     loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, weight.data_ptr(),
+    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, _ptr(weight),
           out.data_ptr(), max(out.stride(0), z.shape[1]))
     return loss, out
 

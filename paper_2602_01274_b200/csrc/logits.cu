@@ -28,7 +28,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_REF = -3.402823466e38f, LOWEST = NO_REF, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
 constexpr float HUGE_M = 1e8f;
-constexpr float LSE_EXACT = 65536.f;       // beyond it an f32 log-sum-exp no longer tells the logits of a row apart
+constexpr float LSE_EXACT = 1024.f;        // a larger f32 log-sum-exp says a row's probabilities to less than 3e-5: it is taken anew
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -840,12 +840,13 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
         for (int k = lane; k < K; k += 32) sum += ex2(ds.tl[k] - ref);
         norm = ref + log2f(warp_add(sum));                             // -inf: no entry that the teacher allows
     }
+    const float over = top == -INFINITY ? 0.f : top;                   // (the student excludes all of them: their sum is 0)
     float Q = 0.f, list = 0.f;
     for (int k = lane; k < K; k += 32) {
         const float q = ds.id[k] >= 0 && norm != -INFINITY ? ex2(ds.tl[k] - norm) : 0.f;
         ds.q[k] = q;
         Q += q;
-        if (TAIL && ds.first[k]) list += ex2(max_nan((ds.zk[k] - top) * scale, FAR));
+        if (TAIL && ds.first[k]) list += ex2(max_nan((ds.zk[k] - over) * scale, FAR));
     }
     Q = warp_add(Q);
     if (TAIL) list = warp_add(list);

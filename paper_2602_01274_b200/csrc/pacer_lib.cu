@@ -967,12 +967,14 @@ static const char *bad_rows(const void *z, int dtype, int64_t ld, int rows, int 
     if (rows < 0 || rows > lg::MAX_ROWS) return "rows out of range";
     if (vocab < 1 || vocab > lg::MAX_VOCAB) return "vocab out of range";
     if (ld < vocab) return "ld is less than vocab";
+    if (ld >> 36) return "ld out of range";                // (addresses are sums of 64 bits)
     if (!z && rows) return "logits is null";
     if ((uintptr_t)z % (dtype == PACER_F32 ? 4 : 2)) return "misaligned logits";
     return nullptr;
 }
 static const char *bad_grad(const void *z, int dtype, int64_t ld, int rows, int vocab, const void *dz, int64_t ld_dz) {
     if (ld_dz < vocab) return "ld_dlogits is less than vocab";
+    if (ld_dz >> 36) return "ld_dlogits out of range";
     if (!dz && rows) return "dlogits is null";
     if ((uintptr_t)dz % (dtype == PACER_F32 ? 4 : 2)) return "misaligned dlogits";
     const int64_t e = dtype == PACER_F32 ? 4 : 2;

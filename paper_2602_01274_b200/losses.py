@@ -38,7 +38,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
     differentiable.  A token outside the vocabulary (-1: padding) has logp 0 and passes no gradient."""
     shape = tokens.shape
     assert logits.shape[:-1] == shape, "tokens: the logits' leading shape"
-    logp, entropy, lse, ids, top_logp = _TokenLogprobs.apply(logits.flatten(0, -2), tokens.reshape(-1), top)
+    logp, entropy, lse, ids, top_logp = _TokenLogprobs.apply(logits.reshape(-1, logits.shape[-1]), tokens.reshape(-1), top)
     return logp.view(shape), entropy.view(shape), lse.view(shape), ids.view(*shape, top), top_logp.view(*shape, top)
 
 
@@ -65,6 +65,6 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
     lead = logits.shape[:-1]
     assert ids.shape[:-1] == lead and teacher.shape == ids.shape, "ids and teacher: the logits' leading shape, then the list"
     k = ids.shape[-1]
-    loss = _Distill.apply(logits.flatten(0, -2), ids.reshape(-1, k), teacher.detach().reshape(-1, k),
+    loss = _Distill.apply(logits.reshape(-1, logits.shape[-1]), ids.reshape(-1, k), teacher.detach().reshape(-1, k),
                           None if teacher_lse is None else teacher_lse.detach().reshape(-1), temperature)
     return loss.view(lead)

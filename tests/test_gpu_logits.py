@@ -2,8 +2,8 @@
 against plain 64-bit forms on the same inputs.
 
 Tolerances.  A row's sum of exponentials in fp32: an exponent |t| <= 40 is off by at most 3 |t| half steps (difference, scaling,
-product's operand), ex2 itself by four, a thread's running sum of at most 150 terms (the largest vocabulary here over 8 blocks of
-256 threads, or 32 000 over one) by 150: S, and each p, are right to EPS = (3 * 40 * ln 2 + 4 + 150) half steps < 240 * 2^-24 =
+product's operand), ex2 itself by four, a thread's two running sums (even and odd elements) of at most 150 terms each (the largest
+vocabulary over 8 blocks of 256 threads, or 70 001 over one) by 150: S, and each p, are right to EPS = (3 * 40 * ln 2 + 4 + 150) half steps < 240 * 2^-24 =
 1.5e-5, and so is its logarithm, absolutely.  lse and logp add roundings of their own size, four half steps at most."""
 import math
 
@@ -303,6 +303,13 @@ def test_distill_at_its_limits():
     z[:, 0] = -math.inf
     loss, d = b.pacer_distill_grad(z, ids, t, one, 1.0)
     assert (loss == math.inf).all() and (d[:, 0] == -1).all() and torch.isfinite(d).all()
+    loss, lse, tail = b.pacer_distill(z, ids, t, 1.0, tl)                # ... with a tail: all that is left is outside the list
+    want = torch.full((4, V), (1 - (1 - math.exp(-0.5))) / (V - 1), dtype=torch.float64, device=DEV)      # p_v Q - q_t w_v, p_v = w_v
+    want[:, 0] = -math.exp(-0.5)
+    assert (loss == math.inf).all() and torch.equal(lse, tail)
+    close(lse, torch.full((4,), math.log(V - 1), device=DEV), 2 * EPS, "excluded list, lse")
+    close(b.pacer_distill_grad(z, ids, t, one, 1.0, tl)[1], want, 4 * EPS, "excluded list")
+    close(b.pacer_distill_backward(z, ids, t, lse, tail, one, 1.0, tl), want, 4 * EPS, "excluded list, second call")
     # rows at the type's lowest value are uniform
     z[:] = torch.finfo(torch.float32).min
     loss, lse, _ = b.pacer_distill(z, ids, t, 0.7)
@@ -344,6 +351,44 @@ def test_rows_beyond_32_bit_offsets():
     z.copy_(copy)
     b.pacer_distill_grad(z, ids, t, w, 1.0, tl, out=z)
     assert torch.equal(z, want2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_largest_vocabulary(dtype):
+    from paper_2602_01274_b200 import binding as b
+    rows, vocab = 3, b.PACER_MAX_VOCAB
+    z = make_logits(rows, vocab, dtype, 0, 1, seed=32)
+    check_logprobs(z, make_tokens(rows, vocab), 128)
+    ids, t, tl = make_teacher(rows, vocab, 256, True, 1.0)
+    ids[0, :4] = torch.tensor([0, vocab - 1, vocab - 2, 1], device=DEV)
+    w = torch.ones(rows, device=DEV)
+    want = ref.distill(z, ids, t, 1.0, tl, w)
+    loss, d = b.pacer_distill_grad(z, ids, t, w, 1.0, tl)
+    close(loss, want[0], 60 * EPS, "loss")
+    half, least = ref.rounding(z.dtype)
+    close(d, want[3], half * 1.01 * want[3].abs() + 4 * EPS * want[4] + least, "dlogits")
+    with pytest.raises(b.PacerError, match="vocab out of range"):
+        b.pacer_logprobs(torch.zeros(1, vocab + 1, device=DEV), make_tokens(1, 5))
+
+
+def test_outputs_that_cannot_be_written_are_refused():
+    from paper_2602_01274_b200 import binding as b
+    z = make_logits(4, 50, "f32", seed=33)
+    t, w = make_tokens(4, 50), torch.ones(4, device=DEV)
+    _, ent, lse, _, _ = b.pacer_logprobs(z, t)
+    for out in (torch.empty(1, 50, device=DEV).expand(4, 50), torch.empty(4, 50, device=DEV, dtype=torch.bfloat16), torch.empty(4, 49, device=DEV),
+                torch.empty(50, 4, device=DEV).t(), torch.empty(4, 50)):
+        with pytest.raises(AssertionError, match="out: like the logits"):
+            b.pacer_logprobs_backward(z, t, lse, ent, w, out=out)
+    with pytest.raises(b.PacerError, match="overlaps"):
+        flat = torch.empty(4 * 50 + 50, device=DEV)
+        b.pacer_logprobs_backward(flat[:200].view(4, 50), t, lse, ent, w, out=flat[50:].view(4, 50))
+    with pytest.raises(AssertionError, match="tokens"):
+        b.pacer_logprobs(z, t.long())
+    with pytest.raises(AssertionError, match="tokens"):
+        b.pacer_logprobs(z, t.cpu())
+    with pytest.raises(AssertionError, match="logits"):
+        b.pacer_logprobs(z.double(), t)
 
 
 def test_no_rows():
