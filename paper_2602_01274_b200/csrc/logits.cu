@@ -564,9 +564,16 @@ __device__ void block_top(const Share<T> &sh, const float (*seg)[THREADS], int r
                 if (at[h] < 0 || (!has_nan && order_key(Vec<T>::max(v + h, 1)) < bound)) continue;
                 float x[E];
                 Vec<T>::unpack(v[h], x);
+                uint32_t hits = 0;                                     // (one or two of a vector: a branch for each element would cost
+#pragma unroll                                                          // the warp eight of them)
+                for (int e = 0; e < E; ++e) hits |= has_nan || x[e] >= least_value ? 1u << e : 0u;
+                for (; hits; hits &= hits - 1) {
+                    const int e = __ffs(hits) - 1;
+                    float z = x[0];
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (has_nan || x[e] >= least_value) test(x[e], sh.begin(sh.lo + at[h]) + e);
+                    for (int q = 1; q < E; ++q) z = q == e ? x[q] : z;
+                    test(z, sh.begin(sh.lo + at[h]) + e);
+                }
             }
         }
     if (const int i = sh.edge(tid); i >= 0) test(Vec<T>::to(sh.row[i]), i);
@@ -598,16 +605,15 @@ __device__ void block_top(const Share<T> &sh, const float (*seg)[THREADS], int r
     }
     for (int i = tid; i < top; i += THREADS)
         if (i >= n) s.best[i] = 0;
-    for (int i0 = 0; i0 < n; i0 += THREADS / 4) {                      // a candidate's place: those above it, by four lanes
-        const int i = i0 + tid / 4;
+    for (int i0 = 0; i0 < n; i0 += THREADS / 2) {                      // a candidate's place: those above it, by two lanes
+        const int i = i0 + tid / 2;
         const uint64_t k = i < n ? s.cand[i] : 0;
         int above = 0;
         if (i < n)
 #pragma unroll 4
-            for (int q = tid % 4; q < n; q += 4) above += s.cand[q] > k;
+            for (int q = tid % 2; q < n; q += 2) above += s.cand[q] > k;
         above += __shfl_xor_sync(~0u, above, 1);
-        above += __shfl_xor_sync(~0u, above, 2);
-        if (i < n && tid % 4 == 0 && above < top) s.best[above] = k;
+        if (i < n && tid % 2 == 0 && above < top) s.best[above] = k;
     }
     __syncthreads();
 }
