@@ -537,8 +537,8 @@ __device__ void block_top(const Share<T> &sh, const float (*seg)[THREADS], int r
     };
     for (int g = 0; g < runs; ++g) {
         const int i0 = g * RUN + tid;
-        const uint32_t k = i0 < nv ? order_key(seg[g][tid]) : 0u;
-        const bool hit = i0 < nv && (has_nan || k > bound || (k == bound && sh.begin(sh.lo + i0) <= bound_idx));
+        const float v = seg[g][tid];
+        const bool hit = i0 < nv && (has_nan || v > least_value || (v == least_value && sh.begin(sh.lo + i0) <= bound_idx));
         const uint32_t all = __ballot_sync(~0u, hit);
         if (!all) continue;
         int at = 0;
@@ -561,7 +561,7 @@ __device__ void block_top(const Share<T> &sh, const float (*seg)[THREADS], int r
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (at[h] < 0 || (!has_nan && order_key(Vec<T>::max(v + h, 1)) < bound)) continue;
+                if (at[h] < 0 || (!has_nan && Vec<T>::max(v + h, 1) < least_value)) continue;
                 float x[E];
                 Vec<T>::unpack(v[h], x);
                 uint32_t hits = 0;                                     // (one or two of a vector: a branch for each element would cost
