@@ -910,8 +910,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         const int i = (id + sh.off) / E - sh.lo;                       // its vector of the share
         if (i >= 0 && i < sh.hi - sh.lo) atomicOr(ds.listed + i % THREADS, 1ull << i / THREADS);
     }
-    __syncthreads();
-    if (tid < 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);
+    if (TAIL) __syncthreads();
+    if (tid >= THREADS - 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);     // (the warp with the fewest vectors)
 
     // log2 p_v = (z_v - al.ref) scale - al.m - log2 al.S; of the others among themselves (w_v) the same with ot
     Sums al, ot;
