@@ -628,6 +628,9 @@ struct ScoreArgs {
     int32_t shift, per;                    // 2^shift blocks of a row; batches of a run
 };
 
+// One row a cluster.  2048 rows of 32 000 bf16: 28 us (4.7 TB/s; loads waited for, an exponential and seven instructions an element),
+// f32 43 us (6.1 TB/s); with 64 alternatives 47 us: another eight instructions an element and five barriers a row.  Five blocks an SM
+// against four: 53 and 57 us when they were compared.
 template <class T, bool TOP>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a) {
     extern __shared__ __align__(16) unsigned char dyn[];
@@ -734,7 +737,8 @@ __device__ __forceinline__ void st_grad(T *out, bool same, int j, int off, const
     }
 }
 
-// dz_v = p_v (g_lse - g_logp) - g_H p_v (log p_v + H) + [v = token] g_logp.  Elementwise: reads and writes each element once.
+// dz_v = p_v (g_lse - g_logp) - g_H p_v (log p_v + H) + [v = token] g_logp.  Elementwise: reads and writes each element once (2048
+// rows of 32 000 bf16: 44 us, 5.9 TB/s).
 template <class T, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS) k_logprobs_back(const BackArgs a) {
     constexpr int E = Vec<T>::E;
@@ -868,7 +872,9 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
 //   dL/dz_v = w_v (Q p_t - q_t) / temperature                  for the others, w_v = p_v / p_t: their softmax among themselves
 // (without q_t: p_v Q / temperature).  The tail's sum is taken over the tokens outside the list themselves (a thread knows its
 // vectors with listed tokens): one minus the list's share would lose it where the student is sure of the list.
-// The gradient of all others is written first, the list's tokens are put right after it.
+// The gradient of all others is written first, the list's tokens are put right after it.  Loss and gradient in one launch read the row
+// twice, the second time out of L2: 2048 rows of 32 000 bf16 55 us (4.8 TB/s of one reading and one writing), 997 of 151 936 f32 with a
+// tail 246 us (4.9 TB/s).
 template <class T, bool TAIL, int MODE>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a) {
     constexpr int E = Vec<T>::E;
