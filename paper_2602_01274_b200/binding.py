@@ -406,10 +406,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _ld(t: torch.Tensor) -> int:
+    """Elements from row to row (a single row's stride says nothing)."""
+    return t.shape[1] if t.is_contiguous() else t.stride(0)
+
+
 def _layout(z: torch.Tensor):
     """The C arguments that describe rows of logits."""
-    rows, vocab = z.shape
-    return z.data_ptr(), _DTYPES[z.dtype], vocab if z.is_contiguous() else z.stride(0), rows, vocab
+    return z.data_ptr(), _DTYPES[z.dtype], _ld(z), *z.shape
 
 
 def _gradient_like(z: torch.Tensor) -> torch.Tensor:
@@ -468,7 +472,7 @@ def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entrop
     gl, gh, gs = _vec(grad_logp, "grad_logp", z, f32), _vec(grad_entropy, "grad_entropy", z, f32), _vec(grad_lse, "grad_lse", z, f32)
     out = _out_like(z, out)
     _call(_lib.pacer_logprobs_backward, z, *_layout(z), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), out.data_ptr(),
-          max(out.stride(0), z.shape[1]))
+          _ld(out))
     return out
 
 
@@ -501,7 +505,7 @@ def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, t
     weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
     loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
     _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, _ptr(weight),
-          out.data_ptr(), max(out.stride(0), z.shape[1]))
+          out.data_ptr(), _ld(out))
     return loss, out
 
 
@@ -513,7 +517,7 @@ def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, tempe
     lse, tail_lse, grad_loss = _vec(lse, "lse", z, f32), _vec(tail_lse, "tail_lse", z, f32), _vec(grad_loss, "grad_loss", z, f32)
     out = _out_like(z, out)
     _call(_lib.pacer_distill_backward, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
-          out.data_ptr(), max(out.stride(0), z.shape[1]))
+          out.data_ptr(), _ld(out))
     return out
 
 
@@ -529,7 +533,7 @@ def pacer_head_logprobs(hidden, head, tokens, bias_ids=None, bias: float = 0.0):
     nbytes = _lib.pacer_head_logprobs_scratch_bytes(rows, vocab)
     logp, entropy, lse = torch.empty(3 * rows, dtype=torch.float32, device=h.device).split_with_sizes((rows, rows, rows))
     scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device)      # (torch aligns an allocation to 512 bytes)
-    _call(_lib.pacer_head_logprobs, h, h.data_ptr(), max(h.stride(0), d), w.data_ptr(), max(w.stride(0), d), rows, vocab, d, _ptr(tokens),
+    _call(_lib.pacer_head_logprobs, h, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), rows, vocab, d, _ptr(tokens),
           _ptr(bias_ids), bias, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), scratch.data_ptr(), nbytes)
     return logp, entropy, lse
 

@@ -25,7 +25,7 @@ constexpr int BATCH = UNROLL * THREADS;    // vectors of a block's batch
 constexpr int PER_SM = 5;                  // blocks on an SM
 constexpr int CAND = 512;                  // candidates for the alternatives that a block collects at most
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float NO_REF = -3.402823466e38f, LOWEST = NO_REF, SLACK = 16.f;
+constexpr float LOWEST = -3.402823466e38f, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
 constexpr float HUGE_M = 1e8f;
 constexpr float LSE_EXACT = 1024.f;        // a larger f32 log-sum-exp says a row's probabilities to less than 3e-5: it is taken anew
@@ -60,9 +60,10 @@ template <> struct Vec<float> {
     __device__ static uint4 pack(const float (&f)[4]) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
-    // Where sums of 2^t t are wanted, what lies below LOW counts as LOW, which has 2^t = 0 over the first reference START already:
-    // 0 * -inf would be NaN.  LEAST: a row whose largest logit is below it is summed apart (LOW could count there).
-    static constexpr float LOW = -1e30f, START = -1e29f, LEAST = -HUGE_M;
+    // The first reference of a sum is START: what lies far below it (a mask of -1e20, say) adds nothing, as it would add nothing to
+    // any row that is not huge().  Where sums of 2^t t are wanted, what lies below LOW counts as LOW, which has 2^t = 0 over START
+    // already: 0 * -inf would be NaN.  LEAST: a row whose largest logit is not above it is summed apart (START or LOW could count).
+    static constexpr float LOW = -1e30f, START = -HUGE_M, LEAST = -HUGE_M;
     __device__ static void lift(uint4 &v) {                             // (NaN stays)
         v.x = __float_as_uint(max_nan(__uint_as_float(v.x), LOW)); v.y = __float_as_uint(max_nan(__uint_as_float(v.y), LOW));
         v.z = __float_as_uint(max_nan(__uint_as_float(v.z), LOW)); v.w = __float_as_uint(max_nan(__uint_as_float(v.w), LOW));
@@ -96,7 +97,7 @@ template <> struct Vec<__nv_bfloat16> {
     }
     __device__ static uint4 pack(const float (&f)[8]) { return make_uint4(one(f[0], f[1]), one(f[2], f[3]), one(f[4], f[5]), one(f[6], f[7])); }
     static constexpr uint32_t LOW = 0xf14af14au;          // -1e30
-    static constexpr float START = -1e29f, LEAST = -HUGE_M;
+    static constexpr float START = -HUGE_M, LEAST = -HUGE_M;
     __device__ static uint32_t lift(uint32_t u) {
         const uint32_t l = LOW;
         const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&l));
@@ -247,14 +248,14 @@ __device__ __forceinline__ float warp_max(float v) {
 
 // S = sum 2^t, S2 = sum 2^t t with t = (z - ref) scale - m.  A logit of -inf adds nothing; NaN and +inf make the sums NaN.
 struct Sums {
-    float ref = 0.f, m = NO_REF, S = 0.f, S2 = 0.f;
+    float ref = 0.f, m = 0.f, S = 0.f, S2 = 0.f;
     __device__ float exponent(float z, float scale) const { return fmaf(z - ref, scale, -m); }
 };
 
 // A thread's sums while it reads its vectors: even and odd elements apart.
 template <class T, bool ENTROPY>
 struct PairSums {
-    float m = ENTROPY ? Vec<T>::START : NO_REF;
+    float m = Vec<T>::START;
     f2 S = 0, S2 = 0;
     __device__ void reach(float top) {                                   // the largest exponent (scaled logit) that comes next
         if (top > m + SLACK) {

@@ -980,7 +980,7 @@ static const char *bad_grad(const void *z, int dtype, int64_t ld, int rows, int 
     const int64_t e = dtype == PACER_F32 ? 4 : 2;
     const uintptr_t z0 = (uintptr_t)z, d0 = (uintptr_t)dz;
     const uintptr_t z1 = z0 + e * ((int64_t)(rows - 1) * ld + vocab), d1 = d0 + e * ((int64_t)(rows - 1) * ld_dz + vocab);
-    if (rows && z0 < d1 && d0 < z1 && !(z0 == d0 && ld == ld_dz)) return "dlogits overlaps the logits";
+    if (rows && z0 < d1 && d0 < z1 && !(z0 == d0 && (ld == ld_dz || rows == 1))) return "dlogits overlaps the logits";
     return nullptr;
 }
 #define REFUSE_IF(cond, what) \

@@ -66,8 +66,11 @@ def logprobs_grad(z, tokens, lse, entropy, gl, gh, gs):
 
 def distill(z, ids, teacher, temperature, teacher_lse, weight):
     """(loss, lse, tail_lse, weight * gradient, size of its terms), entry by entry over the list."""
-    z, t = z.double() / temperature, teacher.double() / temperature
+    z, t = z.double(), teacher.double() / temperature
     R, V = z.shape
+    top = z.max(1, keepdim=True).values
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    z = (z - top) / temperature                    # (a row of huge values keeps its differences)
     ok = (ids >= 0) & (ids < V)
     t = torch.where(ok, t, torch.full_like(t, -math.inf))
     at = torch.where(ok, ids, torch.zeros_like(ids)).long()
@@ -101,4 +104,5 @@ def distill(z, ids, teacher, temperature, teacher_lse, weight):
     loss = torch.where(dead, torch.zeros_like(loss), loss)
     d = torch.where(dead[:, None], torch.zeros_like(d), d)
     g = (weight.double() / temperature)[:, None]
-    return loss, lse, tail, d * g, size * g.abs()
+    top = top[:, 0] / temperature
+    return loss, lse + top, None if tail is None else tail + top, d * g, size * g.abs()

@@ -93,6 +93,13 @@ def test_head_agrees_with_the_logits_operator():
         assert (x - y).abs().max() < 1e-4
 
 
+def test_one_row_whatever_its_stride():
+    from paper_2602_01274_b200 import binding as b
+    h, w, t, _ = make(1, 300, 64)
+    odd = torch.as_strided(h, (1, 64), (67, 1))              # (no second row: the stride says nothing)
+    assert all(torch.equal(x, y) for x, y in zip(b.pacer_head_logprobs(odd, w, t), b.pacer_head_logprobs(h, w, t)))
+
+
 def test_no_rows():
     from paper_2602_01274_b200 import binding as b
     h, w, _, _ = make(1, 100, 64)

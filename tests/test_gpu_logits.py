@@ -94,6 +94,11 @@ def test_logprobs_of_masked_rows(rows, dtype):
         z[6, :] = -1e9 if dtype == "f32" else -1e4
         z[7] = -math.inf
         z[7, -1] = 3.0                                  # one token is left: the last
+        if dtype != "f16":                              # finite masks of any size, in front of what is left and behind it
+            for r, v in enumerate((-1e8, -1e10, -1e20, -3e38)):
+                z[8 + 2 * r, :-500] = v
+                z[9 + 2 * r, 500:] = v
+                z[16 + r] = v
     tokens = make_tokens(rows, vocab)
     tokens[0] = 17
     check_logprobs(z, tokens, top)
@@ -333,6 +338,30 @@ def test_distill_at_its_limits():
     close(b.pacer_distill_backward(z, ids, t, lse, tail, one, 1.0, tl), want, 4 * EPS, "others at the lowest, second call")
 
 
+@pytest.mark.parametrize("dtype,mask", [("f32", -1e8), ("f32", -1e10), ("f32", -1e20), ("f32", -3.4e38), ("bf16", -1e10), ("bf16", -3.38e38), ("f16", -65504.0)])
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 10.0])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_of_rows_masked_with_finite_values(dtype, mask, temperature, tail):
+    """A finite mask leaves what -inf would leave; a row of nothing else is a row of zeros."""
+    from paper_2602_01274_b200 import binding as b
+    rows, vocab = 6, 9001
+    ids, t, tl = make_teacher(rows, vocab, 7, tail, temperature, spoil=False)
+    ids = ids % 400 + vocab - 500                       # the list lies in what is left of rows 0 and 3
+    z = make_logits(rows, vocab, dtype, seed=34)
+    plain = z.clone()
+    z[0, :-500], plain[0, :-500] = mask, -math.inf
+    z[1], plain[1] = mask, 0.0
+    z[3, :-500:2], plain[3, :-500:2] = mask, -math.inf
+    w = torch.ones(rows, device=DEV)
+    got, want = b.pacer_distill_grad(z, ids, t, w, temperature, tl), ref.distill(plain, ids, t, temperature, tl, w)
+    close(got[0], want[0], 60 * EPS, "loss")
+    half, least = ref.rounding(z.dtype)
+    close(got[1], want[3], half * 1.01 * want[3].abs() + 4 * EPS * want[4] + least, "dlogits")
+    _, lse, tail_lse = b.pacer_distill(z, ids, t, temperature, tl)
+    again = b.pacer_distill_backward(z, ids, t, lse, tail_lse, w, temperature, tl)
+    close(again, want[3], half * 1.01 * want[3].abs() + (4 * EPS + 160 * ref.F32) * want[4] + least, "dlogits, second call")
+
+
 def test_rows_beyond_32_bit_offsets():
     from paper_2602_01274_b200 import binding as b
     rows, vocab, ld = 17000, 1000, 131072                # 2.2e9 elements from the first row to the last
@@ -436,6 +465,19 @@ def test_other_streams_and_graphs():
     z[0].copy_(keep)
     graph.replay()
     assert all(torch.equal(x, y) for x, y in zip(out, want[0]))
+
+
+def test_one_row_in_place_whatever_its_stride():
+    from paper_2602_01274_b200 import binding as b
+    z = torch.randn(1, 70, device=DEV)[:, :61].clone()       # a single row: contiguous, with a stride of 70
+    t, w = make_tokens(1, 61), torch.ones(1, device=DEV)
+    ids, teacher, _ = make_teacher(1, 61, 5, False, 1.0)
+    _, want = b.pacer_distill_grad(z, ids, teacher, w)
+    keep = z.clone()
+    assert torch.equal(b.pacer_distill_grad(keep, ids, teacher, w, out=keep)[1], want)
+    _, ent, lse, _, _ = b.pacer_logprobs(z, t)
+    want = b.pacer_logprobs_backward(z, t, lse, ent, w, w)
+    assert torch.equal(b.pacer_logprobs_backward(z, t, lse, ent, w, w, out=z), want)
 
 
 def test_inputs_of_any_stride():
