@@ -297,8 +297,9 @@ int pacer_linear_static(const void *x, const void *w, float *y, int rows, int N,
  * input and output lie alike modulo 16 bytes).  rows <= 2^24, vocab <= PACER_MAX_VOCAB; rows = 0 does nothing.  All other arrays are device,
  * contiguous, f32 or int32 as declared.  Sums and statistics are fp32.  A logit of -inf has probability 0; a row of -inf only has lse -inf,
  * every log probability -inf, entropy 0 and gradient 0; a NaN or +inf logit makes the results of its row NaN.  The calls enqueue
- * one kernel on `cuda_stream` (of the current device), use no workspace and no atomics on global memory: they give the same bits every time,
- * may overlap and may be captured into a graph. */
+ * one kernel on `cuda_stream` (of the current device), use no workspace and no atomics on global memory: the same
+ * call on the same addresses gives the same bits every time (rows that lie otherwise modulo 16 bytes may be summed in another order);
+ * calls may overlap and may be captured into a graph. */
 enum { PACER_F32 = 0, PACER_BF16 = 1, PACER_F16 = 2 };
 #define PACER_MAX_VOCAB 393216
 #define PACER_MAX_TOP 128

@@ -432,7 +432,8 @@ def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
     return out
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream         # torch.cuda.current_stream(..).cuda_stream without the object: 2 us a call
+# torch.cuda.current_stream(..).cuda_stream, where torch has it without the object that costs 2 us a call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _call(fn, like: torch.Tensor, *args):
@@ -447,20 +448,26 @@ def _call(fn, like: torch.Tensor, *args):
         raise PacerError(f"{fn.__name__}: {_lib.pacer_strerror(rc).decode()}: {_lib.pacer_last_error(None).decode()}")
 
 
-def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
+def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, out=None):
     """Log probabilities of given tokens under rows of logits [rows][vocab] (f32, bf16 or f16): returns
     (logp [rows], entropy [rows], lse [rows], top_ids int32 [rows][top], top_logp [rows][top]).  tokens int32 [rows]; one outside
-    the vocabulary (-1, say) has logp 0.  Alternatives: larger logit first, of equal ones the lower id.  No gradient: see
-    pacer_logprobs_backward, and losses.token_logprobs for autograd."""
+    the vocabulary (-1, say) has logp 0.  Alternatives: larger logit first, of equal ones the lower id.  `out`: five such tensors
+    to write (contiguous; else they are made, views of one allocation).  No gradient: see pacer_logprobs_backward, and
+    losses.token_logprobs for autograd."""
     z = _rows(logits)
     tokens = _vec(tokens, "tokens", z, torch.int32)
     rows, dev, n = z.shape[0], z.device, max(top, 0)
-    # (five small tensors out of two allocations)
-    logp, entropy, lse, top_logp = torch.empty((3 + n) * rows, dtype=torch.float32, device=dev).split_with_sizes((rows, rows, rows, n * rows))
-    ids = torch.empty((rows, n), dtype=torch.int32, device=dev)
-    at = logp.data_ptr()
-    _call(_lib.pacer_logprobs, z, *_layout(z), _ptr(tokens), top, at, at + 4 * rows, at + 8 * rows, ids.data_ptr(), at + 12 * rows)
-    return logp, entropy, lse, ids, top_logp.view(rows, n)
+    if out is None:
+        logp, entropy, lse, top_logp = torch.empty((3 + n) * rows, dtype=torch.float32, device=dev).split_with_sizes((rows, rows, rows, n * rows))
+        ids, top_logp = torch.empty((rows, n), dtype=torch.int32, device=dev), top_logp.view(rows, n)
+    else:
+        logp, entropy, lse, ids, top_logp = out
+        for t in out:
+            shape, dtype = ((rows, n) if t is ids or t is top_logp else (rows,)), (torch.int32 if t is ids else torch.float32)
+            assert t.shape == shape and t.dtype == dtype and t.device == dev and t.is_contiguous(), f"out: contiguous {dtype} {shape} on {dev}"
+    _call(_lib.pacer_logprobs, z, *_layout(z), _ptr(tokens), top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), ids.data_ptr(),
+          top_logp.data_ptr())
+    return logp, entropy, lse, ids, top_logp
 
 
 def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entropy=None, grad_lse=None, out=None):
@@ -492,8 +499,8 @@ def pacer_distill(logits, ids, teacher, temperature: float = 1.0, teacher_lse=No
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
     loss, lse = torch.empty(2, z.shape[0], dtype=torch.float32, device=z.device).unbind(0)
     tail = None if teacher_lse is None else torch.empty_like(teacher_lse)
-    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), lse.data_ptr(), _ptr(tail), None, None,
-          0)
+    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature,
+          loss.data_ptr(), lse.data_ptr(), _ptr(tail), None, None, 0)
     return loss, lse, tail
 
 
@@ -504,8 +511,8 @@ def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, t
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
     weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
     loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, loss.data_ptr(), None, None, _ptr(weight),
-          out.data_ptr(), _ld(out))
+    _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature,
+          loss.data_ptr(), None, None, _ptr(weight), out.data_ptr(), _ld(out))
     return loss, out
 
 
@@ -516,8 +523,8 @@ def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, tempe
     f32 = torch.float32
     lse, tail_lse, grad_loss = _vec(lse, "lse", z, f32), _vec(tail_lse, "tail_lse", z, f32), _vec(grad_loss, "grad_loss", z, f32)
     out = _out_like(z, out)
-    _call(_lib.pacer_distill_backward, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss),
-          out.data_ptr(), _ld(out))
+    _call(_lib.pacer_distill_backward, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse),
+          temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss), out.data_ptr(), _ld(out))
     return out
 
 

@@ -302,7 +302,8 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
     }
 }
 
-// Tokens of a tile: the width with the least waves x (time of a tile), counted in tokens; a tile has a fixed cost of about 16.
+// Tokens of a tile: the width with the least waves x (width + 16).  The 16 stands for a tile's start and end: without it many rows would
+// be cut into the narrowest tiles for a fraction of a wave (2048 rows x 32 000: 32 tokens instead of 256; with 16 or 64 the same widths).
 static int tile_width(int mt, int vocab, int n_sm, int step) {
     int best = TN;
     int64_t best_cost = INT64_MAX;
@@ -316,6 +317,8 @@ static int tile_width(int mt, int vocab, int n_sm, int step) {
 struct Tiles { int pair, mt, bn, nt; };
 // Pairs of blocks where that leaves few rows empty: they read a third less out of L2, and the power cap leaves them a higher clock
 // for it (2048 rows x 32 000 x 4096: 4.9 GB and 415 us, tensor pipe 91 % active; by single blocks 7.1 GB and 474 us).
+// With 32 000 tokens x 4096: 256 rows 60 us by pairs, 68 by single blocks; 384 rows (three tiles of 128) 100 and 92; 640 (five) 145 and
+// 141; 1100 (nine) 229 and 237.
 static Tiles tiles_of(int rows, int vocab) {
     Tiles t;
     const int m128 = (rows + TM - 1) / TM;

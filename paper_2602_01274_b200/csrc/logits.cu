@@ -1048,15 +1048,21 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
 
 static int elem_bytes(int dtype) { return dtype == PACER_F32 ? 4 : 2; }
 
-// Blocks per row: more than one while all rows' blocks fit the device at a time and a thread keeps a vector; and, where rows are read
-// twice, while the rows at work (of all SMs) exceed what L2 (126 MB) surely keeps: 997 rows of 151 936 f32, loss and gradient, took
-// 257 us with eight blocks a row (56 MB at work), 288 us with four (112 MB).
+// Blocks per row (log2).  More than one while two blocks an SM take all rows' and a thread keeps a vector, or all block slots do and a
+// block keeps 64 KB: one row of 151 936 f32 with 20 alternatives takes 12.2 us by eight blocks, 13.5 by four, 24.6 by one; 200 such rows
+// 32.5 us by two, 45.5 by one; 136 rows of 32 256 bf16 10.0 by two, 11.7 by four; 300 rows of 32 000 bf16 11.8 by one, 13.7 by two.
+// And, where rows are read twice, while the rows at work (of all SMs) exceed what L2 (126 MB) surely keeps: 997 rows of 151 936 f32,
+// loss and gradient, took 257 us with eight blocks a row (56 MB at work), 288 us with four (112 MB).
 static int blocks_per_row_log2(int rows, int vocab, int elem, bool twice) {
     const int slots = PER_SM * 148;
     const double bytes = (double)vocab * elem;
     int shift = 0;
-    while (1 << shift < MAX_C && (((int64_t)rows << (shift + 1) <= slots && bytes / (2 << shift) >= THREADS * 16) ||
-                                  (twice && std::min(rows, slots >> shift) * bytes > 64e6))) ++shift;
+    for (; 1 << shift < MAX_C; ++shift) {
+        const int64_t blocks = (int64_t)rows << (shift + 1);
+        const double share = bytes / (2 << shift);
+        if (!((blocks <= 2 * 148 && share >= THREADS * 16) || (blocks <= slots && share >= 65536) ||
+              (twice && std::min(rows, slots >> shift) * bytes > 64e6))) break;
+    }
     return shift;
 }
 

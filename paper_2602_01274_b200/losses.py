@@ -18,7 +18,10 @@ from . import binding
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, top):
-        logp, entropy, lse, ids, top_logp = binding.pacer_logprobs(logits, tokens, top)
+        rows, f32 = logits.shape[0], dict(dtype=torch.float32, device=logits.device)
+        logp, entropy, lse = (torch.empty(rows, **f32) for _ in range(3))      # (no views of one tensor: they may be changed in place)
+        ids, top_logp = torch.empty(rows, top, dtype=torch.int32, device=logits.device), torch.empty(rows, top, **f32)
+        binding.pacer_logprobs(logits, tokens, top, out=(logp, entropy, lse, ids, top_logp))
         ctx.save_for_backward(logits, tokens, lse, entropy)
         ctx.mark_non_differentiable(ids, top_logp)
         ctx.set_materialize_grads(False)

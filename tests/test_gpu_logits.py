@@ -3,8 +3,8 @@ against plain 64-bit forms on the same inputs.
 
 Tolerances.  A row's sum of exponentials in fp32: an exponent |t| <= 40 is off by at most 3 |t| half steps (difference, scaling,
 product's operand), ex2 itself by four, a thread's two running sums (even and odd elements) of at most 150 terms each (the largest
-vocabulary over 8 blocks of 256 threads, or 70 001 over one) by 150: S, and each p, are right to EPS = (3 * 40 * ln 2 + 4 + 150) half steps < 240 * 2^-24 =
-1.5e-5, and so is its logarithm, absolutely.  lse and logp add roundings of their own size, four half steps at most."""
+vocabulary over 8 blocks of 256 threads, or 70 001 over one) by 150: S, and each p, are right to
+EPS = (3 * 40 * ln 2 + 4 + 150) half steps < 240 * 2^-24 = 1.5e-5, and so is its logarithm, absolutely.  lse and logp add roundings of their own size, four half steps at most."""
 import math
 
 import pytest
@@ -338,7 +338,8 @@ def test_distill_at_its_limits():
     close(b.pacer_distill_backward(z, ids, t, lse, tail, one, 1.0, tl), want, 4 * EPS, "others at the lowest, second call")
 
 
-@pytest.mark.parametrize("dtype,mask", [("f32", -1e8), ("f32", -1e10), ("f32", -1e20), ("f32", -3.4e38), ("bf16", -1e10), ("bf16", -3.38e38), ("f16", -65504.0)])
+@pytest.mark.parametrize("dtype,mask", [("f32", -1e8), ("f32", -1e10), ("f32", -1e20), ("f32", -3.4e38), ("bf16", -1e10),
+                                        ("bf16", -3.38e38), ("f16", -65504.0)])
 @pytest.mark.parametrize("temperature", [0.5, 1.0, 10.0])
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_of_rows_masked_with_finite_values(dtype, mask, temperature, tail):

@@ -31,6 +31,31 @@ def test_token_logprobs_is_differentiable(dtype):
     close(z.grad.view(24, 1001), want, half * 1.01 * want.abs() + 180 * ref.F32 * size + least, "entropy's grad")
 
 
+def test_outputs_may_be_changed_in_place():
+    from paper_2602_01274_b200 import losses
+    z = make_logits(12, 333, "f32", seed=45).requires_grad_(True)
+    tokens = make_tokens(12, 333)
+    mask = (torch.arange(12, device=DEV) % 2).float()
+    logp, ent, _, _, tlp = losses.token_logprobs(z, tokens, 3)
+    logp.mul_(mask)
+    ent += 1.0
+    tlp.zero_()
+    (logp.sum() + ent.sum()).backward()
+    got, z.grad = z.grad, None
+    logp, ent, _, _, _ = losses.token_logprobs(z, tokens)
+    ((logp * mask).sum() + ent.sum()).backward()
+    assert torch.equal(got, z.grad)
+    # a second stream, and a leaf that a view of it went through
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    leaf = z.detach().clone().requires_grad_(True)
+    with torch.cuda.stream(s):
+        logp, ent, _, _, _ = losses.token_logprobs(leaf.view(3, 4, 333), tokens.view(3, 4))
+        ((logp.view(-1) * mask).sum() + ent.sum()).backward()
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(leaf.grad, z.grad)
+
+
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_loss_is_differentiable(tail):
     from paper_2602_01274_b200 import losses

@@ -17,7 +17,8 @@ def refused(lib, rc, text):
 
 
 LOGITS = [  # changes of (logits, dtype, ld, rows, vocab) and the reason
-    (dict(z=None), "logits is null"), (dict(dtype=3), "unknown type"), (dict(dtype=-1), "unknown type"), (dict(ld=99), "ld is less"), (dict(ld=1 << 36), "ld out of range"),
+    (dict(z=None), "logits is null"), (dict(dtype=3), "unknown type"), (dict(dtype=-1), "unknown type"), (dict(ld=99), "ld is less"),
+    (dict(ld=1 << 36), "ld out of range"),
     (dict(rows=-1), "rows out of range"), (dict(rows=(1 << 24) + 1), "rows out of range"), (dict(vocab=0), "vocab out of range"),
     (dict(vocab=393217, ld=1 << 22), "vocab out of range"), (dict(z=A + 2), "misaligned logits"),
     (dict(z=A + 1, dtype=1), "misaligned logits"),
@@ -48,7 +49,8 @@ def test_logprobs(lib, tokens, top, logp, text):
 
 @pytest.mark.parametrize("change,text", [
     (dict(lse=None), "lse is null"), (dict(gl=None), "no gradient comes in"), (dict(tokens=None), "g_logp without tokens"),
-    (dict(gh=X, entropy=None), "g_entropy without entropy"), (dict(dz=None), "dlogits is null"), (dict(ld_dz=99), "ld_dlogits is less"), (dict(ld_dz=1 << 36), "ld_dlogits out of range"),
+    (dict(gh=X, entropy=None), "g_entropy without entropy"), (dict(dz=None), "dlogits is null"), (dict(ld_dz=99), "ld_dlogits is less"),
+    (dict(ld_dz=1 << 36), "ld_dlogits out of range"),
     (dict(dz=B + 2), "misaligned dlogits"), (dict(dz=A + 4), "overlaps"), (dict(dz=A, ld_dz=101), "overlaps"), (dict(dz=A + 1200), "overlaps"),
 ])
 def test_logprobs_backward(lib, change, text):
