@@ -38,7 +38,8 @@ class _TokenLogprobs(torch.autograd.Function):
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0):
     """(logp, entropy, lse, top_ids, top_logp) of int32 tokens [...] under logits [..., vocab]; the first three are
-    differentiable.  A token outside the vocabulary (-1: padding) has logp 0 and passes no gradient."""
+    differentiable.  A token outside the vocabulary (-1: padding) has logp 0 and passes no gradient.  logp may be changed in
+    place; entropy and lse are kept for the backward pass, as the logits are."""
     shape = tokens.shape
     assert logits.shape[:-1] == shape, "tokens: the logits' leading shape"
     logp, entropy, lse, ids, top_logp = _TokenLogprobs.apply(logits.reshape(-1, logits.shape[-1]), tokens.reshape(-1), top)

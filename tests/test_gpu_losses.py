@@ -31,17 +31,20 @@ def test_token_logprobs_is_differentiable(dtype):
     close(z.grad.view(24, 1001), want, half * 1.01 * want.abs() + 180 * ref.F32 * size + least, "entropy's grad")
 
 
-def test_outputs_may_be_changed_in_place():
+def test_log_probabilities_may_be_changed_in_place():
     from paper_2602_01274_b200 import losses
     z = make_logits(12, 333, "f32", seed=45).requires_grad_(True)
     tokens = make_tokens(12, 333)
     mask = (torch.arange(12, device=DEV) % 2).float()
     logp, ent, _, _, tlp = losses.token_logprobs(z, tokens, 3)
     logp.mul_(mask)
-    ent += 1.0
     tlp.zero_()
     (logp.sum() + ent.sum()).backward()
     got, z.grad = z.grad, None
+    _, ent, _, _, _ = losses.token_logprobs(z, tokens)
+    ent += 1.0                                          # (the backward pass needs it as it was: torch says so)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        ent.sum().backward()
     logp, ent, _, _, _ = losses.token_logprobs(z, tokens)
     ((logp * mask).sum() + ent.sum()).backward()
     assert torch.equal(got, z.grad)
