@@ -203,6 +203,10 @@ int pacer_debug_set_device_status(pacer_ctx *ctx, int code, int block, int warp,
  * Returns PACER_EDEVICE (after filling `out`) when the device status word is set. */
 int pacer_read_state(pacer_ctx *ctx, pacer_seq_state *out, int batch);
 
+/* Sequences of the current run: those of the last pacer_prefill or pacer_generate* whose arguments were taken (a call that
+ * refuses them leaves the run before it).  1 before the first; 0 for a null context. */
+int pacer_batch(const pacer_ctx *ctx);
+
 /* [sync] Copies `bytes` bytes from the start of one device buffer (PACER_BUF_*) to host memory.
  * Returns PACER_EDEVICE (after the copy) when the device status word is set. */
 int pacer_read_buffer(pacer_ctx *ctx, int which, void *host_dst, size_t bytes);
@@ -317,7 +321,8 @@ int pacer_logprobs(const void *logits, int dtype, int64_t ld, int rows, int voca
  * context's stream, without copying its logits to the host: row j of a sequence holds the target's distribution behind
  * [last accepted token, y_1 .. y_j], and its token is the draft y_{j+1}; the row behind the last draft has no token (logp 0).
  * logp, entropy: device f32 [batch][gamma_cap + 1]; top_ids int32, top_logp f32 [batch][gamma_cap + 1][top]; each may be NULL.
- * Rows past a sequence's window, and sequences that have finished, are left as they were. */
+ * Rows past a sequence's window, and sequences that have finished, are left as they were.  batch is the current run's, whoever
+ * began it: pacer_batch. */
 int pacer_verify_logprobs(pacer_ctx *ctx, int top, float *logp, float *entropy, int32_t *top_ids, float *top_logp);
 
 /* Gradient of the above: dlogits[r][v] = g_logp[r] ([v = token] - p_v) + g_lse[r] p_v - g_entropy[r] p_v (log p_v + entropy[r]),

@@ -99,6 +99,7 @@ _lib.pacer_linear_static.argtypes = [_P, _P, _P, C.c_int, C.c_int, C.c_int, _P]
 PACER_LINEAR_STATIC_BYTES = 4 << 20
 _I, _L, _F = C.c_int, C.c_int64, C.c_float
 _lib.pacer_logprobs.argtypes = [_P, _I, _L, _I, _I, _P, _I, _P, _P, _P, _P, _P, _P]
+_lib.pacer_batch.argtypes = [_P]
 _lib.pacer_verify_logprobs.argtypes = [_P, _I, _P, _P, _P, _P]
 _lib.pacer_logprobs_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P, _L, _P]
 _lib.pacer_distill.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, _F, _P, _P, _P, _P, _P, _L, _P]
@@ -119,7 +120,7 @@ def exported_symbols():
     """The C entry points this binding resolved (all declared in pacer.h)."""
     return ["pacer_strerror", "pacer_last_error", "pacer_workspace_bytes", "pacer_create", "pacer_destroy",
             "pacer_load_weights", "pacer_prefill", "pacer_draft_step", "pacer_preverify", "pacer_verify",
-            "pacer_accept_rollback", "pacer_read_state", "pacer_read_buffer", "pacer_generate", "pacer_generate_sched",
+            "pacer_accept_rollback", "pacer_read_state", "pacer_batch", "pacer_read_buffer", "pacer_generate", "pacer_generate_sched",
             "pacer_generate_ar", "pacer_debug_set_device_status",
             "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
             "pacer_logprobs", "pacer_verify_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
@@ -183,7 +184,6 @@ class Context:
             rc = _lib.pacer_create(C.byref(cfg), self._ws_ptr, nbytes, self.stream.cuda_stream, C.byref(h))
         self._h = h
         self._keep = []
-        self._batch = 1                                             # sequences of the run that pacer_prefill began
         self._check(rc)
 
     def _check(self, rc):
@@ -225,7 +225,6 @@ class Context:
         with torch.cuda.device(self.device):
             self._check(_lib.pacer_prefill(self._h, p.ctypes.data, p.shape[0], p.shape[1], max_new, gamma_max,
                                            threshold, mode, seed))
-        self._batch = p.shape[0]
 
     def pacer_draft_step(self):
         with torch.cuda.device(self.device):
@@ -242,8 +241,8 @@ class Context:
     def pacer_verify_logprobs(self, top: int = 0):
         """Between pacer_verify and the next stage call: (logp, entropy f32 [batch][gamma_cap + 1], top_ids int32 and top_logp f32
         [batch][gamma_cap + 1][top]) of the target's distributions behind every row of the window, on the device.  Row j's token
-        is draft j + 1; rows past a sequence's window are NaN (ids -1)."""
-        rows = (self._batch, self.cfg.gamma_cap + 1)
+        is draft j + 1; rows past a sequence's window are NaN (ids -1).  batch: the current run's, whichever call began it."""
+        rows = (_lib.pacer_batch(self._h), self.cfg.gamma_cap + 1)     # (the library writes that many)
         with torch.cuda.device(self.device):
             logp, entropy = (torch.full(rows, math.nan, device=self.device) for _ in range(2))
             ids = torch.full((*rows, max(top, 0)), -1, dtype=torch.int32, device=self.device)

@@ -697,6 +697,8 @@ extern "C" int pacer_debug_set_device_status(pacer_ctx *c, int code, int block, 
     return PACER_OK;
 }
 
+extern "C" int pacer_batch(const pacer_ctx *c) { return c ? c->batch : 0; }
+
 extern "C" int pacer_read_state(pacer_ctx *c, pacer_seq_state *out, int batch) {
     if (!c || !out || batch < 1 || batch > c->cfg.max_batch) return fail(c, PACER_EINVAL, "pacer_read_state: bad argument");
     std::vector<SeqState> hs(batch);
