@@ -6,8 +6,9 @@
 // row twice (its best elements, its gradient) reads it again out of L2.
 // Softmax sums are held as (m, S), S = sum 2^(z scale - m): the reference m is raised only when a logit lies more than 2^SLACK above
 // it (S stays below vocab * 2^SLACK), so that the common path has no rescaling and an exponent is one fused multiply-add.  That is
-// exact whatever the rounding of m, as long as the steps of numbers of m's size stay small: rows whose largest logit is beyond
-// HUGE_M (a row masked with the type's lowest value, say) are summed again, with differences taken first.
+// right to the exponent's own rounding whatever the logits of a row have in common, and m and log2 S stay apart for what is computed
+// from them: their sum would be rounded at the logits' size (0.06 at 1e6), and a log probability with it.  Rows whose largest logit is
+// beyond HUGE_M (a row masked with the type's lowest value, say) are summed again, with differences taken first.
 #include "logits.h"
 
 #include <cuda_bf16.h>
@@ -25,6 +26,8 @@ constexpr int BATCH = UNROLL * THREADS;    // vectors of a block's batch
 constexpr int PER_SM = 5;                  // blocks on an SM
 constexpr int CAND = 512;                  // candidates for the alternatives that a block collects at most
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// 1 / LOG2E as it stands in f32, in two parts: from exponents back to the logits' units at one rounding
+constexpr float UNIT_HI = (float)(1.0 / (double)LOG2E), UNIT_LO = (float)(1.0 / (double)LOG2E - (double)UNIT_HI);
 constexpr float LOWEST = -3.402823466e38f, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
 constexpr float HUGE_M = 1e8f;
@@ -271,6 +274,11 @@ __device__ __forceinline__ float warp_max(float v) {
 struct Sums {
     float ref = 0.f, m = 0.f, S = 0.f, S2 = 0.f;
     __device__ float exponent(float z, float scale) const { return fmaf(z - ref, scale, -m); }
+    // log p of a logit from its exponent (whose range a finite logit far below the others may leave where its log p does not)
+    __device__ float log_p(float z, float scale, float inv_temp, float log2S) const {
+        const float e = exponent(z, scale) - log2S;
+        return e == -INFINITY ? (z - ref) * inv_temp - (m + log2S) * LN2 : e * LN2;
+    }
 };
 
 // A thread's sums while it reads its vectors: even and odd elements apart.
@@ -695,10 +703,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a)
     if (TOP && runs < all_runs) seg[runs][tid] = most;
     if (edge >= 0) ps.add(at_edge, LOG2E);
     const Sums t = row_sums<T>(ps.m, ps.S, ps.S2, sh, sl, rank, C, LOG2E, [](int) { return false; });
-    const float log2S = log2f(t.S), all = (t.m + log2S) * LN2;         // (a row of -inf: S = 0)
-    auto logp = [&](float x) { return t.S == 0.f ? -INFINITY : (x - t.ref) - all; };
+    const float log2S = log2f(t.S);                                    // (a row of -inf: S = 0)
+    auto logp = [&](float x) { return t.S == 0.f ? -INFINITY : t.log_p(x, LOG2E, 1.f, log2S); };
     if (rank == 0 && tid == 0) {
-        if (a.out.lse) a.out.lse[row] = t.S == 0.f ? -INFINITY : t.ref + all;
+        // (ref or m is 0)
+        if (a.out.lse) a.out.lse[row] = t.S == 0.f ? -INFINITY : t.ref + fmaf(t.m, UNIT_HI, fmaf(t.m, UNIT_LO, log2S * LN2));
         if (a.out.entropy) a.out.entropy[row] = t.S == 0.f ? 0.f : (log2S - t.S2 / t.S) * LN2;
         if (a.out.logp) a.out.logp[row] = token >= 0 && token < a.r.vocab ? logp(at_token) : 0.f;
     }
