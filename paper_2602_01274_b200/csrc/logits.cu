@@ -950,9 +950,10 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
     if (TAIL) __syncthreads();
     if (tid >= THREADS - 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);     // (the warp with the fewest vectors)
 
-    // log2 p_v = (z_v - al.ref) scale - al.m - log2 al.S; of the others among themselves (w_v) the same with ot
+    // log2 p_v = (z_v - al.ref) scale - al.m - log2 al.S; of the others among themselves (w_v) the same with ot.  m (or ref scale) and
+    // log2 S are never added up: see the top of the file
     Sums al, ot;
-    float al2, ot2;                                                    // log2 of their sums
+    float al2, ot2, shift = 0.f;                                       // log2 of their sums; ot's reference over al's
     auto in_list = [&](int i) {
         bool in = false;
         if constexpr (TAIL)
@@ -968,6 +969,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
             if (d > 0.f || ot.S == 0.f) {
                 al.ref = ds.top; al.m = 0.f;
                 al.S = ds.list + (ot.S == 0.f ? 0.f : ex2(max_nan(ot2 - d, FAR)));
+                shift = ot.S == 0.f ? 0.f : -d;
                 if (ds.top == -INFINITY) { al.ref = 0.f; al.S = 0.f; }
             } else al.S = ot.S + ds.list * ex2(max_nan(d, FAR));
             al2 = al.S == 0.f ? -INFINITY : log2f(al.S);
@@ -981,10 +983,16 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
             finish();
             if (C > 1) barrier_cluster();                              // the gradient may go where the logits are
         } else {
-            al.ref = ot.ref = 0.f;
-            al2 = lse == -INFINITY ? lse : 0.f;
-            ot2 = tail == -INFINITY ? tail : 0.f;
-            al.m = lse * LOG2E; ot.m = tail * LOG2E;
+            // (a log-sum-exp times log2 e in two parts: its rounding would be as much again as the log-sum-exp's own)
+            auto given = [&](Sums &s, float l) {
+                s.m = l == -INFINITY ? 0.f : l * LOG2E;
+                const float low = l == -INFINITY ? l : fmaf(l, LOG2E, -s.m);
+                s.S = ex2(low);
+                return low;
+            };
+            al2 = given(al, lse);
+            ot2 = given(ot, tail);
+            shift = ot.m - al.m;
         }
     } else {
         PairSums<T, false> ps;
@@ -1022,19 +1030,25 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         ot = row_sums<T>(ps.m, ps.S, ps.S2, sh, sl, rank, C, scale, in_list);
         finish();
         if (rank == 0 && tid < 32) {
-            const float it = a.t.inv_temp, all = (al.m + al2) * LN2;
+            const float it = a.t.inv_temp;
             float loss = 0.f;
             for (int k = tid; k < K; k += 32) {
                 const float q = ds.q[k];
-                if (q > 0.f || isnan(q)) loss += q * ((ds.tl[k] - ds.norm) * LN2 - ((ds.zk[k] - al.ref) * it - all));
+                if (q > 0.f || isnan(q)) loss += q * ((ds.tl[k] - ds.norm) * LN2 - al.log_p(ds.zk[k], scale, it, al2));
             }
             loss = warp_add(loss);
             if (tid == 0) {
-                if (TAIL && ds.qt > 0.f) loss += ds.qt * (log2f(ds.qt) - (ot2 + (ot.ref - al.ref) * scale + (ot.m - al.m) - al2)) * LN2;
-                // (LOWEST where a finite one is out of range: -inf says that nothing is left)
+                if (TAIL && ds.qt > 0.f) loss += ds.qt * (log2f(ds.qt) - (ot2 + shift - al2)) * LN2;
                 if (a.loss) a.loss[row] = ds.any && al2 != -INFINITY ? loss : 0.f;
-                if (a.lse) a.lse[row] = al2 == -INFINITY ? al2 : max_nan(fmaf(al.ref, it, all), LOWEST);
-                if (TAIL && a.tail_lse) a.tail_lse[row] = ot2 == -INFINITY ? ot2 : max_nan(fmaf(ot.ref, it, (ot.m + ot2) * LN2), LOWEST);
+                // ref or m is 0; ref goes by the same 1 / temperature as the exponents.  (LOWEST where a finite log-sum-exp is out of
+                // range: -inf says that nothing is left)
+                const float it_hi = scale * UNIT_HI, it_lo = fmaf(scale, UNIT_HI, -it_hi) + scale * UNIT_LO;
+                auto whole = [&](const Sums &s, float log2S) {
+                    const float l = fmaf(s.ref, it_hi, fmaf(s.ref, it_lo, fmaf(s.m, UNIT_HI, fmaf(s.m, UNIT_LO, log2S * LN2))));
+                    return log2S == -INFINITY ? log2S : max_nan(l, LOWEST);
+                };
+                if (a.lse) a.lse[row] = whole(al, al2);
+                if (TAIL && a.tail_lse) a.tail_lse[row] = whole(ot, ot2);
             }
         }
     }
@@ -1043,9 +1057,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
     T *out = reinterpret_cast<T *>(a.dz) + (int64_t)row * a.ld_dz;
     const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15), none = !ds.any || al2 == -INFINITY, others = !none && ot2 != -INFINITY;
     const float g = a.weight[row] * a.t.inv_temp;
-    const float coef = !TAIL ? g * ds.Q : g * (ds.Q * ex2(max_nan(ot2 + (ot.ref - al.ref) * scale + (ot.m - al.m) - al2, FAR)) - ds.qt);
-    const float less = ot.m + ot2;
-    const f2 c0 = two(-ot.ref, -ot.ref), c1 = two(scale, scale), c2 = two(-less, -less), c3 = two(coef, coef);
+    // (w_v = 2^t / S; two roundings of the quotient at most: S is at least about 1 and below 2^35)
+    const float coef = __fdividef(!TAIL ? g * ds.Q : g * (ds.Q * ex2(max_nan(ot2 + shift - al2, FAR)) - ds.qt), ot.S);
+    const f2 c0 = two(-ot.ref, -ot.ref), c1 = two(scale, scale), c2 = two(-ot.m, -ot.m), c3 = two(coef, coef);
     auto put = [&](const uint4 &v, int j) {
         float f[E], d[E];
         Vec<T>::unpack(v, f);
@@ -1064,7 +1078,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) put(v[u], j + u * THREADS);
     }, [&](uint4 (&v)[1], int j) { put(v[0], j); });
-    if (edge >= 0) out[edge] = Vec<T>::from(others ? coef * ex2(fmaf(at_edge - ot.ref, scale, -less)) : 0.f);
+    if (edge >= 0) out[edge] = Vec<T>::from(others ? coef * ex2(ot.exponent(at_edge, scale)) : 0.f);
     __syncthreads();
     if (here) {                                                        // the list's tokens
         float qs = ds.q[tid];

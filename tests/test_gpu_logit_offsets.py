@@ -19,7 +19,7 @@ OFFSETS = [("f32", o) for o in (-9e7, -1e7, -1e5, -1e3, 0.0, 1e2, 1e3, 1e4, 1e5,
 
 
 def shifted(rows, vocab, dtype, offset, seed=50, pad=0):
-    """Noise a few steps of the type wide (two at least) around the offset."""
+    """Noise around the offset: of width 2, or more where the type's steps there are coarser (some then tell hardly any logits apart)."""
     step = 2.0 ** math.floor(math.log2(max(abs(offset), 1.0))) * torch.finfo(TYPES[dtype]).eps
     z = make_logits(rows, vocab, "f32", pad, seed=seed) * max(1.0, 0.7 * step if step < 16 else 0.1 * step)
     z = z + offset
@@ -109,3 +109,74 @@ def test_the_gradient_of_rows_with_an_offset(dtype, offset, rows, vocab):
     # (further down p falls faster than its logarithm grows)
     flushed = 2.0 ** -126 * 100 * sum(x.double().abs() for x in g)[:, None]
     close(got, want, half * 1.01 * want.abs() + (180 * ref.F32 + EPS + shared) * terms + gh * p * (41 * EPS + shared) + least + flushed, "dlogits")
+
+
+def make_list(z, k, temperature, tail, seed=60):
+    """A teacher's list without repetitions, and its log-sum-exp with three tenths to a half of the mass outside."""
+    rows, vocab = z.shape
+    ids = torch.rand(rows, vocab, generator=gen(seed), device=DEV).topk(k, 1).indices.to(torch.int32)
+    t = torch.randn(rows, k, generator=gen(seed + 1), device=DEV) * 2
+    lse = torch.logsumexp(t / temperature, 1) + 0.4 + 0.2 * torch.rand(rows, generator=gen(seed + 2), device=DEV) if tail else None
+    return ids, t, lse
+
+
+def check_distill(z, ids, t, temperature, tl):
+    """Loss, one-pass and two-call gradient against 64 bits and against each other.  log p of a listed token, and of the tail, is right to
+    EPS and six half steps of its size, and comes in times q, which is right to 100 half steps (exponents of the teacher's values below 30,
+    four roundings of half a step of at most 32 * 0.7, a sum of 20, two exponentials); with a tail, q_t = 1 - sum q is right to 2 EPS, times a logarithm of at most 30 for p_t of the
+    rows here that have one (or of log p_t's size, which the six half steps of the loss's size and 2 EPS of it cover).  The
+    gradient's terms: 4 EPS as in tests/test_gpu_logits.py (exponents down to -126 with five half steps each are 2.6 EPS), what the exponential
+    flushes below 2^-126 (p and w, each times at most 1), and for the second call what its lse below 1024 is off, two half steps."""
+    from paper_2602_01274_b200 import binding as b
+    rows, vocab = z.shape
+    w = torch.randn(rows, generator=gen(63), device=DEV)
+    loss0, lse0, tail0, d0, terms = ref.distill(z, ids, t, temperature, tl, w)
+    top = z.double().amax(1, keepdim=True)
+    logs = size(ref.softmax_parts((z.double() - top) / temperature)[0].gather(1, ids.long())).amax(1)
+    loss, lse, tail = b.pacer_distill(z, ids, t, temperature, tl)
+    close(loss, loss0, (4 if tl is None else 64) * EPS + 106 * ref.F32 * logs + (0 if tl is None else (2 * EPS + 6 * ref.F32) * size(loss0)), "loss")
+    close(lse, lse0, EPS + 4 * ref.F32 * size(lse0), "lse")
+    if tl is not None:
+        close(tail, tail0, EPS + 4 * ref.F32 * size(tail0), "tail")
+    half, least = ref.rounding(z.dtype)
+    flushed = (2 * 2.0 ** -126 * w.double().abs() / temperature)[:, None]
+    loss1, d1 = b.pacer_distill_grad(z, ids, t, w, temperature, tl)
+    assert torch.equal(loss1, loss)
+    close(d1, d0, half * 1.01 * d0.abs() + 4 * EPS * terms + least + flushed, "one pass")
+    shared = torch.where(lse0.abs() < 1024, 2 * ref.F32 * lse0.abs(), 0.0)
+    if tl is not None:
+        shared = shared + torch.where(tail0.abs() < 1024, 2 * ref.F32 * tail0.abs(), 0.0)
+    d2 = b.pacer_distill_backward(z, ids, t, lse, tail, w, temperature, tl)
+    close(d2, d0, half * 1.01 * d0.abs() + (4 * EPS + shared[:, None]) * terms + least + flushed, "two calls")
+    if z.dtype == torch.float32:                        # a row's gradient sums to 0
+        for d, more in ((d1, 0.0), (d2, shared)):
+            assert (d.double().sum(1).abs() <= (4 * EPS + more) * terms.sum(1) + vocab * flushed[:, 0]).all()
+    copy = z.clone()
+    assert torch.equal(b.pacer_distill_grad(copy, ids, t, w, temperature, tl, out=copy)[1], d1)
+    copy = z.clone()
+    assert torch.equal(b.pacer_distill_backward(copy, ids, t, lse, tail, w, temperature, tl, out=copy), d2)
+
+
+@pytest.mark.parametrize("dtype,offset", OFFSETS)
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distillation_of_a_student_with_an_offset(dtype, offset, temperature, tail):
+    for rows, vocab, k in ((3, 4096, 20), (600, 1031, 5)):
+        z = shifted(rows, vocab, dtype, offset)
+        check_distill(z, *make_list(z, k, temperature, tail)[:2], temperature, make_list(z, k, temperature, tail)[2])
+
+
+@pytest.mark.parametrize("offset", [0.0, 20.0, -500.0])
+def test_distillation_at_the_lowest_temperature(offset):
+    z = make_logits(6, 2000, "f32", seed=64) + offset
+    ids, t, _ = make_list(z, 9, 1e-3, False)
+    check_distill(z, ids, t * 1e-3, 1e-3, None)
+
+
+@pytest.mark.parametrize("mask", [-1e3, -1e5, -1e6, -1e7, -9e7])
+def test_distillation_with_a_masked_tail(mask):
+    """All tokens outside the list masked with one finite value: they share the tail's part evenly."""
+    z = make_logits(6, 3001, "f32", seed=65)
+    ids, t, tl = make_list(z, 12, 1.0, True)
+    z = torch.full_like(z, mask).scatter(1, ids.long(), z.gather(1, ids.long()))
+    check_distill(z, ids, t, 1.0, tl)
