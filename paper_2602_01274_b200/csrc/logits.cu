@@ -840,11 +840,11 @@ struct DistillArgs {
 
 struct DistillSlots {
     alignas(16) int32_t id[MAX_K + 4];
-    float tl[MAX_K], zk[MAX_K];            // teacher's entry as an exponent (-inf: no entry), student's logit
+    float tl[MAX_K], zk[MAX_K];            // teacher's value (-inf: no entry), from list_sums on log2 q; student's logit
     float q[MAX_K];
     uint8_t first[MAX_K];                  // 1: the first entry of its id
     unsigned long long listed[THREADS];    // a tail: which of a thread's vectors hold listed tokens
-    float Q, qt, norm, top, list;          // sum q, the rest, log2 of the teacher's sum; largest listed logit, sum 2^((zk - top) scale)
+    float Q, qt, top, list;                // sum q, the rest; largest listed logit, sum 2^((zk - top) scale)
     int32_t any;
 };
 
@@ -860,10 +860,12 @@ __device__ __forceinline__ float load_any(const void *p, int64_t i, int dtype) {
 }
 
 // The list's own sums, by one warp: q, Q, q_t, and (a tail) the listed tokens' sum of exponentials over their largest logit.
+// log2 q = (t - ref) scale - log2 sum: differences of the teacher's values come first here too.  With the teacher's own log-sum-exp L at
+// this temperature it is (t - L temperature) scale, the difference by one fused multiply-add.
 template <bool TAIL>
-__device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, float teacher_lse) {
+__device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, float teacher_lse, float temp) {
     const int lane = threadIdx.x & 31;
-    float norm, top = -INFINITY, tm = -INFINITY;
+    float top = -INFINITY, tm = -INFINITY, ref = 0.f, log2sum = 0.f;
     bool any = false;
     for (int k = lane; k < K; k += 32) {
         any |= ds.id[k] >= 0;
@@ -872,19 +874,21 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
     }
     any = __any_sync(~0u, any);
     if (TAIL) {
-        norm = teacher_lse * LOG2E;
+        if (teacher_lse == -INFINITY) log2sum = -INFINITY;             // (the teacher allows nothing)
         top = warp_max(top);
     } else {
         tm = warp_max(tm);
-        const float ref = tm == -INFINITY ? 0.f : tm;
+        ref = tm == -INFINITY ? 0.f : tm;
         float sum = 0.f;
-        for (int k = lane; k < K; k += 32) sum += ex2(ds.tl[k] - ref);
-        norm = ref + log2f(warp_add(sum));                             // -inf: no entry that the teacher allows
+        for (int k = lane; k < K; k += 32) sum += ex2((ds.tl[k] - ref) * scale);
+        log2sum = log2f(warp_add(sum));                                // -inf: no entry that the teacher allows
     }
     const float over = top == -INFINITY ? 0.f : top;                   // (the student excludes all of them: their sum is 0)
     float Q = 0.f, list = 0.f;
     for (int k = lane; k < K; k += 32) {
-        const float q = ds.id[k] >= 0 && norm != -INFINITY ? ex2(ds.tl[k] - norm) : 0.f;
+        const float log2q = (TAIL ? fmaf(-teacher_lse, temp, ds.tl[k]) : ds.tl[k] - ref) * scale - log2sum;
+        const float q = ds.id[k] >= 0 && log2sum != -INFINITY ? ex2(log2q) : 0.f;
+        ds.tl[k] = log2q;
         ds.q[k] = q;
         Q += q;
         if (TAIL && ds.first[k]) list += ex2(max_nan((ds.zk[k] - over) * scale, FAR));
@@ -893,7 +897,7 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
     if (TAIL) list = warp_add(list);
     if (lane == 0) {
         const float qt = TAIL ? fmaxf(0.f, 1.f - Q) : 0.f;
-        ds.Q = Q + qt; ds.qt = qt; ds.norm = norm; ds.top = top; ds.list = list; ds.any = any;
+        ds.Q = Q + qt; ds.qt = qt; ds.top = top; ds.list = list; ds.any = any;
     }
 }
 
@@ -925,7 +929,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         id = a.t.ids[(int64_t)row * K + tid];
         if (id < 0 || id >= V) id = -1;
         ds.id[tid] = id;
-        ds.tl[tid] = id >= 0 ? load_any(a.t.t, (int64_t)row * K + tid, a.t.dtype) * scale : -INFINITY;
+        ds.tl[tid] = id >= 0 ? load_any(a.t.t, (int64_t)row * K + tid, a.t.dtype) : -INFINITY;
     } else if (tid < K + 4) ds.id[tid] = -1;                           // (ids are compared four at a time)
     if (marked) ds.listed[tid] = 0;
     const float at_edge = edge >= 0 ? Vec<T>::to(z[edge]) : 0.f, my_z = id >= 0 ? Vec<T>::to(z[id]) : -INFINITY;
@@ -948,7 +952,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         if (i >= 0 && i < sh.hi - sh.lo) atomicOr(ds.listed + i % THREADS, 1ull << i / THREADS);
     }
     if (TAIL) __syncthreads();
-    if (tid >= THREADS - 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f);     // (the warp with the fewest vectors)
+    if (tid >= THREADS - 32) list_sums<TAIL>(ds, K, scale, TAIL ? a.t.lse[row] : 0.f, a.t.temp);     // (the warp with the fewest vectors)
 
     // log2 p_v = (z_v - al.ref) scale - al.m - log2 al.S; of the others among themselves (w_v) the same with ot.  m (or ref scale) and
     // log2 S are never added up: see the top of the file
@@ -1034,7 +1038,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
             float loss = 0.f;
             for (int k = tid; k < K; k += 32) {
                 const float q = ds.q[k];
-                if (q > 0.f || isnan(q)) loss += q * ((ds.tl[k] - ds.norm) * LN2 - al.log_p(ds.zk[k], scale, it, al2));
+                if (q > 0.f || isnan(q)) loss += q * (ds.tl[k] * LN2 - al.log_p(ds.zk[k], scale, it, al2));
             }
             loss = warp_add(loss);
             if (tid == 0) {

@@ -41,7 +41,7 @@ struct Teacher {
     const void *t;                         // [rows][k]
     int32_t dtype, k;
     const float *lse;                      // [rows] or NULL: the list is renormalised
-    float inv_temp;
+    float temp, inv_temp;                  // the temperature and one over it
 };
 
 // loss, lse, tail_lse: [rows], each may be NULL.  dz (may be NULL): weight[row] times the gradient of loss[row].

@@ -1052,7 +1052,7 @@ extern "C" int pacer_distill(const void *logits, int dtype, int64_t ld, int rows
         REFUSE_IF(rows && !weight, "dlogits without weight");
     }
     if (!rows) return PACER_OK;
-    CK(lg::distill({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, 1.f / temperature}, loss, lse, tail_lse,
+    CK(lg::distill({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, temperature, 1.f / temperature}, loss, lse, tail_lse,
                    weight, dlogits, ld_dlogits, (cudaStream_t)cuda_stream));
     return PACER_OK;
 }
@@ -1068,7 +1068,7 @@ extern "C" int pacer_distill_backward(const void *logits, int dtype, int64_t ld,
     if (!rows) return PACER_OK;
     REFUSE_IF(!lse || !g_loss, "lse or g_loss is null");
     REFUSE_IF(teacher_lse && !tail_lse, "teacher_lse without tail_lse");
-    CK(lg::distill_backward({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, 1.f / temperature}, lse, tail_lse,
+    CK(lg::distill_backward({logits, dtype, ld, rows, vocab}, {ids, teacher, teacher_dtype, k, teacher_lse, temperature, 1.f / temperature}, lse, tail_lse,
                             g_loss, dlogits, ld_dlogits, (cudaStream_t)cuda_stream));
     return PACER_OK;
 }

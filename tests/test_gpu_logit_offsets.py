@@ -180,3 +180,27 @@ def test_distillation_with_a_masked_tail(mask):
     ids, t, tl = make_list(z, 12, 1.0, True)
     z = torch.full_like(z, mask).scatter(1, ids.long(), z.gather(1, ids.long()))
     check_distill(z, ids, t, 1.0, tl)
+
+
+@pytest.mark.parametrize("teacher,offset", [("f32", o) for o in (-3e38, -9e7, -1e5, 1e3, 1e5, 1e6, 9e7, 3e38)] +
+                         [("bf16", -3e38), ("bf16", 1e4), ("f16", -6e4), ("f16", 6e4)])
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 3.0])
+def test_a_teacher_with_an_offset(teacher, offset, temperature):
+    """Values that share an offset: the renormalised list is that of their differences."""
+    z = make_logits(40, 3001, "f32", seed=66)
+    ids = make_list(z, 20, 1.0, False)[0]
+    t = shifted(40, 20, teacher, offset, seed=67) if abs(offset) < 1e30 else torch.full((40, 20), offset, device=DEV).to(TYPES[teacher])
+    t[:20, ::3] = torch.finfo(t.dtype).min if offset > -1e30 else -math.inf       # some that the teacher masks
+    t[7] = torch.finfo(t.dtype).min                                               # ... and all of them alike
+    check_distill(z, ids, t, temperature, None)
+
+
+@pytest.mark.parametrize("teacher,offset", [("f32", -1e6), ("f32", -1e4), ("f32", 1e3), ("f32", 1e5), ("bf16", 1e4), ("f16", 6e4)])
+@pytest.mark.parametrize("temperature", [0.5, 0.7, 1.0, 3.0])
+def test_a_teacher_with_an_offset_and_a_tail(teacher, offset, temperature):
+    """q from the given values, the given log-sum-exp, which f32 holds to 0.03 at 1e6, and the given temperature, an f32 number too."""
+    temperature = float(torch.tensor(temperature, dtype=torch.float32))
+    z = make_logits(40, 3001, "f32", seed=66)
+    ids = make_list(z, 20, 1.0, False)[0]
+    t = (shifted(40, 20, "f32", 0.0, seed=67) + offset).to(TYPES[teacher])
+    check_distill(z, ids, t, temperature, (torch.logsumexp(t.double() / temperature, 1) + 0.5).float())
