@@ -340,7 +340,9 @@ int pacer_logprobs_backward(const void *logits, int dtype, int64_t ld, int rows,
  * teacher: [rows][k] logits (or log probabilities) of type teacher_dtype.  teacher_lse NULL: q = softmax(teacher / temperature)
  * over the list.  teacher_lse f32 [rows]: the log-sum-exp of the teacher's whole row AT THIS TEMPERATURE;
  * q_k = exp(teacher_k / temperature - teacher_lse), and all tokens outside the list form one further class with
- * q_t = max(0, 1 - sum_k q_k), p_t the student's mass outside the list.
+ * q_t = max(0, 1 - sum_k q_k), p_t the student's mass outside the list.  Where p_t is 0 in f32 (the list holds all that the student
+ * allows) the loss is infinite, or as large as the masks are, unless q_t is no more than what rounding may leave of 1 - sum_k q_k,
+ * 2^-24 (40 + 4 |teacher_lse|): it then counts as 0.
  * A row without entries has loss 0 and gradient 0.  loss, lse (of z / temperature), tail_lse (the log-sum-exp of z / temperature
  * over the tokens outside the list; only with teacher_lse): f32 [rows], each may be NULL.
  * dlogits (may be NULL): weight[row] (f32 [rows]) times the gradient of loss[row], in the logits' type, in the same pass; it may be

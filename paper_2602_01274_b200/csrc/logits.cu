@@ -844,7 +844,7 @@ struct DistillSlots {
     float q[MAX_K];
     uint8_t first[MAX_K];                  // 1: the first entry of its id
     unsigned long long listed[THREADS];    // a tail: which of a thread's vectors hold listed tokens
-    float Q, qt, top, list;                // sum q, the rest; largest listed logit, sum 2^((zk - top) scale)
+    float Q, qt, least, top, list;         // sum q, the rest, what may be rounding of it; largest listed logit, sum 2^((zk - top) scale)
     int32_t any;
 };
 
@@ -897,6 +897,9 @@ __device__ __forceinline__ void list_sums(DistillSlots &ds, int K, float scale, 
     if (TAIL) list = warp_add(list);
     if (lane == 0) {
         const float qt = TAIL ? fmaxf(0.f, 1.f - Q) : 0.f;
+        // q_t where the list holds all of the teacher's mass: Q is off by 40 half steps at most (two exponentials' four, a sum's 13, and
+        // three of each exponent's size, which is the list's entropy of at most ln 256 on average), the given log-sum-exp by a few of its size
+        if (TAIL) ds.least = 5.9604645e-8f * fmaf(4.f, fabsf(teacher_lse), 40.f);
         ds.Q = Q + qt; ds.qt = qt; ds.top = top; ds.list = list; ds.any = any;
     }
 }
@@ -1042,7 +1045,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
             }
             loss = warp_add(loss);
             if (tid == 0) {
-                if (TAIL && ds.qt > 0.f) loss += ds.qt * (log2f(ds.qt) - (ot2 + shift - al2)) * LN2;
+                // (a student without a tail, p_t = 0 in f32: a q_t that may be rounding is none, else the loss would be infinite for it)
+                const float pt2 = ot2 + shift - al2;
+                if (TAIL && ds.qt > 0.f && !(pt2 < -149.f && ds.qt <= ds.least)) loss += ds.qt * (log2f(ds.qt) - pt2) * LN2;
                 if (a.loss) a.loss[row] = ds.any && al2 != -INFINITY ? loss : 0.f;
                 // ref or m is 0; ref goes by the same 1 / temperature as the exponents.  (LOWEST where a finite log-sum-exp is out of
                 // range: -inf says that nothing is left)

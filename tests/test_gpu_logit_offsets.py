@@ -204,3 +204,30 @@ def test_a_teacher_with_an_offset_and_a_tail(teacher, offset, temperature):
     ids = make_list(z, 20, 1.0, False)[0]
     t = (shifted(40, 20, "f32", 0.0, seed=67) + offset).to(TYPES[teacher])
     check_distill(z, ids, t, temperature, (torch.logsumexp(t.double() / temperature, 1) + 0.5).float())
+
+
+@pytest.mark.parametrize("k", [1, 5, 64, 256])
+@pytest.mark.parametrize("level", [0.0, 20.0, -100.0, 1000.0])
+@pytest.mark.parametrize("outside", [None, -math.inf, -1e9, -3e38, -300.0])
+def test_no_tail_of_either_has_a_finite_loss(k, level, outside):
+    """A list that holds all of the teacher's and all of the student's mass: 1 - sum q is a rounding, not a tail."""
+    from paper_2602_01274_b200 import binding as b
+    rows, vocab = 500, k if outside is None else k + 300
+    inside = torch.randn(rows, k, generator=gen(70), device=DEV)
+    z = torch.full((rows, vocab), outside or 0.0, device=DEV)
+    ids = torch.rand(rows, vocab, generator=gen(71), device=DEV).topk(k, 1).indices
+    z.scatter_(1, ids, inside)
+    ids = ids.to(torch.int32)
+    t = torch.randn(rows, k, generator=gen(72), device=DEV) * 2 + level
+    tl, w = torch.logsumexp(t, 1), torch.ones(rows, device=DEV)
+    want, _, _, d0, terms = ref.distill(z, ids, t, 1.0, None, w)       # (the list renormalised)
+    logs = size(ref.softmax_parts(z.double())[0].gather(1, ids.long())).amax(1)
+    # the q sum to 1 but for the log-sum-exp's own rounding and the list's: 2^-24 (40 + 4 |lse|), times logarithms of at most logs + 20
+    rest = ref.F32 * (40 + 4 * tl.double().abs())
+    loss, d = b.pacer_distill_grad(z, ids, t, w, 1.0, tl)
+    close(loss, want, 4 * EPS + 106 * ref.F32 * logs + rest * (logs + 20), "loss")
+    others = torch.ones_like(z, dtype=torch.bool).scatter(1, ids.long(), False)
+    close(d, d0, 4 * EPS * terms + 2 * rest[:, None] * torch.where(others, 1.0, terms), "gradient")
+    # what is more than a rounding is a tail
+    loss, _, tail = b.pacer_distill(z, ids, t, 1.0, tl + 0.05 * max(1.0, abs(level)))
+    assert (loss > 5.0).all() and (outside is not None and outside > -1e38 or (loss > 1e30).all())
