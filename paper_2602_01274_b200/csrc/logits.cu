@@ -977,7 +977,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
                 al.ref = ds.top; al.m = 0.f;
                 al.S = ds.list + (ot.S == 0.f ? 0.f : ex2(max_nan(ot2 - d, FAR)));
                 shift = ot.S == 0.f ? 0.f : -d;
-                if (ds.top == -INFINITY) { al.ref = 0.f; al.S = 0.f; }
+                if (ds.top == -INFINITY) al.ref = 0.f;                 // (the list's sum over 0: 0 or, of NaN, NaN)
             } else al.S = ot.S + ds.list * ex2(max_nan(d, FAR));
             al2 = al.S == 0.f ? -INFINITY : log2f(al.S);
         }
@@ -1064,7 +1064,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
     if (MODE == LOSS) return;
 
     T *out = reinterpret_cast<T *>(a.dz) + (int64_t)row * a.ld_dz;
-    const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15), none = !ds.any || al2 == -INFINITY, others = !none && ot2 != -INFINITY;
+    const bool same = ((uintptr_t)z & 15) == ((uintptr_t)out & 15), none = !ds.any || al2 == -INFINITY, others = !none && (ot2 != -INFINITY || isnan(al2));
     const float g = a.weight[row] * a.t.inv_temp;
     // (w_v = 2^t / S; two roundings of the quotient at most: S is at least about 1 and below 2^35)
     const float coef = __fdividef(!TAIL ? g * ds.Q : g * (ds.Q * ex2(max_nan(ot2 + shift - al2, FAR)) - ds.qt), ot.S);

@@ -231,3 +231,30 @@ def test_no_tail_of_either_has_a_finite_loss(k, level, outside):
     # what is more than a rounding is a tail
     loss, _, tail = b.pacer_distill(z, ids, t, 1.0, tl + 0.05 * max(1.0, abs(level)))
     assert (loss > 5.0).all() and (outside is not None and outside > -1e38 or (loss > 1e30).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab,k", [(64, 64), (256, 256), (3, 3), (4099, 20)])
+def test_rows_with_nan_are_nan_whatever_the_list_holds(dtype, vocab, k):
+    """NaN inside the list, outside it and everywhere, beside -inf and beside numbers, with a tail and without."""
+    from paper_2602_01274_b200 import binding as b
+    z = make_logits(7, vocab, dtype, seed=80)
+    ids = torch.arange(k, device=DEV, dtype=torch.int32).flip(0).repeat(7, 1)
+    z[0] = math.nan
+    z[1] = -math.inf
+    z[1, k - 1] = math.nan                              # one listed NaN, nothing else left
+    z[2, 0] = math.nan
+    z[3, -1] = math.nan
+    z[4, k:] = math.nan                                 # (nothing where the list is the whole vocabulary)
+    t = torch.randn(7, k, generator=gen(81), device=DEV)
+    w = torch.ones(7, device=DEV)
+    bad = [0, 1, 2, 3] + ([4] if vocab > k else [])
+    good = [r for r in range(7) if r not in bad]
+    for tl in (None, torch.logsumexp(t, 1) + 0.3):
+        loss, lse, tail = b.pacer_distill(z, ids, t, 1.0, tl)
+        _, d = b.pacer_distill_grad(z, ids, t, w, 1.0, tl)
+        d2 = b.pacer_distill_backward(z, ids, t, lse, tail, w, 1.0, tl)
+        for r in bad:
+            assert torch.isnan(loss[r]) and torch.isnan(lse[r]) and torch.isnan(d[r]).all() and torch.isnan(d2[r]).all(), (r, tl is None)
+        for r in good:
+            assert not torch.isnan(loss[r]) and torch.isfinite(lse[r]) and torch.isfinite(d[r]).all() and torch.isfinite(d2[r]).all(), (r, tl is None)
