@@ -310,7 +310,8 @@ enum { PACER_F32 = 0, PACER_BF16 = 1, PACER_F16 = 2 };
 #define PACER_MAX_DISTILL_K 256
 
 /* Log probabilities of given tokens, with entropy and the best alternatives of every row:
- *   lse = log sum_v exp(z_v), logp = z[token] - lse, entropy = -sum_v p_v log p_v (nats).
+ *   lse = log sum_v exp(z_v), logp = z[token] - lse, entropy = -sum_v p_v log p_v (nats); logp <= 0 and entropy >= 0.
+ * They go by the logits' differences: what a row's logits have in common costs logp, entropy and top_logp no accuracy.
  * tokens: int32 [rows] or NULL; a token outside [0, vocab) (-1, say) names nothing: logp 0.  top (0 .. min(PACER_MAX_TOP, vocab)):
  * top_ids int32 [rows][top] and top_logp f32 [rows][top] are the best tokens in order: larger logit first, of equal ones the
  * lower id, NaN last.  Every output may be NULL. */

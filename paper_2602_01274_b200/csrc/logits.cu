@@ -274,10 +274,11 @@ __device__ __forceinline__ float warp_max(float v) {
 struct Sums {
     float ref = 0.f, m = 0.f, S = 0.f, S2 = 0.f;
     __device__ float exponent(float z, float scale) const { return fmaf(z - ref, scale, -m); }
-    // log p of a logit from its exponent (whose range a finite logit far below the others may leave where its log p does not)
+    // log p of a logit from its exponent (whose range a finite logit far below the others may leave where its log p does not).  At most 0:
+    // m is a rounded product, so the only token of a row has 2^t a rounding off 1, and log S one off t
     __device__ float log_p(float z, float scale, float inv_temp, float log2S) const {
         const float e = exponent(z, scale) - log2S;
-        return e == -INFINITY ? (z - ref) * inv_temp - (m + log2S) * LN2 : e * LN2;
+        return e == -INFINITY ? (z - ref) * inv_temp - (m + log2S) * LN2 : e > 0.f ? 0.f : e * LN2;
     }
 };
 
@@ -708,7 +709,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_logprobs(const ScoreArgs a)
     if (rank == 0 && tid == 0) {
         // (ref or m is 0)
         if (a.out.lse) a.out.lse[row] = t.S == 0.f ? -INFINITY : t.ref + fmaf(t.m, UNIT_HI, fmaf(t.m, UNIT_LO, log2S * LN2));
-        if (a.out.entropy) a.out.entropy[row] = t.S == 0.f ? 0.f : (log2S - t.S2 / t.S) * LN2;
+        const float h = log2S - t.S2 / t.S;                            // (at least 0, as log p is at most 0)
+        if (a.out.entropy) a.out.entropy[row] = t.S == 0.f || h < 0.f ? 0.f : h * LN2;
         if (a.out.logp) a.out.logp[row] = token >= 0 && token < a.r.vocab ? logp(at_token) : 0.f;
     }
     if (!TOP) return;

@@ -258,3 +258,20 @@ def test_rows_with_nan_are_nan_whatever_the_list_holds(dtype, vocab, k):
             assert torch.isnan(loss[r]) and torch.isnan(lse[r]) and torch.isnan(d[r]).all() and torch.isnan(d2[r]).all(), (r, tl is None)
         for r in good:
             assert not torch.isnan(loss[r]) and torch.isfinite(lse[r]) and torch.isfinite(d[r]).all() and torch.isfinite(d2[r]).all(), (r, tl is None)
+
+
+@pytest.mark.parametrize("rows,vocab", [(2000, 1), (2000, 7), (2000, 1000), (300, 32003), (40, 151936)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_no_probability_above_one(rows, vocab, dtype):
+    """Rows that are sure of one token: no log probability above 0, no entropy below."""
+    from paper_2602_01274_b200 import binding as b
+    z = torch.randn(rows, vocab, generator=gen(90), device=DEV) * 10
+    at = torch.randint(0, vocab, (rows, 1), generator=gen(91), device=DEV)
+    z.scatter_(1, at, z.amax(1, keepdim=True) + 40 * torch.rand(rows, 1, generator=gen(92), device=DEV))
+    logp, ent, _, _, tlp = check_rows(z.to(TYPES[dtype]), at[:, 0].to(torch.int32), min(vocab, 3))
+    assert (logp <= 0).all() and (tlp <= 0).all() and (ent >= 0).all()
+    h, w = torch.zeros(rows, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(min(vocab, 4099), 64, dtype=torch.bfloat16, device=DEV)
+    h[:, 0] = 1 + torch.rand(rows, generator=gen(93), device=DEV)
+    w[:, 0] = z[0, :len(w)]
+    logp, ent, _ = b.pacer_head_logprobs(h, w, w[:, 0].argmax().to(torch.int32).expand(rows))
+    assert (logp <= 0).all() and (ent >= 0).all()
