@@ -431,6 +431,14 @@ def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
     return out
 
 
+def _written(*outputs: Optional[torch.Tensor]):
+    """Tensors of the caller that a call has written: autograd has to know, as of torch's own in-place functions, so that a backward
+    pass which saved them (or what they are views of) says so instead of computing with what is there now."""
+    for t in outputs:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 # torch.cuda.current_stream(..).cuda_stream, where torch has it without the object that costs 2 us a call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
@@ -466,6 +474,8 @@ def pacer_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, out
             assert t.shape == shape and t.dtype == dtype and t.device == dev and t.is_contiguous(), f"out: contiguous {dtype} {shape} on {dev}"
     _call(_lib.pacer_logprobs, z, *_layout(z), _ptr(tokens), top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), ids.data_ptr(),
           top_logp.data_ptr())
+    if out is not None:
+        _written(*out)
     return logp, entropy, lse, ids, top_logp
 
 
@@ -476,9 +486,10 @@ def pacer_logprobs_backward(logits, tokens, lse, entropy, grad_logp, grad_entrop
     f32 = torch.float32
     tokens, lse, entropy = _vec(tokens, "tokens", z, torch.int32), _vec(lse, "lse", z, f32), _vec(entropy, "entropy", z, f32)
     gl, gh, gs = _vec(grad_logp, "grad_logp", z, f32), _vec(grad_entropy, "grad_entropy", z, f32), _vec(grad_lse, "grad_lse", z, f32)
-    out = _out_like(z, out)
+    given, out = out, _out_like(z, out)
     _call(_lib.pacer_logprobs_backward, z, *_layout(z), _ptr(tokens), _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), out.data_ptr(),
           _ld(out))
+    _written(given)
     return out
 
 
@@ -508,10 +519,12 @@ def pacer_distill_grad(logits, ids, teacher, weight, temperature: float = 1.0, t
     type; `out` may be the logits themselves): (loss, dlogits)."""
     z = _rows(logits)
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
-    weight, out = _vec(weight, "weight", z, torch.float32), _out_like(z, out)
+    weight = _vec(weight, "weight", z, torch.float32)
+    given, out = out, _out_like(z, out)
     loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
     _call(_lib.pacer_distill, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse), temperature,
           loss.data_ptr(), None, None, _ptr(weight), out.data_ptr(), _ld(out))
+    _written(given)
     return loss, out
 
 
@@ -521,9 +534,10 @@ def pacer_distill_backward(logits, ids, teacher, lse, tail_lse, grad_loss, tempe
     ids, teacher, teacher_lse, k = _teacher(z, ids, teacher, teacher_lse)
     f32 = torch.float32
     lse, tail_lse, grad_loss = _vec(lse, "lse", z, f32), _vec(tail_lse, "tail_lse", z, f32), _vec(grad_loss, "grad_loss", z, f32)
-    out = _out_like(z, out)
+    given, out = out, _out_like(z, out)
     _call(_lib.pacer_distill_backward, z, *_layout(z), ids.data_ptr(), teacher.data_ptr(), _DTYPES[teacher.dtype], k, _ptr(teacher_lse),
           temperature, _ptr(lse), _ptr(tail_lse), _ptr(grad_loss), out.data_ptr(), _ld(out))
+    _written(given)
     return out
 
 

@@ -164,3 +164,44 @@ def test_draft_training_runs_and_its_gradient_is_right():
     prompt = synth.make_prompts(cfg.target.vocab, 1, 32, seed=4).numpy()
     assert (ctx.pacer_generate(prompt, 24, cfg.gamma_cap, -1.0)[0] == ctx.pacer_generate_ar(prompt, 24)[0]).all()
     ctx.close()
+
+
+def test_autograd_sees_what_calls_write():
+    """Outputs of the caller count as changed in place: a backward pass that saved them raises, as with torch's own functions."""
+    from paper_2602_01274_b200 import binding as b, losses
+    tokens = make_tokens(12, 333)
+    ids, t, _ = make_teacher(12, 333, 5, False, 1.0)
+    w = torch.ones(12, device=DEV)
+    leaf = make_logits(12, 333, "f32", seed=46).requires_grad_(True)
+
+    def saved():
+        z = leaf * 1.0
+        logp, _, lse, _, _ = losses.token_logprobs(z, tokens)
+        return z.detach(), logp, lse.detach()
+
+    z, logp, lse = saved()
+    ent = b.pacer_logprobs(z, tokens)[1]
+    saved_loss, saved_lse, _ = b.pacer_distill(z, ids, t)
+    writes = [lambda z: b.pacer_distill_grad(z, ids, t, w, out=z), lambda z: b.pacer_logprobs_backward(z, tokens, lse, ent, w, out=z),
+              lambda z: b.pacer_distill_backward(z, ids, t, saved_lse, None, w, out=z),
+              lambda z: b.pacer_distill_grad(z.clone(), ids, t, w, out=z), lambda z: b.pacer_logprobs_backward(z[:5], tokens[:5], lse[:5], ent[:5], w[:5], out=z[:5])]
+    for write in writes:
+        z, logp, _ = saved()
+        write(z)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            logp.sum().backward()
+    out = [torch.empty(12, device=DEV) for _ in range(3)] + [torch.empty(12, 2, dtype=torch.int32, device=DEV), torch.empty(12, 2, device=DEV)]
+    x = torch.ones(12, device=DEV, requires_grad=True)
+    y = x * out[0]                                      # (saves out[0])
+    b.pacer_logprobs(z, tokens, 2, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    # outputs that the call makes, and calls that write nothing of the caller's, disturb nothing
+    z, logp, lse = saved()
+    b.pacer_distill_grad(z, ids, t, w)
+    b.pacer_logprobs_backward(z, tokens, lse, ent, w)
+    logp.sum().backward()
+    assert torch.isfinite(leaf.grad).all()
+    with torch.inference_mode():
+        z = make_logits(12, 333, "f32", seed=46)
+        b.pacer_distill_grad(z, ids, t, w, out=z)
