@@ -107,3 +107,11 @@ def test_no_rows():
     h, w, _, _ = make(1, 100, 64)
     e = torch.empty(0, dtype=torch.int32, device=DEV)
     assert [tuple(x.shape) for x in b.pacer_head_logprobs(h[:0], w, e)] == [(0,)] * 3
+
+
+@pytest.mark.parametrize("rows,vocab,d", [(1025, 4099, 72), (1100, 32003, 136), (1152, 257, 1024), (1300, 33, 8), (1664, 5003, 256)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_pairs_of_blocks_over_an_odd_number_of_row_tiles(rows, vocab, d, biased):
+    """From nine tiles of 128 rows on pairs of blocks work on odd numbers of them too: the second block's last tile has no rows."""
+    assert -(-rows // 128) % 2 == 1
+    test_head_logprobs(rows, vocab, d, 0, biased)
