@@ -344,6 +344,7 @@ int pacer_logprobs_backward(const void *logits, int dtype, int64_t ld, int rows,
  * q_t = max(0, 1 - sum_k q_k), p_t the student's mass outside the list.  Where p_t is 0 in f32 (the list holds all that the student
  * allows) the loss is infinite, or as large as the masks are, unless q_t is no more than what rounding may leave of 1 - sum_k q_k,
  * 2^-24 (40 + 4 |teacher_lse|): it then counts as 0.
+ * (With teacher_lse the time grows with k where many of a row's 16-byte vectors hold a listed token.)
  * A row without entries has loss 0 and gradient 0.  loss, lse (of z / temperature), tail_lse (the log-sum-exp of z / temperature
  * over the tokens outside the list; only with teacher_lse): f32 [rows], each may be NULL.
  * dlogits (may be NULL): weight[row] (f32 [rows]) times the gradient of loss[row], in the logits' type, in the same pass; it may be

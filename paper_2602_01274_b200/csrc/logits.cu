@@ -31,7 +31,7 @@ constexpr float UNIT_HI = (float)(1.0 / (double)LOG2E), UNIT_LO = (float)(1.0 / 
 constexpr float LOWEST = -3.402823466e38f, SLACK = 16.f;
 constexpr float FAR = -1000.f;             // exponents are cut here: 2^FAR is 0, and 0 * FAR too
 constexpr float HUGE_M = 1e8f;
-constexpr float LSE_EXACT = 1024.f;        // a larger f32 log-sum-exp says a row's probabilities to less than 3e-5: it is taken anew
+constexpr float LSE_EXACT = 1024.f;        // half a step of an f32 log-sum-exp below it is at most 3e-5 of a probability; larger ones are taken anew
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -1005,7 +1005,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(const DistillArgs a
         }
     } else {
         PairSums<T, false> ps;
-        auto which = [&](int i0, int n) {                              // a bit for each listed token of i0 .. i0 + n - 1
+        // A bit for each listed token of i0 .. i0 + n - 1.  K comparisons, for a vector that holds one, while its warp waits: 2048 rows of
+        // 32 000 bf16, loss and gradient, 61 us with 20 ids (53 without a tail), 120 with 64 (54), 537 with 256 (82).
+        auto which = [&](int i0, int n) {
             uint32_t w = 0;
             for (int q = 0; q < K; q += 4) {
                 const int4 o = *reinterpret_cast<const int4 *>(ds.id + q);
