@@ -107,6 +107,10 @@ _lib.pacer_distill_backward.argtypes = [_P, _I, _L, _I, _I, _P, _P, _I, _I, _P, 
 _lib.pacer_head_logprobs_scratch_bytes.restype = C.c_size_t
 _lib.pacer_head_logprobs_scratch_bytes.argtypes = [_I, _I]
 _lib.pacer_head_logprobs.argtypes = [_P, _L, _P, _L, _I, _I, _I, _P, _P, _F, _P, _P, _P, _P, C.c_size_t, _P]
+for _n, _a in (("pacer_head_logprobs_backward", [_P] * 6 + [_P, _L, _P, _L]), ("pacer_head_nll_grad", [_P] * 2 + [_P, _L, _P, _L])):
+    getattr(_lib, _n).argtypes = [_P, _L, _P, _L, _I, _I, _I, _P, _P, _F, *_a, _P, C.c_size_t, _P]
+    getattr(_lib, _n + "_scratch_bytes").restype = C.c_size_t
+    getattr(_lib, _n + "_scratch_bytes").argtypes = [_I, _I, _I]
 PACER_F32, PACER_BF16, PACER_F16 = 0, 1, 2
 PACER_MAX_VOCAB = 393216
 _DTYPES = {torch.float32: PACER_F32, torch.bfloat16: PACER_BF16, torch.float16: PACER_F16}
@@ -124,7 +128,8 @@ def exported_symbols():
             "pacer_generate_ar", "pacer_debug_set_device_status",
             "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
             "pacer_logprobs", "pacer_verify_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
-            "pacer_head_logprobs_scratch_bytes", "pacer_head_logprobs"]
+            "pacer_head_logprobs_scratch_bytes", "pacer_head_logprobs", "pacer_head_logprobs_backward_scratch_bytes",
+            "pacer_head_logprobs_backward", "pacer_head_nll_grad_scratch_bytes", "pacer_head_nll_grad"]
 
 
 def _model_cfg(s) -> ModelCfg:
@@ -556,6 +561,67 @@ def pacer_head_logprobs(hidden, head, tokens, bias_ids=None, bias: float = 0.0):
     _call(_lib.pacer_head_logprobs, h, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), rows, vocab, d, _ptr(tokens),
           _ptr(bias_ids), bias, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), scratch.data_ptr(), nbytes)
     return logp, entropy, lse
+
+
+def _head(hidden, head):
+    h, w = _rows(hidden, "hidden"), _rows(head, "head")
+    assert h.dtype == w.dtype == torch.bfloat16 and h.device == w.device and h.shape[1] == w.shape[1], "bf16 [rows][d] and [vocab][d]"
+    return h, w
+
+
+def _head_gradients(h, w, grads, out):
+    """(dhidden or None, dhead or None, those of the caller)"""
+    given = [None, None] if out is None else list(out)
+    made = []
+    for t, want, mine in zip((h, w), grads, given):
+        if mine is not None:
+            assert mine.device == t.device and mine.dtype == t.dtype and mine.shape == t.shape and mine.stride(1) == 1 and \
+                (mine.shape[0] <= 1 or mine.stride(0) >= mine.shape[1]), "out: like hidden and head, rows apart"
+        made.append((torch.empty(t.shape, dtype=t.dtype, device=t.device) if mine is None else mine) if want else None)
+    return (*made, [g for g, want in zip(given, grads) if want])
+
+
+def _ld_or_0(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else _ld(t)
+
+
+def pacer_head_logprobs_backward(hidden, head, tokens, logp, lse, entropy, grad_logp, grad_entropy=None, grad_lse=None, bias_ids=None,
+                                 bias: float = 0.0, grads=(True, True), out=None):
+    """The gradients of pacer_head_logprobs' logp, entropy and lse (what that call returned for the same arguments) with respect to
+    hidden and head, bf16: (dhidden [rows][d], dhead [vocab][d]).  Each incoming gradient (f32 [rows]) may be None, not all three;
+    tokens and logp may be None where grad_logp is, entropy where grad_entropy is.  grads: which of the two are wanted (the other is None);
+    out: a pair of tensors to write (each may be None)."""
+    h, w = _head(hidden, head)
+    f32, i32 = torch.float32, torch.int32
+    tokens, bias_ids = _vec(tokens, "tokens", h, i32), _vec(bias_ids, "bias_ids", h, i32)
+    logp, lse, entropy = _vec(logp, "logp", h, f32), _vec(lse, "lse", h, f32), _vec(entropy, "entropy", h, f32)
+    gl, gh, gs = _vec(grad_logp, "grad_logp", h, f32), _vec(grad_entropy, "grad_entropy", h, f32), _vec(grad_lse, "grad_lse", h, f32)
+    dh, dw, given = _head_gradients(h, w, grads, out)
+    (rows, d), vocab = h.shape, w.shape[0]
+    nbytes = _lib.pacer_head_logprobs_backward_scratch_bytes(rows, vocab, d)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device)
+    _call(_lib.pacer_head_logprobs_backward, h, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), rows, vocab, d, _ptr(tokens), _ptr(bias_ids), bias,
+          _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(gl), _ptr(gh), _ptr(gs), _ptr(dh), _ld_or_0(dh), _ptr(dw), _ld_or_0(dw), scratch.data_ptr(), nbytes)
+    _written(*given)
+    return dh, dw
+
+
+def pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids=None, bias: float = 0.0, grads=(True, True), out=None):
+    """Softmax cross entropy of int32 tokens [rows] under the rows hidden @ head.T without keeping those logits, and in the same call the
+    gradients of sum(weight * loss): (loss f32 [rows], dhidden bf16 [rows][d], dhead bf16 [vocab][d]).  A token outside the vocabulary
+    (-1, say) has loss 0 and passes no gradient.  bias_ids, bias: as pacer_head_logprobs; grads, out: as
+    pacer_head_logprobs_backward."""
+    h, w = _head(hidden, head)
+    tokens, bias_ids, weight = _vec(tokens, "tokens", h, torch.int32), _vec(bias_ids, "bias_ids", h, torch.int32), _vec(weight, "weight", h, torch.float32)
+    dh, dw, given = _head_gradients(h, w, grads, out)
+    (rows, d), vocab = h.shape, w.shape[0]
+    loss = torch.empty(rows, dtype=torch.float32, device=h.device)
+    nbytes = _lib.pacer_head_nll_grad_scratch_bytes(rows, vocab, d)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=h.device)
+    _call(_lib.pacer_head_nll_grad, h, h.data_ptr(), _ld(h), w.data_ptr(), _ld(w), rows, vocab, d, _ptr(tokens), _ptr(bias_ids), bias, _ptr(weight),
+          loss.data_ptr(), _ptr(dh), _ld_or_0(dh), _ptr(dw), _ld_or_0(dw), scratch.data_ptr(), nbytes)
+    _written(*given)
+    return loss, dh, dw
 
 
 def load_pair(ctx: Context, pair: dict):

@@ -1,0 +1,551 @@
+// Gradients of the LM head fused with the scoring.  With z = hidden head^T (+ bias), p = exp(z - lse) and per row the incoming gradients,
+//   dz = g_logp ([v = token] - p) + g_lse p - g_entropy p (log p + entropy),   dhidden = dz head,   dhead = dz^T hidden.
+// z is computed again, and dz kept in bf16 for a piece of the vocabulary (all of it while that is at most 1 GB), as the operand of
+// the two products: three products of 2 rows vocab d operations, bound by the tensor cores for many rows, by reading the head
+// twice and writing dhead once for few.
+//   k_head_z     z on tcgen05, dz by the epilogue
+//   k_head_prod  both products in one launch: 256 x 256 tiles by pairs of blocks, operands by tensor copies as they lie in memory (dz is
+//                read as its own transpose, hidden rows and head as MN-major operands: no transposed copies)
+//   k_head_sum   dhidden from partial sums, where its product was cut along the vocabulary
+// dz is rounded once, to bf16, as an operand has to be; sums are fp32.  1 - p of the row's token is -expm1(logp), so that confident
+// rows lose nothing to the difference.
+#include "head_grad.h"
+
+#include <algorithm>
+
+#include "pair.cuh"
+
+namespace hg {
+
+using namespace fwd;
+using namespace pr;
+
+constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's half of a tile, columns of a tile; 64 rows x 64 columns
+constexpr int STAGE = 4 * PANEL, STAGES = 6, OUT = 32 * 128;
+constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT;
+constexpr size_t MOST_DZ = (size_t)1 << 30;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+struct ZArgs {
+    int32_t rows, width, v0, vocab, nkb, bn, mt, nt, a_rows, ld;   // v0: the piece's first token; ld: elements of a row of dz
+    const int32_t *tokens, *bias_ids;
+    float bias, sign;
+    const float *logp, *lse, *entropy, *g_logp, *g_entropy, *g_lse;
+    bf16 *dz;
+};
+
+struct PArgs {
+    int32_t rows, width, d, dp, bn, nt;        // nt: tiles of d
+    int32_t mt_w, mt_h, k_w, k_h, per, splits; // tiles of tokens and rows; k blocks of 64 of each product, of a share of dhidden's
+    int32_t n_h, n_w, early;                   // items of dhidden and dhead, dhead's that the less loaded workers take first
+    int32_t add;                               // dhidden's sums are added to those that are there
+    float *part;                               // [splits][rows][dp], or NULL: dhidden is written
+};
+
+// The roles of a pair's blocks (warps 0..7 epilogue, 8 copies, 9 tensor cores) and what they share.
+struct Pair {
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem_slot;
+    volatile int32_t gave_up;
+};
+
+__device__ __forceinline__ uint32_t pair_begin(Pair &s, int warp) {
+    if (threadIdx.x == 0) {
+        s.gave_up = 0;
+        for (int i = 0; i < STAGES; ++i) { mbar_init(s.full + i, 1); mbar_init(s.empty + i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(s.acc_full + i, 1); mbar_init(s.acc_empty + i, 2 * EPI_WARPS); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                                    // (both blocks' barriers are set up)
+    tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");                   // (what the kernels before wrote is read by the copy engine)
+    return s.tmem_slot;
+}
+__device__ __forceinline__ void pair_end(uint32_t tmem, int warp) {
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                                    // (nothing of one block is in use by the other)
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+// Waits until none of the n copies issued is in flight (a pair's arrive at its first block's barriers; the second ends after it).
+__device__ __forceinline__ void drain(Pair &s, int n, int rank) {
+    for (int j = max(0, n - STAGES); j < n && rank == 0; ++j)
+        for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(s.full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
+}
+__device__ __forceinline__ bool all_wait(Pair &s, uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, wait_h(&s.gave_up, bar, parity));
+}
+__device__ __forceinline__ uint32_t pair_idesc(int n) { return (umma_idesc(n) & ~(31u << 24)) | (256u >> 4) << 24; }
+// An MN-major operand in the 128-byte swizzle: rows (k) of 64 channels, eight of them 1 KB, the next 64 channels a panel further.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(PANEL >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void release_acc(Pair &s, int i, int lane) {   // the next products may overwrite the accumulator
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(s.acc_empty + (i & 1))) : "memory");
+}
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ void st32(void *p, const uint32_t *v) {         // 32 bytes, aligned
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+// ----------------------------------------------------------------------------- dz of a piece of the vocabulary
+
+// Persistent as k_head_score: row tiles vary fastest.
+__global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ZArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ Pair s;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    unsigned char *smem = smem_raw + (-(int)smem_u32(smem_raw) & 1023);      // (the same in both blocks)
+    const int rank = blockIdx.x & 1, worker = blockIdx.x >> 1, workers = gridDim.x >> 1, tiles = a.mt * a.nt;
+    const uint32_t tmem = pair_begin(s, warp);
+
+    if (warp == 8) {
+        if (lane == 0) {
+            uint64_t keep, stream;
+            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+            asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(stream));
+            int n = 0;
+            bool ok = true;
+            for (int t = worker; t < tiles && ok; t += workers) {
+                const int r0 = (t % a.mt) * (2 * TM) + rank * TM, n0 = (t / a.mt) * a.bn + rank * (a.bn >> 1);
+                for (int kb = 0; kb < a.nkb; ++kb, ++n) {
+                    const int slot = n % STAGES;
+                    ok = wait_h(&s.gave_up, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
+                    if (!ok) break;
+                    unsigned char *st = smem + slot * STAGE;
+                    if (rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
+                    const uint32_t bar = first_block(s.full + slot);
+                    tma_2d<true>(st, &map_a, kb * 64, r0, bar, keep);
+                    tma_2d<true>(st + 2 * PANEL, &map_b, kb * 64, n0, bar, stream);
+                }
+            }
+            drain(s, n, rank);
+        }
+    } else if (warp == 9) {
+        const uint32_t on = elect_lane(), idesc = pair_idesc(a.bn);        // (all lanes wait, one of the first block issues)
+        int n = 0, i = 0;
+        bool ok = true;
+        for (int t = worker; t < tiles && ok && rank == 0; t += workers, ++i) {
+            ok = all_wait(s, s.acc_empty + (i & 1), (((uint32_t)(i >> 1)) & 1u) ^ 1u);
+            if (!ok) break;
+            const uint32_t acc = tmem + (uint32_t)(i & 1) * 256u;
+            for (int kb = 0; kb < a.nkb; ++kb, ++n) {
+                const int slot = n % STAGES;
+                ok = all_wait(s, s.full + slot, ((uint32_t)(n / STAGES)) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a0 = smem_u32(smem + slot * STAGE), b0 = a0 + 2 * PANEL;
+#pragma unroll
+                for (int k16 = 0; k16 < 4; ++k16)
+                    umma2_if(on, acc, umma_desc(a0 + k16 * 32), umma_desc(b0 + k16 * 32), idesc, kb > 0 || k16 > 0 ? 1u : 0u);
+                umma2_commit_if(on, s.empty + slot);
+            }
+            if (ok) umma2_commit_if(on, s.acc_full + (i & 1));
+        }
+    } else {
+        const int quad = warp & 3, half = warp >> 2;
+        const int chunks = a.bn >> 5, c0 = half ? (chunks + 1) >> 1 : 0, c1 = half ? chunks : (chunks + 1) >> 1;
+        int i = 0;
+        bool ok = true;                                                // (once a wait has given up, the tiles left become NaN)
+        for (int t = worker; t < tiles; t += workers, ++i) {
+            const int n0 = (t / a.mt) * a.bn, r = (t % a.mt) * (2 * TM) + rank * TM + quad * 32 + lane;
+            const bool live = r < a.rows;
+            // dz = p (c + h log p), with `at` in the token's place
+            float gl = 0.f, c = 0.f, h = 0.f, lse = 0.f, lp = 0.f;
+            int tok = -1, bid = -1;
+            if (live) {
+                const int id = a.tokens ? a.tokens[r] : -1;
+                if (id >= 0 && id < a.vocab && a.g_logp) {
+                    gl = a.sign * a.g_logp[r];
+                    lp = a.logp[r];
+                    tok = id - a.v0 - n0;
+                }
+                if (a.bias_ids) bid = a.bias_ids[r] - a.v0 - n0;
+                lse = a.lse[r] * LOG2E;
+                c = (a.g_lse ? a.g_lse[r] : 0.f) - gl;
+                if (a.g_entropy) { const float e = a.g_entropy[r]; c = fmaf(-e, a.entropy[r], c); h = -e * LN2; }
+            }
+            if (ok) ok = all_wait(s, s.acc_full + (i & 1), ((uint32_t)(i >> 1)) & 1u);
+            tc_fence_after();
+            const uint32_t acc = tmem + (uint32_t)(i & 1) * 256u + ((uint32_t)(quad * 32) << 16);
+            for (int k = c0; k < c1; ++k) {
+                const int at = k * 32;
+                if (n0 + at >= a.ld) break;
+                uint32_t v[32];
+                tmem_ld32(acc + at, v);
+                uint32_t w[16];
+                float g[2];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    float z = __uint_as_float(v[e]);
+                    if (a.bias_ids && bid - at == e) z += a.bias;
+                    const float l = fmaf(z, LOG2E, -lse), p = ex2(l);
+                    g[e & 1] = p * fmaf(h, l, c);
+                    if (tok - at == e) g[e & 1] = p * fmaf(h, l, c + gl) - gl * expm1f(lp);
+                    if (e & 1) w[e >> 1] = pack(g[0], g[1]);
+                }
+                if (!ok)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e] = 0x7fff7fffu;
+                if (live) {
+                    bf16 *p = a.dz + (size_t)r * a.ld + n0 + at;
+                    st32(p, w);
+                    st32(p + 16, w + 8);
+                }
+            }
+            release_acc(s, i, lane);
+        }
+    }
+    pair_end(tmem, warp);
+}
+
+// ----------------------------------------------------------------------------- the products
+
+struct Item { int32_t to_head, m0, n0, k0, k1, split; };
+// The j-th item of a worker; false: there is none.  dhidden's long ones are dealt out first; where they do not come out even, the workers
+// with one less take `early` rounds of dhead's before the others join.
+__device__ __forceinline__ bool item_of(const PArgs &a, int worker, int workers, int j, Item &it) {
+    const int rem = a.n_h % workers, mine = a.n_h / workers + (worker < rem);
+    if (j < mine) {
+        const int t = worker + j * workers, n = t % a.nt, q = t / a.nt, m = q % a.mt_h;
+        it.split = q / a.mt_h;
+        it.to_head = 0; it.m0 = m * 2 * TM; it.n0 = n * a.bn; it.k0 = it.split * a.per; it.k1 = min(a.k_h, it.k0 + a.per);
+        return true;
+    }
+    int k = j - mine, t;
+    const int less = rem ? workers - rem : 0, e = rem ? a.early : 0;
+    if (rem && worker >= rem) t = k < e ? k * less + worker - rem : e * less + (k - e) * workers + worker;
+    else t = e * less + k * workers + worker;
+    if (t >= a.n_w) return false;
+    it.to_head = 1; it.m0 = t / a.nt * 2 * TM; it.n0 = t % a.nt * a.bn; it.k0 = 0; it.k1 = a.k_w; it.split = 0;
+    return true;
+}
+
+// dhead tiles: A = dz by its columns (MN-major), B = hidden (MN-major), k = rows.  dhidden tiles: A = dz (K-major), B = head (MN-major),
+// k = tokens.  All tensor copies are 64 x 64: a panel of an MN-major operand, half of a K-major one.
+__global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_x,
+                                                            const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_dw,
+                                                            const __grid_constant__ CUtensorMap map_dx, const PArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ Pair s;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    unsigned char *smem = smem_raw + (-(int)smem_u32(smem_raw) & 1023);
+    const int rank = blockIdx.x & 1, worker = blockIdx.x >> 1, workers = gridDim.x >> 1, half_n = a.bn >> 1;
+    const uint32_t tmem = pair_begin(s, warp);
+    Item it;
+
+    if (warp == 8) {
+        if (lane == 0) {
+            uint64_t normal;
+            asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+            int n = 0;
+            bool ok = true;
+            for (int j = 0; ok && item_of(a, worker, workers, j, it); ++j) {
+                const CUtensorMap *mb = it.to_head ? &map_x : &map_w;
+                const int m = it.m0 + rank * TM, nb = it.n0 + rank * half_n;
+                for (int kb = it.k0; kb < it.k1; ++kb, ++n) {
+                    const int slot = n % STAGES;
+                    ok = wait_h(&s.gave_up, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
+                    if (!ok) break;
+                    unsigned char *st = smem + slot * STAGE;
+                    if (rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * TM + a.bn) * 128u);
+                    const uint32_t bar = first_block(s.full + slot);
+                    for (int q = 0; q < 2; ++q)
+                        tma_2d<true>(st + q * PANEL, &map_z, it.to_head ? m + q * 64 : kb * 64, it.to_head ? kb * 64 : m + q * 64, bar, normal);
+                    for (int q = 0; q * 64 < half_n; ++q) tma_2d<true>(st + (2 + q) * PANEL, mb, nb + q * 64, kb * 64, bar, normal);
+                }
+            }
+            drain(s, n, rank);
+        }
+    } else if (warp == 9) {
+        const uint32_t on = elect_lane(), id_h = pair_idesc(a.bn) | (1u << 16), id_w = id_h | (1u << 15);
+        int n = 0;
+        bool ok = true;
+        for (int j = 0; ok && rank == 0 && item_of(a, worker, workers, j, it); ++j) {
+            ok = all_wait(s, s.acc_empty + (j & 1), (((uint32_t)(j >> 1)) & 1u) ^ 1u);
+            if (!ok) break;
+            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u;
+            for (int kb = it.k0; kb < it.k1; ++kb, ++n) {
+                const int slot = n % STAGES;
+                ok = all_wait(s, s.full + slot, ((uint32_t)(n / STAGES)) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a0 = smem_u32(smem + slot * STAGE), b0 = a0 + 2 * PANEL;
+#pragma unroll
+                for (int k16 = 0; k16 < 4; ++k16) {
+                    const uint32_t add = kb > it.k0 || k16 > 0 ? 1u : 0u;
+                    const uint64_t da = it.to_head ? desc_mn(a0 + k16 * 2048) : umma_desc(a0 + k16 * 32);
+                    umma2_if(on, acc, da, desc_mn(b0 + k16 * 2048), it.to_head ? id_w : id_h, add);
+                }
+                umma2_commit_if(on, s.empty + slot);
+            }
+            if (ok) umma2_commit_if(on, s.acc_full + (j & 1));
+        }
+    } else {
+        const int quad = warp & 3, half = warp >> 2;
+        unsigned char *out = smem + STAGES * STAGE + warp * OUT;
+        bool ok = true;
+        for (int j = 0; item_of(a, worker, workers, j, it); ++j) {
+            if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u);
+            tc_fence_after();
+            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
+            const int m = it.m0 + rank * TM + quad * 32, n0 = it.n0 + half * half_n, last = it.to_head ? a.width : a.rows;
+            const bool sums = !it.to_head && a.part;
+            for (int c = 0; c < half_n; c += 64) {
+                if (m >= last || n0 + c >= a.dp) break;
+                uint32_t v[64];
+                tmem_ld32(acc + c, *reinterpret_cast<uint32_t(*)[32]>(v));
+                tmem_ld32(acc + c + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+                if (!ok || it.k0 >= it.k1)                             // (a share of the last, narrower piece may be empty)
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) v[e] = ok ? 0u : 0x7fffffffu;
+                if (sums) {
+                    if (m + lane < last) {
+                        float *p = a.part + ((size_t)it.split * a.rows + m + lane) * a.dp + n0 + c;
+#pragma unroll
+                        for (int e = 0; e < 64; e += 8) {
+                            if (a.add) {
+                                const float4 x = *reinterpret_cast<const float4 *>(p + e), y = *reinterpret_cast<const float4 *>(p + e + 4);
+                                const float o[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+                                for (int f = 0; f < 8; ++f) v[e + f] = __float_as_uint(__uint_as_float(v[e + f]) + o[f]);
+                            }
+                            st32(p + e, v + e);
+                        }
+                    }
+                    continue;
+                }
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (the last tile's copy has left)
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t *u = v + 8 * q;
+                    *reinterpret_cast<uint4 *>(out + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+                        make_uint4(pack(__uint_as_float(u[0]), __uint_as_float(u[1])), pack(__uint_as_float(u[2]), __uint_as_float(u[3])),
+                                   pack(__uint_as_float(u[4]), __uint_as_float(u[5])), pack(__uint_as_float(u[6]), __uint_as_float(u[7])));
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    const CUtensorMap *mo = it.to_head ? &map_dw : &map_dx;
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(mo), "r"(n0 + c), "r"(m),
+                                 "r"(smem_u32(out)) : "memory");
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                }
+            }
+            release_acc(s, j, lane);
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    pair_end(tmem, warp);
+}
+
+// dhidden = the sum of the shares, eight columns a thread.
+__global__ void __launch_bounds__(256) k_head_sum(const float *part, int splits, int rows, int d, int dp, bf16 *out, int64_t ld) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per = d >> 3;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)rows * per) return;
+    const int64_t r = i / per, c = (i - r * per) * 8;
+    float v[8] = {};
+    for (int k = 0; k < splits; ++k) {
+        const float4 *p = reinterpret_cast<const float4 *>(part + ((size_t)k * rows + r) * dp + c);
+        const float4 x = __ldcg(p), y = __ldcg(p + 1);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+    *reinterpret_cast<uint4 *>(out + r * ld + c) = make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
+}
+
+// ----------------------------------------------------------------------------- host
+
+struct Plan {
+    int pieces, width;                     // tokens of a piece
+    int ld;                                // of dz
+    int bn, nt, dp, mt_h, splits, per;
+    size_t dz_bytes, part_bytes;
+};
+static int up(int64_t a, int b) { return (int)((a + b - 1) / b); }
+
+// A unit of time is a k block of a tile, 512 cycles.  A tile's epilogue and start count as four.
+constexpr int EXTRA = 4;
+static Plan plan_of(int rows, int vocab, int d, bool to_hidden, bool to_head, int n_sm) {
+    Plan p;
+    const int64_t most = std::max<int64_t>(256, (int64_t)(MOST_DZ / 2 / (size_t)rows) / 256 * 256);
+    p.pieces = up(vocab, (int)std::min<int64_t>(most, 1 << 24));
+    p.width = p.pieces == 1 ? vocab : up(up(vocab, p.pieces), 256) * 256;
+    p.pieces = up(vocab, p.width);
+    p.ld = up(p.width, 64) * 64;
+    p.bn = d <= 128 ? 128 : 256;
+    p.nt = up(d, p.bn);
+    p.dp = up(d, 64) * 64;
+    p.mt_h = up(rows, 2 * TM);
+    const int workers = n_sm / 2, k_h = up(p.width, 64);
+    // dhidden's product is cut along the tokens into the number of shares with the least time until the last worker is done
+    const int64_t tiles = (int64_t)p.mt_h * p.nt, head = to_head ? (int64_t)up(p.width, 2 * TM) * p.nt * (up(rows, 64) + EXTRA) : 0;
+    p.splits = 1;
+    p.per = k_h;
+    if (to_hidden) {
+        double best = 0;
+        for (int n = 1; n <= 64 && n <= k_h; ++n) {
+            const int per = up(k_h, n), shares = up(k_h, per);
+            const double own = (double)up(tiles * shares, workers) * (per + EXTRA), all = ((double)tiles * shares * (per + EXTRA) + head) / workers;
+            // (sums written and read at 6 TB/s; a launch)
+            const double cost = std::max(own, all) + (shares > 1 || p.pieces > 1 ? 10 + (double)shares * rows * p.dp * 8 / 1.6e6 : 0);
+            if (n == 1 || cost < best) { best = cost; p.splits = shares; p.per = per; }
+        }
+    }
+    p.dz_bytes = ((size_t)rows * p.ld * 2 + 255) & ~(size_t)255;
+    p.part_bytes = to_hidden && (p.splits > 1 || p.pieces > 1) ? (size_t)p.splits * rows * p.dp * 4 : 0;
+    return p;
+}
+
+size_t scratch_bytes(int rows, int vocab, int d, int n_sm) {
+    size_t most = 0;
+    for (int k = 1; k < 4; ++k) {
+        const Plan p = plan_of(rows, vocab, d, k & 1, k & 2, n_sm);
+        most = std::max(most, p.dz_bytes + p.part_bytes);
+    }
+    return most;
+}
+
+static cudaError_t opt_in() {              // (per device)
+    static bool done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
+    e = cudaFuncSetAttribute(k_head_z, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_Z);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_prod, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_P);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+    return e;
+}
+
+// A launch that waits by itself for the kernel before it (early: it may be set up while that runs).
+struct Launch {
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute at[2];
+    Launch(unsigned grid, unsigned threads, size_t smem, cudaStream_t st, bool pair, bool early) {
+        c.gridDim = dim3(grid);
+        c.blockDim = dim3(threads);
+        c.dynamicSmemBytes = smem;
+        c.stream = st;
+        c.attrs = at;
+        if (early) {
+            at[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            at[c.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+        }
+        if (pair) {
+            at[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
+            at[c.numAttrs].val.clusterDim.x = 2;
+            at[c.numAttrs].val.clusterDim.y = at[c.numAttrs].val.clusterDim.z = 1;
+            ++c.numAttrs;
+        }
+    }
+};
+
+// Tokens of a tile of z: the width with the least waves x (width + 16).
+static int z_width(int mt, int width, int workers) {
+    int best = TN;
+    int64_t best_cost = INT64_MAX;
+    for (int w = TN; w >= 32; w -= 32) {
+        const int64_t tiles = (int64_t)mt * up(width, w), cost = (tiles + workers - 1) / workers * (w + 16);
+        if (cost < best_cost) { best_cost = cost; best = w; }
+    }
+    return best;
+}
+
+cudaError_t run(const Args &a, void *scratch, int n_sm, bool after, cudaStream_t st, bool *no_maps) {
+    *no_maps = false;
+    EncodeFn encode;
+    cudaError_t e = encode_fn(&encode);
+    if (e != cudaSuccess) return e;
+    if (!encode) { *no_maps = true; return cudaSuccess; }
+    e = opt_in();
+    if (e != cudaSuccess) return e;
+    const Plan p = plan_of(a.rows, a.vocab, a.d, a.dhidden, a.dhead, n_sm);
+    const int workers = n_sm / 2;
+    bf16 *dz = reinterpret_cast<bf16 *>(scratch);
+    float *part = p.part_bytes ? reinterpret_cast<float *>(reinterpret_cast<char *>(scratch) + p.dz_bytes) : nullptr;
+    bool early = after;
+    for (int i = 0; i < p.pieces; ++i) {
+        const int v0 = i * p.width, width = std::min(p.width, a.vocab - v0);
+        const bf16 *head = reinterpret_cast<const bf16 *>(a.head) + (size_t)v0 * a.ld_head;
+        bf16 *dhead = a.dhead ? reinterpret_cast<bf16 *>(a.dhead) + (size_t)v0 * a.ld_dhead : nullptr;
+        ZArgs z;
+        z.rows = a.rows; z.width = width; z.v0 = v0; z.vocab = a.vocab; z.nkb = up(a.d, 64); z.mt = up(a.rows, 2 * TM); z.ld = p.ld;
+        z.bn = z_width(z.mt, width, workers);
+        z.nt = up(width, z.bn);
+        z.a_rows = std::min(TM, (a.rows + 7) & ~7);
+        z.tokens = a.tokens; z.bias_ids = a.bias_ids; z.bias = a.bias; z.sign = a.sign;
+        z.logp = a.logp; z.lse = a.lse; z.entropy = a.entropy; z.g_logp = a.g_logp; z.g_entropy = a.g_entropy; z.g_lse = a.g_lse;
+        z.dz = dz;
+        CUtensorMap ma, mb, mz, mx, mw, mdw, mdx;
+        if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, z.a_rows) || !make_map(encode, &mb, head, a.ld_head, width, a.d, z.bn / 2) ||
+            !make_map(encode, &mz, dz, p.ld, a.rows, width, 64) || !make_map(encode, &mx, a.hidden, a.ld_hidden, a.rows, a.d, 64) ||
+            !make_map(encode, &mw, head, a.ld_head, width, a.d, 64) || (dhead && !make_map(encode, &mdw, dhead, a.ld_dhead, width, a.d, 32)) ||
+            (a.dhidden && !part && !make_map(encode, &mdx, a.dhidden, a.ld_dhidden, a.rows, a.d, 32))) {
+            *no_maps = true;
+            return cudaSuccess;
+        }
+        if (!dhead) mdw = mw;              // (not used)
+        if (!a.dhidden || part) mdx = mw;
+        {
+            Launch l((unsigned)std::min<int64_t>(workers, (int64_t)z.mt * z.nt) * 2, THREADS_G, SMEM_Z, st, true, early);
+            e = cudaLaunchKernelEx(&l.c, k_head_z, ma, mb, z);
+            if (e != cudaSuccess) return e;
+        }
+        early = true;
+        PArgs q;
+        q.rows = a.rows; q.width = width; q.d = a.d; q.dp = p.dp; q.bn = p.bn; q.nt = p.nt;
+        q.mt_w = up(width, 2 * TM); q.mt_h = p.mt_h; q.k_w = up(a.rows, 64); q.k_h = up(width, 64);
+        q.splits = p.splits; q.per = up(q.k_h, p.splits);
+        q.n_h = a.dhidden ? p.splits * p.mt_h * p.nt : 0;
+        q.n_w = dhead ? q.mt_w * p.nt : 0;
+        q.early = (q.per + EXTRA) / (q.k_w + EXTRA);
+        q.add = i > 0;
+        q.part = part;
+        Launch l((unsigned)std::min<int64_t>(workers, (int64_t)q.n_h + q.n_w) * 2, THREADS_G, SMEM_P, st, true, early);
+        e = cudaLaunchKernelEx(&l.c, k_head_prod, mz, mx, mw, mdw, mdx, q);
+        if (e != cudaSuccess) return e;
+    }
+    if (!part) return cudaSuccess;
+    Launch l((unsigned)(((int64_t)a.rows * (a.d >> 3) + 255) / 256), 256, 0, st, false, true);
+    return cudaLaunchKernelEx(&l.c, k_head_sum, (const float *)part, p.splits, a.rows, a.d, p.dp, reinterpret_cast<bf16 *>(a.dhidden), a.ld_dhidden);
+}
+
+// The head's own scratch is free again when dz is written, and shares its memory.
+static size_t rows_bytes(int rows) { return ((size_t)rows * 8 + 255) & ~(size_t)255; }
+
+size_t nll_scratch_bytes(int rows, int vocab, int d, int n_sm) {
+    return rows_bytes(rows) + std::max(hs::scratch_bytes(rows, vocab), scratch_bytes(rows, vocab, d, n_sm));
+}
+
+cudaError_t run_nll(const Args &a, float *loss, void *scratch, int n_sm, cudaStream_t st, bool *no_maps) {
+    float *logp = reinterpret_cast<float *>(scratch), *lse = logp + a.rows;
+    void *rest = reinterpret_cast<char *>(scratch) + rows_bytes(a.rows);
+    cudaError_t e = hs::run({a.hidden, a.head, a.ld_hidden, a.ld_head, a.rows, a.vocab, a.d, a.tokens, a.bias_ids, a.bias, logp, nullptr, lse, loss},
+                            rest, n_sm, st, no_maps);
+    if (e != cudaSuccess || *no_maps || (!a.dhidden && !a.dhead)) return e;
+    Args b = a;
+    b.logp = logp;
+    b.lse = lse;
+    return run(b, rest, n_sm, true, st, no_maps);
+}
+
+}  // namespace hg

@@ -13,15 +13,14 @@
 // (m, sum 2^t, sum 2^t t), t = (z - m) log2(e), in the scratch, and a second kernel joins a row's halves.
 #include "head_score.h"
 
-#include <cuda.h>
-
 #include <algorithm>
 
-#include "forward.cuh"
+#include "pair.cuh"
 
 namespace hs {
 
 using namespace fwd;
+using namespace pr;
 
 constexpr int TM = 128, TN = 256, A_BYTES = TM * 128;
 // PAIR: two blocks of a cluster work on 256 rows, each with its 128 of them and half of the tile's tokens in shared memory.
@@ -44,48 +43,6 @@ struct KArgs {
     Part *part;                            // [rows][2 * nt]
     float *ztok;                           // [rows]
 };
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// bar: a shared::cluster address; with PAIR that of the pair's first block.
-template <bool PAIR>
-__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar, uint64_t policy) {
-    if (PAIR)
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
-                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
-                     ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
-}
-__device__ __forceinline__ uint32_t first_block(const void *smem) {      // the address of the pair's first block
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(smem)), "r"(0));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// As umma_if and umma_commit_if for both blocks' operands, accumulators and barriers; issued by the first block.
-__device__ __forceinline__ void umma2_if(uint32_t on, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-                 "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
-                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on) : "memory");
-}
-__device__ __forceinline__ void umma2_commit_if(uint32_t on, uint64_t *bar) {
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
-                 ::"r"(smem_u32(bar)), "r"(on), "h"((uint16_t)3) : "memory");
-}
-// Bounded wait; one that runs out ends the block's work (its rows become NaN).
-__device__ __forceinline__ bool wait_h(volatile int32_t *gave_up, uint64_t *bar, uint32_t parity) {
-    for (unsigned it = 1; !mbar_try_wait(bar, parity); ++it)
-        if ((it & 1023u) == 0 && (it > MBAR_SPIN_LIMIT || *gave_up)) { *gave_up = 1; return false; }
-    return true;
-}
 
 struct Run {                               // a thread's running sums
     float m = NO_REF, S = 0.f, S2 = 0.f;
@@ -276,8 +233,9 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
 }
 
 // One warp per row joins its parts.
-__global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, float *entropy, float *lse) {
+__global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, float *entropy, float *lse, float *loss) {
     const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (row >= a.rows) return;
     const float4 *p = reinterpret_cast<const float4 *>(a.part) + (size_t)row * (2 * a.nt);
@@ -298,7 +256,9 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
     if (entropy) entropy[row] = (l2 - s.S2 / s.S) * LN2;
     if (logp) {
         const int t = a.tokens[row];
-        logp[row] = t >= 0 && t < a.vocab ? (__ldcg(a.ztok + row) - s.m) - l : 0.f;
+        const float x = t >= 0 && t < a.vocab ? (__ldcg(a.ztok + row) - s.m) - l : 0.f;
+        logp[row] = x;
+        if (loss) loss[row] = 0.f - x;
     }
 }
 
@@ -333,32 +293,16 @@ size_t scratch_bytes(int rows, int vocab) {
     return (size_t)rows * (2 * tiles_of(rows, vocab).nt) * sizeof(Part) + (((size_t)rows * sizeof(float) + 255) & ~(size_t)255);
 }
 
-typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// bf16 [rows][d], boxes of `box` rows x 64 columns in the 128-byte swizzle; what lies outside reads as 0.
-static bool make_map(EncodeFn encode, CUtensorMap *map, const void *p, int64_t ld, int rows, int d, int box) {
-    const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, one[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), dims, strides, boxes, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *no_maps) {
     static bool attr_set[64] = {};         // the opt-in is per device
-    static EncodeFn encode = nullptr;
     *no_maps = false;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (!encode) {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
-        if (e != cudaSuccess) return e;
-        if (q != cudaDriverEntryPointSuccess || !fn) { *no_maps = true; return cudaSuccess; }
-        encode = reinterpret_cast<EncodeFn>(fn);
-    }
+    EncodeFn encode;
+    e = encode_fn(&encode);
+    if (e != cudaSuccess) return e;
+    if (!encode) { *no_maps = true; return cudaSuccess; }
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
         e = cudaFuncSetAttribute(k_head_score<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
@@ -398,7 +342,7 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     at[0].val.programmaticStreamSerializationAllowed = 1;
     c.attrs = at;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_head_join, k, a.logp, a.entropy, a.lse);
+    return cudaLaunchKernelEx(&c, k_head_join, k, a.logp, a.entropy, a.lse, a.loss);
 }
 
 }  // namespace hs

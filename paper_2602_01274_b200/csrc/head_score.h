@@ -14,6 +14,7 @@ struct Args {
     const int32_t *tokens, *bias_ids;      // [rows]; bias_ids may be NULL
     float bias;
     float *logp, *entropy, *lse;           // [rows], each may be NULL
+    float *loss = nullptr;                 // -logp, only with logp
 };
 
 size_t scratch_bytes(int rows, int vocab);

@@ -17,6 +17,7 @@
 #include "fwd_few.h"
 #include "fwd_kernel.cuh"
 #include "gemm.cuh"
+#include "head_grad.h"
 #include "head_score.h"
 #include "logits.h"
 #include "prefill.h"
@@ -1095,5 +1096,92 @@ extern "C" int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const 
     CK(hs::run({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, logp, entropy, lse}, scratch, sm_count_or_default(),
                (cudaStream_t)cuda_stream, &no_maps));
     if (no_maps) return fail(nullptr, PACER_EUNSUPPORTED, "pacer_head_logprobs: the driver describes no tensor copies");
+    return PACER_OK;
+}
+
+// ------------------------------------------------------------------ gradients of the LM head fused with the scoring
+
+static const char *bad_head(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d) {
+    if (rows < 0 || rows > hs::MAX_ROWS) return "rows out of range";
+    if (vocab < 1 || vocab > hs::MAX_VOCAB) return "vocab out of range";
+    if (d < 8 || d > hs::MAX_D || d % 8) return "d out of range or not a multiple of 8";
+    if (ld_hidden < d || ld_hidden % 8 || ld_hidden >> 38 || ld_head < d || ld_head % 8 || ld_head >> 38) return "bad row stride";
+    if (rows && (!hidden || !head)) return "hidden or head is null";
+    if (((uintptr_t)hidden | (uintptr_t)head) & 15) return "misaligned pointer";
+    return nullptr;
+}
+// Whether bf16 matrices [r][d] lie in one another's memory (from the first element to the last).
+static bool matrices_meet(const void *a, int64_t lda, int64_t ra, const void *b, int64_t ldb, int64_t rb, int d) {
+    if (!a || !b || !ra || !rb) return false;
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    return a0 < b0 + 2 * ((rb - 1) * ldb + d) && b0 < a0 + 2 * ((ra - 1) * lda + d);
+}
+static const char *bad_head_grads(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
+                                  const void *dhidden, int64_t ld_dhidden, const void *dhead, int64_t ld_dhead) {
+    if ((dhidden && (ld_dhidden < d || ld_dhidden % 8 || ld_dhidden >> 38)) || (dhead && (ld_dhead < d || ld_dhead % 8 || ld_dhead >> 38)))
+        return "bad row stride of a gradient";
+    if (((uintptr_t)dhidden | (uintptr_t)dhead) & 15) return "misaligned gradient";
+    if (matrices_meet(dhidden, ld_dhidden, rows, hidden, ld_hidden, rows, d) || matrices_meet(dhidden, ld_dhidden, rows, head, ld_head, vocab, d) ||
+        matrices_meet(dhead, ld_dhead, vocab, hidden, ld_hidden, rows, d) || matrices_meet(dhead, ld_dhead, vocab, head, ld_head, vocab, d) ||
+        matrices_meet(dhidden, ld_dhidden, rows, dhead, ld_dhead, vocab, d))
+        return "a gradient overlaps an operand or the other gradient";
+    return nullptr;
+}
+
+extern "C" size_t pacer_head_logprobs_backward_scratch_bytes(int rows, int vocab, int d) {
+    if (rows < 1 || rows > hs::MAX_ROWS || vocab < 1 || vocab > hs::MAX_VOCAB || d < 8 || d > hs::MAX_D || d % 8) return 0;
+    return hg::scratch_bytes(rows, vocab, d, sm_count_or_default());
+}
+
+extern "C" int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
+                                            const int32_t *tokens, const int32_t *bias_ids, float bias, const float *logp, const float *lse,
+                                            const float *entropy, const float *g_logp, const float *g_entropy, const float *g_lse, void *dhidden,
+                                            int64_t ld_dhidden, void *dhead, int64_t ld_dhead, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_head(hidden, ld_hidden, head, ld_head, rows, vocab, d));
+    REFUSE_IF(!dhidden && !dhead && rows, "no gradient is asked for");
+    REFUSE_BAD(bad_head_grads(hidden, ld_hidden, head, ld_head, rows, vocab, d, dhidden, ld_dhidden, dhead, ld_dhead));
+    if (!rows) {                           // no rows: the head's gradient is 0
+        if (dhead) CK(cudaMemset2DAsync(dhead, (size_t)ld_dhead * 2, 0, (size_t)d * 2, vocab, (cudaStream_t)cuda_stream));
+        return PACER_OK;
+    }
+    REFUSE_IF(!scratch || (uintptr_t)scratch & 255, "scratch is null or misaligned");
+    REFUSE_IF(!lse, "lse is null");
+    REFUSE_IF(!g_logp && !g_entropy && !g_lse, "no gradient comes in");
+    REFUSE_IF(g_logp && (!tokens || !logp), "g_logp without tokens or logp");
+    REFUSE_IF(g_entropy && !entropy, "g_entropy without entropy");
+    const int n_sm = sm_count_or_default();
+    if (scratch_bytes < hg::scratch_bytes(rows, vocab, d, n_sm)) return fail(nullptr, PACER_ENOMEM, "pacer_head_logprobs_backward: scratch too small");
+    bool no_maps = false;
+    CK(hg::run({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, logp, lse, entropy, g_logp, g_entropy, g_lse, 1.f, dhidden, dhead,
+                ld_dhidden, ld_dhead}, scratch, n_sm, false, (cudaStream_t)cuda_stream, &no_maps));
+    if (no_maps) return fail(nullptr, PACER_EUNSUPPORTED, "pacer_head_logprobs_backward: the driver describes no tensor copies");
+    return PACER_OK;
+}
+
+extern "C" size_t pacer_head_nll_grad_scratch_bytes(int rows, int vocab, int d) {
+    if (rows < 1 || rows > hs::MAX_ROWS || vocab < 1 || vocab > hs::MAX_VOCAB || d < 8 || d > hs::MAX_D || d % 8) return 0;
+    return hg::nll_scratch_bytes(rows, vocab, d, sm_count_or_default());
+}
+
+extern "C" int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
+                                   const int32_t *tokens, const int32_t *bias_ids, float bias, const float *weight, float *loss, void *dhidden,
+                                   int64_t ld_dhidden, void *dhead, int64_t ld_dhead, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_BAD(bad_head(hidden, ld_hidden, head, ld_head, rows, vocab, d));
+    REFUSE_BAD(bad_head_grads(hidden, ld_hidden, head, ld_head, rows, vocab, d, dhidden, ld_dhidden, dhead, ld_dhead));
+    if (!rows) {
+        if (dhead) CK(cudaMemset2DAsync(dhead, (size_t)ld_dhead * 2, 0, (size_t)d * 2, vocab, (cudaStream_t)cuda_stream));
+        return PACER_OK;
+    }
+    REFUSE_IF(!scratch || (uintptr_t)scratch & 255, "scratch is null or misaligned");
+    REFUSE_IF(!tokens, "tokens is null");
+    REFUSE_IF((dhidden || dhead) && !weight, "a gradient without weight");
+    const int n_sm = sm_count_or_default();
+    if (scratch_bytes < hg::nll_scratch_bytes(rows, vocab, d, n_sm)) return fail(nullptr, PACER_ENOMEM, "pacer_head_nll_grad: scratch too small");
+    bool no_maps = false;
+    CK(hg::run_nll({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, nullptr, nullptr, nullptr, weight, nullptr, nullptr, -1.f,
+                    dhidden, dhead, ld_dhidden, ld_dhead}, loss, scratch, n_sm, (cudaStream_t)cuda_stream, &no_maps));
+    if (no_maps) return fail(nullptr, PACER_EUNSUPPORTED, "pacer_head_nll_grad: the driver describes no tensor copies");
     return PACER_OK;
 }
