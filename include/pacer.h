@@ -399,6 +399,56 @@ int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head,
                         const int32_t *tokens, const int32_t *bias_ids, float bias, const float *weight, float *loss, void *dhidden,
                         int64_t ld_dhidden, void *dhead, int64_t ld_dhead, void *scratch, size_t scratch_bytes, void *cuda_stream);
 
+/* An AdamW step over many tensors at once (in one launch up to 480 of them):
+ *   m <- beta_one m + (1 - beta_one) g,   v <- beta_two v + (1 - beta_two) g^2,
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta_one^step) m / (sqrt(v) / sqrt(1 - beta_two^step) + eps)
+ * in f32.  tbl: host array of n tensors, read before the call returns; all other pointers are device addresses, element-aligned (16 bytes
+ * let whole pieces be moved), arrays contiguous and apart; a tensor of no elements is passed over, a param listed twice refused. */
+typedef struct {
+    void *param;             /* param_type: PACER_F32 or PACER_BF16 */
+    void *copy;              /* bf16 [numel] or NULL: the new parameter rounded (with an f32 param: the master of 16-bit weights) */
+    const void *grad;        /* grad_type: PACER_F32, PACER_BF16 or PACER_F16 */
+    void *exp_avg, *exp_avg_sq;   /* m, v: f32, or 8-bit codes */
+    float *scales;           /* with 8-bit states: [ceil(numel / 256)][2], else not read */
+    int64_t numel;
+    int32_t param_type, grad_type;
+} pacer_adamw_tensor;
+
+/* state_bits 8: m and v are held in blocks of 256 elements, m as sign, 4 exponent and 3 mantissa bits (0, 2^-9 .. 480) times scales[b][0], v as
+ * 5 exponent and 3 mantissa bits (0, 2^-18 .. 61440) times scales[b][1]; the block's largest gets the largest code.  The step itself
+ * uses the new moments before they are rounded.  A v above 0 does not become 0 (a block whose largest moment is at most 1e-30 is held as
+ * 0).  Codes and scales of 0 are the start.  A NaN or infinite moment spoils its block.
+ * seeded: 8-bit states and bf16 parameters are rounded up or down at random, with 16 bits of a hash of (seed, step, the tensor's place
+ * in tbl, element), so that the mean is the value; else to nearest.  copies are rounded to nearest.
+ * norm (device f32, may be NULL): the gradients' global norm (pacer_grad_norm).  With max_norm > 0 gradients are multiplied by
+ * min(1, max_norm / (norm + 1e-6)); where it is not finite nothing is changed.
+ * step_device (device int32) and lr_device (device f32), each may be NULL, stand for step and lr where the call is captured into a graph. */
+typedef struct {
+    double lr, beta_one, beta_two, eps, weight_decay, max_norm;
+    int64_t step;            /* 1 for the first */
+    uint64_t seed;
+    const float *norm, *lr_device;
+    const int32_t *step_device;
+    int32_t state_bits;      /* 32 or 8 */
+    int32_t seeded;
+} pacer_adamw_cfg;
+
+int pacer_adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg *cfg, void *cuda_stream);
+
+/* 8-bit states as f32: exp_avg[i] and exp_avg_sq[i] (host arrays of device addresses, f32 [numel], entries and arrays may be NULL) get what the
+ * codes of tbl[i] stand for. */
+int pacer_adamw_states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, void *cuda_stream);
+
+/* norm (device f32) = sqrt of the sum of all squares of n gradients (host array tbl, read before the call returns), summed in 64 bits in a
+ * fixed order.  scratch: device, 8-byte aligned, at least pacer_grad_norm_scratch_bytes(n) bytes. */
+typedef struct {
+    const void *grad;
+    int64_t numel;
+    int32_t type;            /* PACER_F32, PACER_BF16 or PACER_F16 */
+} pacer_gradient;
+size_t pacer_grad_norm_scratch_bytes(int n);
+int pacer_grad_norm(const pacer_gradient *tbl, int n, float *norm, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

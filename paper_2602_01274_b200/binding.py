@@ -49,6 +49,12 @@ class Tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("dev_ptr", C.c_void_p), ("numel", C.c_int64)]
 
 
+class AdamwCfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta_one", C.c_double), ("beta_two", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("max_norm", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64), ("norm", C.c_void_p), ("lr_device", C.c_void_p),
+                ("step_device", C.c_void_p), ("state_bits", C.c_int32), ("seeded", C.c_int32)]
+
+
 class Stats(C.Structure):
     _fields_ = [("n_draft_fwd", C.c_int64), ("n_mb_calls", C.c_int64), ("n_target_fwd", C.c_int64),
                 ("n_steps", C.c_int64), ("n_generated", C.c_int64), ("n_kernel_launches", C.c_int64),
@@ -111,6 +117,11 @@ for _n, _a in (("pacer_head_logprobs_backward", [_P] * 6 + [_P, _L, _P, _L]), ("
     getattr(_lib, _n).argtypes = [_P, _L, _P, _L, _I, _I, _I, _P, _P, _F, *_a, _P, C.c_size_t, _P]
     getattr(_lib, _n + "_scratch_bytes").restype = C.c_size_t
     getattr(_lib, _n + "_scratch_bytes").argtypes = [_I, _I, _I]
+_lib.pacer_adamw.argtypes = [_P, _I, C.POINTER(AdamwCfg), _P]
+_lib.pacer_adamw_states.argtypes = [_P, _I, _P, _P, _P]
+_lib.pacer_grad_norm.argtypes = [_P, _I, _P, _P, C.c_size_t, _P]
+_lib.pacer_grad_norm_scratch_bytes.restype = C.c_size_t
+_lib.pacer_grad_norm_scratch_bytes.argtypes = [_I]
 PACER_F32, PACER_BF16, PACER_F16 = 0, 1, 2
 PACER_MAX_VOCAB = 393216
 _DTYPES = {torch.float32: PACER_F32, torch.bfloat16: PACER_BF16, torch.float16: PACER_F16}
@@ -129,7 +140,8 @@ def exported_symbols():
             "pacer_profile_begin", "pacer_profile_end", "pacer_linear_scratch_bytes", "pacer_linear", "pacer_linear_static",
             "pacer_logprobs", "pacer_verify_logprobs", "pacer_logprobs_backward", "pacer_distill", "pacer_distill_backward",
             "pacer_head_logprobs_scratch_bytes", "pacer_head_logprobs", "pacer_head_logprobs_backward_scratch_bytes",
-            "pacer_head_logprobs_backward", "pacer_head_nll_grad_scratch_bytes", "pacer_head_nll_grad"]
+            "pacer_head_logprobs_backward", "pacer_head_nll_grad_scratch_bytes", "pacer_head_nll_grad",
+            "pacer_adamw", "pacer_adamw_states", "pacer_grad_norm_scratch_bytes", "pacer_grad_norm"]
 
 
 def _model_cfg(s) -> ModelCfg:
@@ -622,6 +634,127 @@ def pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids=None, bias: float
           loss.data_ptr(), _ptr(dh), _ld_or_0(dh), _ptr(dw), _ld_or_0(dw), scratch.data_ptr(), nbytes)
     _written(*given)
     return loss, dh, dw
+
+
+# ----------------------------------------------------------------------------- AdamW over many tensors
+
+
+class AdamwTensors:
+    """The tensors of an optimiser as the library takes them, checked once and kept: params f32 or bf16, exp_avg and exp_avg_sq of the same
+    sizes (f32; with `scales` uint8 codes, scales f32 [ceil(numel / 256)][2]), copies (bf16, with f32 params) or None; all contiguous, on
+    one GPU.  Holds references to them."""
+
+    def __init__(self, params, exp_avg, exp_avg_sq, scales=None, copies=None):
+        self.tensors = tuple(None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales))
+        params, copies, exp_avg, exp_avg_sq, scales = self.tensors
+        self.state_bits, n = 32 if scales is None else 8, len(params)
+        for x in self.tensors:
+            if x is not None and len(x) != n:
+                raise AssertionError("AdamwTensors: lists of one length")
+        state = torch.float32 if scales is None else torch.uint8
+        self.device = params[0].device if n else None
+        for i, p in enumerate(params):
+            if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16)):
+                raise AssertionError(f"param {i}: f32 or bf16 on the GPU")
+            for t, dtype, name in ((exp_avg[i], state, "exp_avg"), (exp_avg_sq[i], state, "exp_avg_sq"), (copies and copies[i], torch.bfloat16, "copy")):
+                if t is not None and t is not False and (t.dtype != dtype or t.numel() != p.numel()):
+                    raise AssertionError(f"{name} {i}: {dtype} of the param's size")
+            if scales is not None and (scales[i].dtype != torch.float32 or scales[i].shape != (-(-p.numel() // 256), 2)):
+                raise AssertionError(f"scales {i}: torch.float32 [{-(-p.numel() // 256)}][2]")
+            for x in self.tensors:
+                if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == self.device):
+                    raise AssertionError(f"tensors of param {i}: contiguous, on {self.device}")
+        # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type)
+        self.numel = [p.numel() for p in params]
+        self._types = np.array([_DTYPES[p.dtype] for p in params], dtype=np.int64)
+        self.table = np.zeros((n, 8), dtype=np.int64)
+        self.table[:, 6], self.table[:, 7] = self.numel, self._types
+        self._place()
+
+    def _place(self):
+        """The addresses, as they are now (a program may exchange a parameter's storage)."""
+        for col, x in zip((0, 1, 3, 4, 5), self.tensors):
+            if x is not None:
+                self.table[:, col] = [0 if t is None else t.data_ptr() for t in x]
+
+    def with_grads(self, grads):
+        if len(grads) != len(self.numel):
+            raise AssertionError("grads: one for each param")
+        types, at = [], []
+        for g, n in zip(grads, self.numel):
+            if g.numel() != n or g.dtype not in _DTYPES or not g.is_contiguous() or g.device != self.device:
+                raise AssertionError(f"grads: f32, bf16 or f16 of the params' sizes, contiguous, on {self.device}")
+            types.append(_DTYPES[g.dtype])
+            at.append(g.data_ptr())
+        self._place()
+        self.table[:, 2] = at
+        self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32)
+        return self.table
+
+
+def pacer_grad_norm(grads) -> torch.Tensor:
+    """The global 2-norm of a list of gradients (f32, bf16 or f16, contiguous, on one GPU) as an f32 scalar on the device, summed in 64
+    bits.  Nothing is read back."""
+    grads = list(grads)
+    if not grads:
+        raise AssertionError("grads: at least one")
+    dev = grads[0].device
+    rows = []
+    for g in grads:
+        if not g.is_cuda or g.device != dev or g.dtype not in _DTYPES or not g.is_contiguous():
+            raise AssertionError("grads: f32, bf16 or f16, contiguous, on one GPU")
+        rows.append((g.data_ptr(), g.numel(), _DTYPES[g.dtype]))
+    table = np.array(rows, dtype=np.int64)
+    nbytes = _lib.pacer_grad_norm_scratch_bytes(len(rows))
+    buf = torch.empty(nbytes // 4 + 2, dtype=torch.float32, device=dev)          # the result, then the scratch
+    _call(_lib.pacer_grad_norm, buf, table.ctypes.data, len(rows), buf.data_ptr(), buf.data_ptr() + 8, nbytes)
+    return buf[0]
+
+
+def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, seed=None, norm=None,
+                max_norm: float = 0.0):
+    """An AdamW step over all of `tensors`, in place, in one launch for up to 480 of them.  step (1 for the first) and lr: numbers, or
+    int32 and f32 scalars on the device (for a call that is captured into a graph).  seed: 8-bit states and bf16 params are rounded
+    at random with a hash of it, the step and the element (None: to nearest).  norm: the gradients' global norm (pacer_grad_norm);
+    they are scaled to at most max_norm (0: not at all), and where it is not finite nothing is changed."""
+    table = tensors.with_grads(grads)
+    if not len(table):
+        return
+    cfg = AdamwCfg(beta_one=betas[0], beta_two=betas[1], eps=eps, weight_decay=weight_decay, max_norm=max_norm, state_bits=tensors.state_bits,
+                   seeded=seed is not None, seed=0 if seed is None else seed & ((1 << 64) - 1))
+    for name, x, dtype in (("step", step, torch.int32), ("lr", lr, torch.float32)):
+        if torch.is_tensor(x):
+            assert x.dtype == dtype and x.numel() == 1 and x.device == tensors.device, f"{name}: one {dtype} on {tensors.device}"
+            setattr(cfg, name + "_device", x.data_ptr())
+        else:
+            setattr(cfg, name, x)
+    if norm is not None:
+        assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == tensors.device, f"norm: one torch.float32 on {tensors.device}"
+        cfg.norm = norm.data_ptr()
+    _call(_lib.pacer_adamw, tensors, table.ctypes.data, len(table), C.byref(cfg))
+    for x in tensors.tensors:
+        if x is not None:
+            _written(*x)
+
+
+def pacer_adamw_states(tensors: AdamwTensors, out=None):
+    """What the 8-bit states stand for: (exp_avg, exp_avg_sq), lists of f32 tensors of the params' sizes, or written to `out` (two lists;
+    contiguous, of those sizes)."""
+    assert tensors.state_bits == 8, "8-bit states"
+    if out is None:
+        out = tuple([torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in tensors.tensors[0]] for _ in range(2))
+    for x in out:
+        if len(x) != len(tensors.numel):
+            raise AssertionError("out: one for each param")
+        for t, n in zip(x, tensors.numel):
+            if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.device != tensors.device:
+                raise AssertionError(f"out: f32 of the params' sizes, contiguous, on {tensors.device}")
+    if len(tensors.numel):
+        tensors._place()
+        m, v = (np.array([t.data_ptr() for t in x], dtype=np.int64) for x in out)
+        _call(_lib.pacer_adamw_states, tensors, tensors.table.ctypes.data, len(m), m.ctypes.data, v.ctypes.data)
+        _written(*out[0], *out[1])
+    return out
 
 
 def load_pair(ctx: Context, pair: dict):

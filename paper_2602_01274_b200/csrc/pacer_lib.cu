@@ -17,6 +17,7 @@
 #include "fwd_few.h"
 #include "fwd_kernel.cuh"
 #include "gemm.cuh"
+#include "adamw.h"
 #include "head_grad.h"
 #include "head_score.h"
 #include "logits.h"
@@ -1183,5 +1184,87 @@ extern "C" int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const 
     CK(hg::run_nll({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, nullptr, nullptr, nullptr, weight, nullptr, nullptr, -1.f,
                     dhidden, dhead, ld_dhidden, ld_dhead}, loss, scratch, n_sm, (cudaStream_t)cuda_stream, &no_maps));
     if (no_maps) return fail(nullptr, PACER_EUNSUPPORTED, "pacer_head_nll_grad: the driver describes no tensor copies");
+    return PACER_OK;
+}
+
+// ------------------------------------------------------------------ AdamW over many tensors
+
+static int type_bytes(int type) { return type == PACER_F32 ? 4 : type == PACER_BF16 || type == PACER_F16 ? 2 : 0; }
+static bool off(const void *p, int bytes) { return (uintptr_t)p % bytes != 0; }
+
+static const char *bad_states(const pacer_adamw_tensor &t) {
+    if (t.numel < 0 || t.numel >> 40) return "numel out of range";
+    if (!t.numel) return nullptr;
+    if (!t.exp_avg || !t.exp_avg_sq || !t.scales) return "a state is null";
+    if (off(t.scales, 8)) return "misaligned scales";
+    return nullptr;
+}
+static const char *bad_adamw(const pacer_adamw_tensor *tbl, int n, int bits) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> at;
+    at.reserve(n);
+    for (int i = 0; i < n; ++i) {
+        const pacer_adamw_tensor &t = tbl[i];
+        if (t.numel < 0 || t.numel >> 40) return "numel out of range";
+        if (!t.numel) continue;
+        if (t.param_type != PACER_F32 && t.param_type != PACER_BF16) return "unknown type of param";
+        if (!type_bytes(t.grad_type)) return "unknown type of grad";
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return "param, grad or a state is null";
+        if (t.copy && t.param_type != PACER_F32) return "a copy of a 16-bit param";
+        if (off(t.param, type_bytes(t.param_type)) || off(t.grad, type_bytes(t.grad_type)) || off(t.copy, 2)) return "misaligned param, copy or grad";
+        if (bits == 32 && (off(t.exp_avg, 4) || off(t.exp_avg_sq, 4))) return "misaligned states";
+        if (bits == 8)
+            if (const char *bad = bad_states(t)) return bad;
+        at.emplace_back((uintptr_t)t.param, (uintptr_t)t.param + t.numel * type_bytes(t.param_type));
+    }
+    std::sort(at.begin(), at.end());
+    for (size_t i = 1; i < at.size(); ++i)
+        if (at[i].first < at[i - 1].second) return "two params overlap";
+    return nullptr;
+}
+
+extern "C" int pacer_adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg *cfg, void *cuda_stream) try {
+    pacer_ctx *c = nullptr;
+    REFUSE_IF(!cfg, "cfg is null");
+    REFUSE_IF(n < 0 || n > 1 << 20, "n out of range");
+    REFUSE_IF(n && !tbl, "tbl is null");
+    REFUSE_IF(cfg->state_bits != 32 && cfg->state_bits != 8, "state_bits is neither 32 nor 8");
+    REFUSE_IF(!(cfg->beta_one >= 0 && cfg->beta_one < 1 && cfg->beta_two >= 0 && cfg->beta_two < 1), "a beta outside [0, 1)");
+    REFUSE_IF(!(cfg->eps >= 0) || std::isinf(cfg->eps) || !std::isfinite(cfg->weight_decay) || !(cfg->lr_device || std::isfinite(cfg->lr)), "eps, weight_decay or lr");
+    REFUSE_IF(!cfg->step_device && (cfg->step < 1 || cfg->step > 0x7fffffff), "step out of range");
+    REFUSE_IF(std::isnan(cfg->max_norm) || (cfg->max_norm > 0 && !cfg->norm), "max_norm without norm");
+    REFUSE_BAD(bad_adamw(tbl, n, cfg->state_bits));
+    CK(ow::adamw(tbl, n, *cfg, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+} catch (const std::bad_alloc &) {
+    return PACER_ENOMEM;
+}
+
+extern "C" int pacer_adamw_states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_IF(n < 0 || n > 1 << 20, "n out of range");
+    REFUSE_IF(n && !tbl, "tbl is null");
+    for (int i = 0; i < n; ++i) {
+        REFUSE_BAD(bad_states(tbl[i]));
+        REFUSE_IF((exp_avg && off(exp_avg[i], 4)) || (exp_avg_sq && off(exp_avg_sq[i], 4)), "misaligned output");
+    }
+    CK(ow::states(tbl, n, exp_avg, exp_avg_sq, (cudaStream_t)cuda_stream));
+    return PACER_OK;
+}
+
+extern "C" size_t pacer_grad_norm_scratch_bytes(int n) { return n < 0 || n > 1 << 20 ? 0 : ow::norm_scratch_bytes(std::max(n, 1)); }
+
+extern "C" int pacer_grad_norm(const pacer_gradient *tbl, int n, float *norm, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    pacer_ctx *c = nullptr;
+    REFUSE_IF(n < 0 || n > 1 << 20, "n out of range");
+    REFUSE_IF(n && !tbl, "tbl is null");
+    REFUSE_IF(!norm || off(norm, 4), "norm is null or misaligned");
+    REFUSE_IF(!scratch || off(scratch, 8), "scratch is null or misaligned");
+    for (int i = 0; i < n; ++i) {
+        REFUSE_IF(tbl[i].numel < 0 || tbl[i].numel >> 40, "numel out of range");
+        REFUSE_IF(!type_bytes(tbl[i].type), "unknown type of grad");
+        REFUSE_IF(tbl[i].numel && (!tbl[i].grad || off(tbl[i].grad, type_bytes(tbl[i].type))), "grad is null or misaligned");
+    }
+    if (scratch_bytes < ow::norm_scratch_bytes(std::max(n, 1))) return fail(nullptr, PACER_ENOMEM, "pacer_grad_norm: scratch too small");
+    CK(ow::grad_norm(tbl, n, norm, (double *)scratch, (cudaStream_t)cuda_stream));
     return PACER_OK;
 }
