@@ -451,9 +451,9 @@ def _out_like(z: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
 def _written(*outputs: Optional[torch.Tensor]):
     """Tensors of the caller that a call has written: autograd has to know, as of torch's own in-place functions, so that a backward
     pass which saved them (or what they are views of) says so instead of computing with what is there now."""
-    for t in outputs:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+    changed = [t for t in outputs if t is not None]
+    if changed:
+        torch.autograd.graph.increment_version(changed)
 
 
 # torch.cuda.current_stream(..).cuda_stream, where torch has it without the object that costs 2 us a call
@@ -664,32 +664,45 @@ class AdamwTensors:
             for x in self.tensors:
                 if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == self.device):
                     raise AssertionError(f"tensors of param {i}: contiguous, on {self.device}")
+        self.all = [t for x in self.tensors if x is not None for t in x]
         # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type)
         self.numel = [p.numel() for p in params]
         self._types = np.array([_DTYPES[p.dtype] for p in params], dtype=np.int64)
         self.table = np.zeros((n, 8), dtype=np.int64)
         self.table[:, 6], self.table[:, 7] = self.numel, self._types
+        self._at = self._grads_at = None
+        self._gaps = any(t is None for t in self.all)
         self._place()
 
     def _place(self):
         """The addresses, as they are now (a program may exchange a parameter's storage)."""
-        for col, x in zip((0, 1, 3, 4, 5), self.tensors):
-            if x is not None:
-                self.table[:, col] = [0 if t is None else t.data_ptr() for t in x]
+        at = [0 if t is None else t.data_ptr() for t in self.all] if self._gaps else list(map(torch.Tensor.data_ptr, self.all))
+        if at != self._at:
+            self._at, n = at, len(self.numel)
+            for i, col in enumerate(c for c, x in zip((0, 1, 3, 4, 5), self.tensors) if x is not None):
+                self.table[:, col] = at[i * n:(i + 1) * n]
 
     def with_grads(self, grads):
-        if len(grads) != len(self.numel):
+        if not self.numel:
             raise AssertionError("grads: one for each param")
-        types, at = [], []
-        for g, n in zip(grads, self.numel):
-            if g.numel() != n or g.dtype not in _DTYPES or not g.is_contiguous() or g.device != self.device:
-                raise AssertionError(f"grads: f32, bf16 or f16 of the params' sizes, contiguous, on {self.device}")
-            types.append(_DTYPES[g.dtype])
-            at.append(g.data_ptr())
+        types, at = _gradients(grads, self.device)
+        if list(map(torch.Tensor.numel, grads)) != self.numel:
+            raise AssertionError("grads: one of each param's size")
         self._place()
-        self.table[:, 2] = at
+        if at != self._grads_at:
+            self._grads_at = at
+            self.table[:, 2] = at
         self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32)
         return self.table
+
+
+def _gradients(grads, device):
+    """Types (one for all, where they are alike) and addresses of gradients."""
+    dtypes = {g.dtype for g in grads}
+    if not dtypes <= _DTYPES.keys() or not all(map(torch.Tensor.is_contiguous, grads)) or set(map(torch.Tensor.get_device, grads)) - {device.index} or \
+            device.type != "cuda":
+        raise AssertionError(f"grads: f32, bf16 or f16, contiguous, on one GPU ({device})")
+    return _DTYPES[dtypes.pop()] if len(dtypes) == 1 else [_DTYPES[g.dtype] for g in grads], list(map(torch.Tensor.data_ptr, grads))
 
 
 def pacer_grad_norm(grads) -> torch.Tensor:
@@ -698,16 +711,13 @@ def pacer_grad_norm(grads) -> torch.Tensor:
     grads = list(grads)
     if not grads:
         raise AssertionError("grads: at least one")
-    dev = grads[0].device
-    rows = []
-    for g in grads:
-        if not g.is_cuda or g.device != dev or g.dtype not in _DTYPES or not g.is_contiguous():
-            raise AssertionError("grads: f32, bf16 or f16, contiguous, on one GPU")
-        rows.append((g.data_ptr(), g.numel(), _DTYPES[g.dtype]))
-    table = np.array(rows, dtype=np.int64)
-    nbytes = _lib.pacer_grad_norm_scratch_bytes(len(rows))
+    dev, n = grads[0].device, len(grads)
+    table = np.empty((n, 3), dtype=np.int64)                                     # pacer_gradient
+    table[:, 2], table[:, 0] = _gradients(grads, dev)
+    table[:, 1] = list(map(torch.Tensor.numel, grads))
+    nbytes = _lib.pacer_grad_norm_scratch_bytes(n)
     buf = torch.empty(nbytes // 4 + 2, dtype=torch.float32, device=dev)          # the result, then the scratch
-    _call(_lib.pacer_grad_norm, buf, table.ctypes.data, len(rows), buf.data_ptr(), buf.data_ptr() + 8, nbytes)
+    _call(_lib.pacer_grad_norm, buf, table.ctypes.data, n, buf.data_ptr(), buf.data_ptr() + 8, nbytes)
     return buf[0]
 
 
@@ -717,9 +727,9 @@ def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps:
     int32 and f32 scalars on the device (for a call that is captured into a graph).  seed: 8-bit states and bf16 params are rounded
     at random with a hash of it, the step and the element (None: to nearest).  norm: the gradients' global norm (pacer_grad_norm);
     they are scaled to at most max_norm (0: not at all), and where it is not finite nothing is changed."""
-    table = tensors.with_grads(grads)
-    if not len(table):
+    if not tensors.numel and not len(grads):
         return
+    table = tensors.with_grads(grads)
     cfg = AdamwCfg(beta_one=betas[0], beta_two=betas[1], eps=eps, weight_decay=weight_decay, max_norm=max_norm, state_bits=tensors.state_bits,
                    seeded=seed is not None, seed=0 if seed is None else seed & ((1 << 64) - 1))
     for name, x, dtype in (("step", step, torch.int32), ("lr", lr, torch.float32)):
@@ -732,9 +742,7 @@ def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps:
         assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == tensors.device, f"norm: one torch.float32 on {tensors.device}"
         cfg.norm = norm.data_ptr()
     _call(_lib.pacer_adamw, tensors, table.ctypes.data, len(table), C.byref(cfg))
-    for x in tensors.tensors:
-        if x is not None:
-            _written(*x)
+    _written(*tensors.all)
 
 
 def pacer_adamw_states(tensors: AdamwTensors, out=None):

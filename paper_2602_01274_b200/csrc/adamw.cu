@@ -25,7 +25,7 @@ namespace ow {
 
 typedef __nv_bfloat16 bf16;
 
-constexpr int THREADS_W = 256, PASS = 8 * THREADS_W, CHUNK = 2 * PASS;
+constexpr int THREADS_W = 256, PASS = 8 * THREADS_W, CHUNK = 4 * PASS;
 constexpr float TOP_M = 480.f, TOP_V = 61440.f, LEAST = 1e-30f;
 constexpr float DOWN_M = 0x1p-120f, UP_M = 0x1p120f, DOWN_V = 0x1p-111f, UP_V = 0x1p111f;
 
@@ -36,14 +36,13 @@ struct Item {
     void *m, *v;
     float *scales;
     int64_t numel;
-    uint32_t first;                        // chunk
-    uint16_t ptype, gtype;
+    uint32_t first, number;                // chunk; place in the call
 };
 static_assert(sizeof(Item) == 64, "the table's rows");
 
 struct Hyper {
     float b1, c1, b2, c2, eps, decay, a, s2;
-    float max_norm;
+    float max_norm, one;                   // one: 1 (see update)
     uint32_t seed, step;
     const float *norm, *lr_dev;
     const int32_t *step_dev;
@@ -53,7 +52,7 @@ struct Hyper {
 
 template <int CAP> struct Table {
     Hyper h;
-    int32_t n, number;                     // tensors; the first one's number in the call
+    int32_t n, pad;
     Item t[CAP];
 };
 
@@ -66,28 +65,44 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {     // an integer
 // Eight values of a lane: side by side (VEC), or 32 apart, those below n.
 template <bool VEC> __device__ __forceinline__ int64_t place(int64_t base, int lane, int k) { return base + (VEC ? lane * 8 + k : lane + 32 * k); }
 
-template <bool VEC> __device__ __forceinline__ void load(const void *p, int type, int64_t base, int lane, int64_t n, float (&x)[8]) {
-    if (type == PACER_F32) {
-        const float *q = reinterpret_cast<const float *>(p);
-        if (VEC) {
-            const float4 u = *reinterpret_cast<const float4 *>(q + base + lane * 8), w = *reinterpret_cast<const float4 *>(q + base + lane * 8 + 4);
-            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
-        } else
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); x[k] = i < n ? q[i] : 0.f; }
+__device__ __forceinline__ uint4 ld16(const void *p) {              // (read once: kept out of L1)
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+template <int TYPE> __device__ __forceinline__ float widen(uint32_t h) {
+    return TYPE == PACER_BF16 ? __uint_as_float(h << 16) : __half2float(__ushort_as_half((unsigned short)h));
+}
+// Eight values as they lie in memory.
+template <int TYPE> struct Raw { uint4 v[TYPE == PACER_F32 ? 2 : 1]; };
+template <bool VEC, int TYPE> __device__ __forceinline__ void fetch(const void *p, int64_t base, int lane, int64_t n, Raw<TYPE> &r) {
+    if (VEC) {
+        const char *q = reinterpret_cast<const char *>(p) + (base + lane * 8) * (TYPE == PACER_F32 ? 4 : 2);
+        r.v[0] = ld16(q);
+        if (TYPE == PACER_F32) r.v[TYPE == PACER_F32] = ld16(q + 16);
     } else {
-        uint32_t h[8];
-        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
-        if (VEC) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(q + base + lane * 8);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint32_t w[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu;
-        } else
+        for (int k = 0; k < 8; ++k) {
+            const int64_t i = place<false>(base, lane, k);
+            w[k] = i >= n ? 0u : TYPE == PACER_F32 ? reinterpret_cast<const uint32_t *>(p)[i] : reinterpret_cast<const uint16_t *>(p)[i];
+        }
+        if (TYPE == PACER_F32) {
+            r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            r.v[TYPE == PACER_F32] = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+            r.v[0] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        }
+    }
+}
+template <int TYPE> __device__ __forceinline__ void widen8(const Raw<TYPE> &r, float (&x)[8]) {
+    const uint4 u = r.v[0], z = r.v[TYPE == PACER_F32];
+    const uint32_t w[8] = {u.x, u.y, u.z, u.w, z.x, z.y, z.z, z.w};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); h[k] = i < n ? q[i] : 0u; }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = type == PACER_BF16 ? __uint_as_float(h[k] << 16) : __half2float(__ushort_as_half((unsigned short)h[k]));
+    for (int k = 0; k < 8; ++k) {
+        if (TYPE == PACER_F32) x[k] = __uint_as_float(w[k]);
+        else if (TYPE == PACER_BF16) x[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+        else x[k] = widen<TYPE>(k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu);
     }
 }
 template <bool VEC> __device__ __forceinline__ void store(float *q, int64_t base, int lane, int64_t n, const float (&x)[8]) {
@@ -98,32 +113,88 @@ template <bool VEC> __device__ __forceinline__ void store(float *q, int64_t base
 #pragma unroll
         for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); if (i < n) q[i] = x[k]; }
 }
-// h: eight 16-bit patterns
+// The upper halves of eight words
 template <bool VEC> __device__ __forceinline__ void store16(bf16 *p, int64_t base, int lane, int64_t n, const uint32_t (&h)[8]) {
     uint16_t *q = reinterpret_cast<uint16_t *>(p);
-    if (VEC) *reinterpret_cast<uint4 *>(q + base + lane * 8) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    if (VEC) *reinterpret_cast<uint4 *>(q + base + lane * 8) = make_uint4(__byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x7632),
+                                                                          __byte_perm(h[4], h[5], 0x7632), __byte_perm(h[6], h[7], 0x7632));
     else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); if (i < n) q[i] = (uint16_t)h[k]; }
+        for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); if (i < n) q[i] = (uint16_t)(h[k] >> 16); }
 }
-template <bool VEC> __device__ __forceinline__ void load_codes(const uint8_t *q, int64_t base, int lane, int64_t n, uint32_t (&c)[8]) {
-    if (VEC) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(q + base + lane * 8);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) c[k] = ((k < 4 ? u.x : u.y) >> (8 * (k & 3))) & 0xffu;
-    } else
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); c[k] = i < n ? q[i] : 0u; }
-}
-template <bool VEC> __device__ __forceinline__ void store_codes(uint8_t *q, int64_t base, int lane, int64_t n, const uint32_t (&c)[8]) {
-    if (VEC) *reinterpret_cast<uint2 *>(q + base + lane * 8) = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+// Eight codes, four to a word
+template <bool VEC> __device__ __forceinline__ uint2 load_codes(const uint8_t *q, int64_t base, int lane, int64_t n) {
+    uint2 u = make_uint2(0u, 0u);
+    if (VEC) asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(u.x), "=r"(u.y) : "l"(q + base + lane * 8));
     else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); if (i < n) q[i] = (uint8_t)c[k]; }
+        for (int k = 0; k < 8; ++k) {
+            const int64_t i = place<false>(base, lane, k);
+            const uint32_t c = i < n ? q[i] : 0u;
+            if (k < 4) u.x |= c << (8 * k);
+            else u.y |= c << (8 * k - 32);
+        }
+    return u;
+}
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+__device__ __forceinline__ uint32_t top_bytes(const float *x) {
+    return top_bytes(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+template <bool VEC> __device__ __forceinline__ void store_codes(uint8_t *q, int64_t base, int lane, int64_t n, uint2 u) {
+    if (VEC) *reinterpret_cast<uint2 *>(q + base + lane * 8) = u;
+    else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { const int64_t i = place<false>(base, lane, k); if (i < n) q[i] = (uint8_t)((k < 4 ? u.x : u.y) >> (8 * (k & 3))); }
+}
+// The largest size of eight; NaN where there is one.
+__device__ __forceinline__ float largest(const float (&x)[8]) {
+    float a, b;
+    asm("{\n\t.reg .f32 a, b, c;\n\tabs.f32 a, %1;\n\tabs.f32 b, %2;\n\tabs.f32 c, %3;\n\tmax.NaN.f32 %0, a, b, c;\n\t}" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
+    asm("{\n\t.reg .f32 a, b, c;\n\tabs.f32 a, %1;\n\tabs.f32 b, %2;\n\tabs.f32 c, %3;\n\tmax.NaN.f32 %0, a, b, c;\n\t}" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
+    asm("{\n\t.reg .f32 a, b;\n\tabs.f32 a, %2;\n\tabs.f32 b, %3;\n\tmax.NaN.f32 %0, %1, a, b;\n\t}" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(b));
+    return a;
 }
 
-__device__ __forceinline__ float value_m(uint32_t c, float scale) { return __fmul_rn(__uint_as_float((c & 0x7fu) << 20 | (c & 0x80u) << 24) * UP_M, scale); }
-__device__ __forceinline__ float value_v(uint32_t c, float scale) { return __fmul_rn(__uint_as_float(c << 20) * UP_V, scale); }
+// Two f32 operations in one instruction, each rounded by itself.
+struct Two { uint64_t b; };
+__device__ __forceinline__ Two two(float x, float y) {
+    Two t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t.b) : "f"(x), "f"(y));
+    return t;
+}
+__device__ __forceinline__ void apart(Two t, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(t.b)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two t;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t.b) : "l"(a.b), "l"(b.b));
+    return t;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two t;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(t.b) : "l"(a.b), "l"(b.b), "l"(c.b));
+    return t;
+}
+__device__ __forceinline__ void scale2(float (&x)[8], float f) {
+    const Two t = two(f, f);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) apart(mul2(two(x[k], x[k + 1]), t), x[k], x[k + 1]);
+}
+
+// What eight codes stand for.  The move of the exponents and the scale are one factor, unless that would overflow.
+template <bool SIGNED> __device__ __forceinline__ void values(uint2 c, float scale, float (&x)[8]) {
+    constexpr float UP = SIGNED ? UP_M : UP_V, MOST = SIGNED ? 128.f : 65536.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t w = k < 4 ? c.x : c.y;
+        if (SIGNED) x[k] = __uint_as_float((uint32_t)((int32_t)(w << (24 - 8 * (k & 3))) >> 4) & 0x87f00000u);
+        else x[k] = __uint_as_float(__byte_perm(w, 0u, (uint32_t)(k & 3) << 8 | 0x4044u) << 4);
+    }
+    if (scale < MOST) scale *= UP;
+    else scale2(x, UP);
+    scale2(x, scale);
+}
 
 // The scale of a block from its largest bits (NaN above all, so that a block with one is NaN from then on).
 __device__ __forceinline__ void scale_of(uint32_t bits, float top, float one_by_top, float &scale, float &inverse) {
@@ -133,56 +204,92 @@ __device__ __forceinline__ void scale_of(uint32_t bits, float top, float one_by_
     inverse = none ? 0.f : __fdiv_rn(top, peak);
 }
 
-// Eight elements of one lane, all of a warp 256: a block of 8-bit states.  seed: the tensor's.
-template <int BITS, bool VEC>
-__device__ __forceinline__ void update(const Item &t, const Hyper &h, float a, float s2, float decay, float clip, bool clipped, uint32_t key, int64_t base, int lane) {
+struct Step { float a, s2, decay, clip; bool clipped; };
+
+// What a lane reads of its eight elements, of a warp's 256: a block of 8-bit states.
+template <int BITS, int PT, int GT> struct In {
+    Raw<GT> g;
+    Raw<PT> p;
+    Raw<PACER_F32> m, v;                   // (32-bit states)
+    uint2 cm, cv;
+    float2 scale;
+};
+template <int BITS, int PT, int GT, bool VEC> __device__ __forceinline__ void fetch_all(const Item &t, int64_t base, int lane, In<BITS, PT, GT> &in) {
+    fetch<VEC, GT>(t.grad, base, lane, t.numel, in.g);
+    fetch<VEC, PT>(t.param, base, lane, t.numel, in.p);
+    if (BITS == 32) {
+        fetch<VEC, PACER_F32>(t.m, base, lane, t.numel, in.m);
+        fetch<VEC, PACER_F32>(t.v, base, lane, t.numel, in.v);
+    } else {
+        in.cm = load_codes<VEC>(reinterpret_cast<const uint8_t *>(t.m), base, lane, t.numel);
+        in.cv = load_codes<VEC>(reinterpret_cast<const uint8_t *>(t.v), base, lane, t.numel);
+        in.scale = *reinterpret_cast<const float2 *>(t.scales + (base >> 8) * 2);
+    }
+}
+
+// key: the tensor's.
+template <int BITS, int PT, int GT, bool SEEDED, bool VEC>
+__device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step &q, uint32_t key, int64_t base, int lane, const In<BITS, PT, GT> &in) {
     const int64_t n = t.numel;
     float p[8], g[8], m[8], v[8];
-    uint32_t cm[8], cv[8];
-    load<VEC>(t.grad, t.gtype, base, lane, n, g);
-    load<VEC>(t.param, t.ptype, base, lane, n, p);
+    widen8<GT>(in.g, g);
+    widen8<PT>(in.p, p);
     if (BITS == 32) {
-        load<VEC>(t.m, PACER_F32, base, lane, n, m);
-        load<VEC>(t.v, PACER_F32, base, lane, n, v);
+        widen8<PACER_F32>(in.m, m);
+        widen8<PACER_F32>(in.v, v);
     } else {
-        load_codes<VEC>(reinterpret_cast<const uint8_t *>(t.m), base, lane, n, cm);
-        load_codes<VEC>(reinterpret_cast<const uint8_t *>(t.v), base, lane, n, cv);
-        const float2 s = *reinterpret_cast<const float2 *>(t.scales + (base >> 8) * 2);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { m[k] = value_m(cm[k], s.x); v[k] = value_v(cv[k], s.y); }
+        values<true>(in.cm, in.scale.x, m);
+        values<false>(in.cv, in.scale.y, v);
     }
+    if (q.clipped) scale2(g, q.clip);
+    const Two b1 = two(h.b1, h.b1), c1 = two(h.c1, h.c1), b2 = two(h.b2, h.b2), c2 = two(h.c2, h.c2);
+    // (as a sum of two products of pairs the assembler would make one product and a multiply-add of it: times 1 they stay what they are)
+    const Two one = two(h.one, h.one);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (clipped) g[k] = __fmul_rn(g[k], clip);
-        m[k] = __fadd_rn(__fmul_rn(m[k], h.b1), __fmul_rn(g[k], h.c1));
-        v[k] = __fadd_rn(__fmul_rn(v[k], h.b2), __fmul_rn(__fmul_rn(g[k], g[k]), h.c2));
-        float root, share;
-        asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[k]));
+    for (int k = 0; k < 8; k += 2) {
+        const Two x = two(g[k], g[k + 1]);
+        apart(fma2(mul2(two(m[k], m[k + 1]), b1), one, mul2(x, c1)), m[k], m[k + 1]);
+        apart(fma2(mul2(two(v[k], v[k + 1]), b2), one, mul2(mul2(x, x), c2)), v[k], v[k + 1]);
+        float r0, r1;
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v[k]));
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v[k + 1]));
+        apart(fma2(two(r0, r1), two(q.s2, q.s2), two(h.eps, h.eps)), r0, r1);
         // (the update is a small part of the parameter: 2^-22 of it is far below the parameter's own rounding)
-        asm("div.approx.f32 %0, %1, %2;" : "=f"(share) : "f"(m[k]), "f"(fmaf(root, s2, h.eps)));
-        p[k] = fmaf(-a, share, __fmul_rn(p[k], decay));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(r0));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(r1));
+        const Two share = mul2(two(m[k], m[k + 1]), two(r0, r1));
+        apart(fma2(share, two(-q.a, -q.a), mul2(two(p[k], p[k + 1]), two(q.decay, q.decay))), p[k], p[k + 1]);
     }
     uint32_t r[8];
-    if (h.seeded && (BITS == 8 || t.ptype == PACER_BF16))
+    constexpr bool seeded = SEEDED && (BITS == 8 || PT == PACER_BF16);
+    if (seeded) {
+        // (base is a multiple of 256: the number's lowest bits are the lane's)
+        const uint32_t x = (uint32_t)base ^ key ^ ((base >> 32) ? mix((uint32_t)(base >> 32)) : 0u) ^ (uint32_t)(VEC ? lane * 8 : lane);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t i = place<VEC>(base, lane, k);
-            r[k] = mix((uint32_t)i ^ key ^ (i >> 32 ? mix((uint32_t)(i >> 32)) : 0u));
-        }
-    if (t.ptype == PACER_F32) {
+        for (int k = 0; k < 8; ++k) r[k] = mix(x ^ (uint32_t)(VEC ? k : 32 * k));
+    }
+    if (PT == PACER_F32) {
         store<VEC>(reinterpret_cast<float *>(t.param), base, lane, n, p);
         if (t.copy) {
             uint32_t o[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = __bfloat16_as_ushort(__float2bfloat16_rn(p[k]));
+            for (int k = 0; k < 8; ++k) o[k] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(p[k])) << 16;
             store16<VEC>(t.copy, base, lane, n, o);
         }
     } else {
         uint32_t o[8];
+        float odd = 0.f;                   // NaN where one of the eight is not finite: their bits are not to be added to
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t b = __float_as_uint(p[k]);
-            o[k] = h.seeded && (~b & 0x7f800000u) ? (b + ((r[k] * 0x9E3779B1u) >> 16)) >> 16 : __bfloat16_as_ushort(__float2bfloat16_rn(p[k]));
+        for (int k = 0; k < 8; ++k) odd = fmaf(p[k], 0.f, odd);
+        if (seeded && odd == 0.f) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(p[k]) + ((r[k] * 0x9E3779B1u) >> 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t b = __float_as_uint(p[k]);
+                o[k] = seeded && (~b & 0x7f800000u) ? b + ((r[k] * 0x9E3779B1u) >> 16) : (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(p[k])) << 16;
+            }
         }
         store16<VEC>(reinterpret_cast<bf16 *>(t.param), base, lane, n, o);
     }
@@ -191,29 +298,50 @@ __device__ __forceinline__ void update(const Item &t, const Hyper &h, float a, f
         store<VEC>(reinterpret_cast<float *>(t.v), base, lane, n, v);
         return;
     }
-    uint32_t top_m = 0, top_v = 0;
+    if (!VEC)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const bool in = VEC || place<VEC>(base, lane, k) < n;
-        top_m = max(top_m, in ? __float_as_uint(m[k]) & 0x7fffffffu : 0u);
-        top_v = max(top_v, in ? __float_as_uint(v[k]) & 0x7fffffffu : 0u);
-    }
-    top_m = __reduce_max_sync(0xffffffffu, top_m);
-    top_v = __reduce_max_sync(0xffffffffu, top_v);
-    float sm, im, sv, iv;
+        for (int k = 0; k < 8; ++k)
+            if (place<VEC>(base, lane, k) >= n) m[k] = v[k] = 0.f;
+    const uint32_t top_m = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(m))), top_v = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(v)));
+    float sm, im, sv, iv, um[8], uv[8];
     scale_of(top_m, TOP_M, 1.f / TOP_M, sm, im);
     scale_of(top_v, TOP_V, 1.f / TOP_V, sv, iv);
 #pragma unroll
+    for (int k = 0; k < 8; ++k) { um[k] = m[k]; uv[k] = v[k]; }
+    scale2(um, im); scale2(um, DOWN_M);
+    scale2(uv, iv); scale2(uv, DOWN_V);
+    // A code above the last (the largest, where its quotient was rounded up; NaN) or of 0 with v above 0 is rare, and looked for in a block as a whole.
+    uint32_t low = __float_as_uint(uv[0]);
+#pragma unroll
+    for (int k = 1; k < 8; ++k) low = min(low, __float_as_uint(uv[k]));
+    const bool plain = VEC && __reduce_min_sync(0xffffffffu, low) >= 1u << 20 &&
+                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_m), im), DOWN_M)) <= 127u << 20 &&
+                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_v), iv), DOWN_V)) <= 255u << 20;
+    uint32_t cm[8], cv[8];                 // the codes in the topmost bytes (m's sign has left)
+#pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint32_t dm = h.seeded ? (r[k] & 0xffffu) << 4 : 1u << 19, dv = h.seeded ? (r[k] >> 16) << 4 : 1u << 19;
-        const uint32_t bm = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(m[k]), im), DOWN_M)), bv = __float_as_uint(__fmul_rn(__fmul_rn(v[k], iv), DOWN_V));
-        cm[k] = min((bm + dm) >> 20, 127u) | (m[k] < 0.f ? 128u : 0u);
-        cv[k] = min((bv + dv) >> 20, 255u);
-        if (v[k] > 0.f) cv[k] = max(cv[k], 1u);
+        const uint32_t dm = seeded ? __byte_perm(r[k], 0u, 0x4104) : 1u << 23, dv = seeded ? __byte_perm(r[k], 0u, 0x4324) : 1u << 23;
+        cm[k] = __float_as_uint(um[k]) * 16u + dm;
+        cv[k] = __float_as_uint(uv[k]) * 16u + dv;
     }
-    store_codes<VEC>(reinterpret_cast<uint8_t *>(t.m), base, lane, n, cm);
-    store_codes<VEC>(reinterpret_cast<uint8_t *>(t.v), base, lane, n, cv);
+    if (!plain)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t dm = seeded ? (r[k] << 4) & 0xffff0u : 1u << 19, dv = seeded ? (r[k] >> 12) & 0xffff0u : 1u << 19;
+            cm[k] = min(((__float_as_uint(um[k]) & 0x7fffffffu) + dm) >> 20, 127u) << 24;
+            cv[k] = max(min((__float_as_uint(uv[k]) + dv) >> 20, 255u), min(__float_as_uint(v[k]), 1u)) << 24;
+        }
+    store_codes<VEC>(reinterpret_cast<uint8_t *>(t.m), base, lane, n,
+                     make_uint2(top_bytes(cm[0], cm[1], cm[2], cm[3]) | (top_bytes(m) & 0x80808080u), top_bytes(cm[4], cm[5], cm[6], cm[7]) | (top_bytes(m + 4) & 0x80808080u)));
+    store_codes<VEC>(reinterpret_cast<uint8_t *>(t.v), base, lane, n, make_uint2(top_bytes(cv[0], cv[1], cv[2], cv[3]), top_bytes(cv[4], cv[5], cv[6], cv[7])));
     if (lane == 0) *reinterpret_cast<float2 *>(t.scales + (base >> 8) * 2) = make_float2(sm, sv);
+}
+// (a tensor's last elements, and all of one that lies off the 16-byte grid)
+template <int BITS, int PT, int GT, bool SEEDED>
+__device__ __noinline__ void update_slow(const Item &t, const Hyper &h, const Step &q, uint32_t key, int64_t base, int lane) {
+    In<BITS, PT, GT> in;
+    fetch_all<BITS, PT, GT, false>(t, base, lane, in);
+    update<BITS, PT, GT, SEEDED, false>(t, h, q, key, base, lane, in);
 }
 
 template <class T> __device__ __forceinline__ int tensor_of(const T &tab, uint32_t chunk) {
@@ -227,54 +355,76 @@ template <class T> __device__ __forceinline__ int tensor_of(const T &tab, uint32
 }
 __device__ __forceinline__ bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
-template <int BITS, int CAP>
-__global__ void __launch_bounds__(THREADS_W) k_adamw(const __grid_constant__ Table<CAP> tab) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+template <int BITS, int PT, int GT, bool SEEDED, int CAP>
+__global__ void __launch_bounds__(THREADS_W, BITS == 8 ? 3 : 4) k_adamw(const __grid_constant__ Table<CAP> tab) {
     const Hyper &h = tab.h;
-    float clip = 1.f;
-    bool clipped = false;
+    Step q{h.a, h.s2, h.decay, 1.f, false};
     if (h.norm) {
         const float norm = __ldcg(h.norm);
         if (!isfinite(norm)) return;       // nothing is changed
-        clipped = h.max_norm > 0.f;
-        if (clipped) clip = fminf(__fdiv_rn(h.max_norm, __fadd_rn(norm, 1e-6f)), 1.f);
+        q.clipped = h.max_norm > 0.f;
+        if (q.clipped) q.clip = fminf(__fdiv_rn(h.max_norm, __fadd_rn(norm, 1e-6f)), 1.f);
     }
-    float a = h.a, s2 = h.s2, decay = h.decay;
     uint32_t step = h.step;
     if (h.step_dev || h.lr_dev) {
         if (h.step_dev) step = (uint32_t)*h.step_dev;
         const double lr = h.lr_dev ? (double)*h.lr_dev : h.lr;
-        a = (float)(lr / (1.0 - pow(h.b1d, (double)step)));
-        s2 = (float)(1.0 / sqrt(1.0 - pow(h.b2d, (double)step)));
-        decay = (float)(1.0 - lr * h.wd);
+        q.a = (float)(lr / (1.0 - pow(h.b1d, (double)step)));
+        q.s2 = (float)(1.0 / sqrt(1.0 - pow(h.b2d, (double)step)));
+        q.decay = (float)(1.0 - lr * h.wd);
     }
-    const int i = tensor_of(tab, blockIdx.x), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Item t = tab.t[i];
-    const uint32_t key = mix(h.seed ^ mix(step ^ mix((uint32_t)(tab.number + i))));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Item &t = tab.t[tensor_of(tab, blockIdx.x)];
+    const uint32_t key = mix(h.seed ^ mix(step ^ mix(t.number)));
     const bool vec = aligned(t.param, 16) && aligned(t.copy, 16) && aligned(t.grad, 16) && aligned(t.m, BITS == 32 ? 16 : 8) && aligned(t.v, BITS == 32 ? 16 : 8);
-    const int64_t start = (int64_t)(blockIdx.x - t.first) * CHUNK + warp * 256;
+    const int64_t start = (int64_t)(blockIdx.x - t.first) * CHUNK + warp * 256, end = min(start - warp * 256 + CHUNK, t.numel);
+    int64_t base = start;
+    if (vec && BITS == 32) {
 #pragma unroll 1
-    for (int64_t base = start; base < start + CHUNK && base < t.numel; base += PASS) {
-        if (vec && base + 256 <= t.numel) update<BITS, true>(t, h, a, s2, decay, clip, clipped, key, base, lane);
-        else update<BITS, false>(t, h, a, s2, decay, clip, clipped, key, base, lane);
+        for (; base + 256 <= end; base += PASS) {
+            In<BITS, PT, GT> in;
+            fetch_all<BITS, PT, GT, true>(t, base, lane, in);
+            update<BITS, PT, GT, SEEDED, true>(t, h, q, key, base, lane, in);
+        }
+    } else if (vec && base + 256 <= end) { // (the next elements are on their way while these are worked on: codes take ten times the instructions)
+        In<BITS, PT, GT> in, next;
+        fetch_all<BITS, PT, GT, true>(t, base, lane, in);
+#pragma unroll 1
+        while (true) {
+            const bool more = base + PASS + 256 <= end;
+            if (more) fetch_all<BITS, PT, GT, true>(t, base + PASS, lane, next);
+            update<BITS, PT, GT, SEEDED, true>(t, h, q, key, base, lane, in);
+            base += PASS;
+            if (!more) break;
+            in = next;
+        }
     }
+#pragma unroll 1
+    for (; base < end; base += PASS) update_slow<BITS, PT, GT, SEEDED>(t, h, q, key, base, lane);
 }
 
-template <int BITS, int CAP> static cudaError_t launch(const pacer_adamw_tensor *tbl, int from, int to, const Hyper &h, cudaStream_t st) {
+// The tensors at[0 .. n).
+template <int BITS, int PT, int GT, bool SEEDED, int CAP> static cudaError_t launch(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
     Table<CAP> tab;
     tab.h = h;
-    tab.number = from;
-    tab.n = 0;
+    tab.n = n;
     uint64_t chunks = 0;
-    for (int i = from; i < to; ++i) {
-        const pacer_adamw_tensor &t = tbl[i];
-        tab.t[tab.n++] = {t.param, (bf16 *)t.copy, t.grad, t.exp_avg, t.exp_avg_sq, t.scales, t.numel, (uint32_t)chunks, (uint16_t)t.param_type, (uint16_t)t.grad_type};
+    for (int i = 0; i < n; ++i) {
+        const pacer_adamw_tensor &t = tbl[at[i]];
+        tab.t[i] = {t.param, (bf16 *)t.copy, t.grad, t.exp_avg, t.exp_avg_sq, t.scales, t.numel, (uint32_t)chunks, (uint32_t)at[i]};
         chunks += (uint64_t)(t.numel + CHUNK - 1) / CHUNK;
     }
-    if (!chunks) return cudaSuccess;
     if (chunks > 0x7fffffffu) return cudaErrorInvalidValue;
-    k_adamw<BITS, CAP><<<(unsigned)chunks, THREADS_W, 0, st>>>(tab);
+    k_adamw<BITS, PT, GT, SEEDED, CAP><<<(unsigned)chunks, THREADS_W, 0, st>>>(tab);
     return cudaGetLastError();
+}
+constexpr int MOST = 480;                  // tensors a launch: 32 KB of arguments
+template <int BITS, int PT, int GT, bool SEEDED> static cudaError_t launch_sized(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
+    return n <= 32 ? launch<BITS, PT, GT, SEEDED, 32>(tbl, at, n, h, st) : launch<BITS, PT, GT, SEEDED, MOST>(tbl, at, n, h, st);
+}
+template <int BITS, int PT, int GT> static cudaError_t launch_some(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
+    if (h.seeded && (BITS == 8 || PT == PACER_BF16)) return launch_sized<BITS, PT, GT, BITS == 8 || PT == PACER_BF16>(tbl, at, n, h, st);
+    return launch_sized<BITS, PT, GT, false>(tbl, at, n, h, st);
 }
 
 cudaError_t adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg &cfg, cudaStream_t st) {
@@ -286,17 +436,27 @@ cudaError_t adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg &c
     h.s2 = (float)(1.0 / std::sqrt(1.0 - std::pow(cfg.beta_two, (double)cfg.step)));
     h.b1d = cfg.beta_one; h.b2d = cfg.beta_two; h.lr = cfg.lr; h.wd = cfg.weight_decay;
     h.max_norm = (float)cfg.max_norm;
+    h.one = 1.f;
     h.norm = cfg.norm; h.lr_dev = cfg.lr_device; h.step_dev = cfg.step_device;
     h.seeded = cfg.seeded;
     h.seed = (uint32_t)cfg.seed ^ mix((uint32_t)(cfg.seed >> 32));
     h.step = (uint32_t)cfg.step;
-    constexpr int MOST = 480;
-    for (int i = 0; i < n; i += MOST) {
-        const int to = std::min(n, i + MOST), k = to - i;
-        cudaError_t e;
-        if (cfg.state_bits == 32) e = k <= 16 ? launch<32, 16>(tbl, i, to, h, st) : k <= 96 ? launch<32, 96>(tbl, i, to, h, st) : launch<32, MOST>(tbl, i, to, h, st);
-        else e = k <= 16 ? launch<8, 16>(tbl, i, to, h, st) : k <= 96 ? launch<8, 96>(tbl, i, to, h, st) : launch<8, MOST>(tbl, i, to, h, st);
-        if (e != cudaSuccess) return e;
+    typedef cudaError_t (*Fn)(const pacer_adamw_tensor *, const int *, int, const Hyper &, cudaStream_t);
+    static const Fn fn[2][2][3] = {
+        {{launch_some<32, PACER_F32, PACER_F32>, launch_some<32, PACER_F32, PACER_BF16>, launch_some<32, PACER_F32, PACER_F16>},
+         {launch_some<32, PACER_BF16, PACER_F32>, launch_some<32, PACER_BF16, PACER_BF16>, launch_some<32, PACER_BF16, PACER_F16>}},
+        {{launch_some<8, PACER_F32, PACER_F32>, launch_some<8, PACER_F32, PACER_BF16>, launch_some<8, PACER_F32, PACER_F16>},
+         {launch_some<8, PACER_BF16, PACER_F32>, launch_some<8, PACER_BF16, PACER_BF16>, launch_some<8, PACER_BF16, PACER_F16>}}};
+    for (int types = 0; types < 6; ++types) {                          // (one launch for each pair of types that there is)
+        int at[MOST], k = 0;
+        for (int i = 0; i <= n; ++i) {
+            if (k == MOST || (i == n && k)) {
+                const cudaError_t e = fn[cfg.state_bits == 8][types / 3][types % 3](tbl, at, k, h, st);
+                if (e != cudaSuccess) return e;
+                k = 0;
+            }
+            if (i < n && tbl[i].numel && tbl[i].param_type == types / 3 && tbl[i].grad_type == types % 3) at[k++] = i;
+        }
     }
     return cudaSuccess;
 }
@@ -316,19 +476,14 @@ template <int CAP> struct StateTable {
 };
 
 template <bool VEC> __device__ __forceinline__ void read_states(const StateItem &t, int64_t base, int lane) {
-    uint32_t c[8];
     float x[8];
     const float2 s = *reinterpret_cast<const float2 *>(t.scales + (base >> 8) * 2);
     if (t.om) {
-        load_codes<VEC>(t.m, base, lane, t.numel, c);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = value_m(c[k], s.x);
+        values<true>(load_codes<VEC>(t.m, base, lane, t.numel), s.x, x);
         store<VEC>(t.om, base, lane, t.numel, x);
     }
     if (t.ov) {
-        load_codes<VEC>(t.v, base, lane, t.numel, c);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = value_v(c[k], s.y);
+        values<false>(load_codes<VEC>(t.v, base, lane, t.numel), s.y, x);
         store<VEC>(t.ov, base, lane, t.numel, x);
     }
 }
@@ -360,7 +515,6 @@ static cudaError_t launch_states(const pacer_adamw_tensor *tbl, int from, int to
     return cudaGetLastError();
 }
 cudaError_t states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, cudaStream_t st) {
-    constexpr int MOST = 480;
     for (int i = 0; i < n; i += MOST) {
         const int to = std::min(n, i + MOST), k = to - i;
         const cudaError_t e = k <= 16 ? launch_states<16>(tbl, i, to, exp_avg, exp_avg_sq, st) : k <= 96 ? launch_states<96>(tbl, i, to, exp_avg, exp_avg_sq, st)
@@ -377,13 +531,48 @@ struct NormItem {
     int64_t numel;
     uint32_t first, type;
 };
+constexpr int NORM_CHUNK = 4 * PASS;
+
 template <int CAP> struct NormTable {
     double *part;                          // of this launch's blocks
     int32_t n;
     uint32_t chunks;
     NormItem t[CAP];
 };
-constexpr int NORM_CHUNK = 4 * PASS;
+// |x| in 64 bits by moving its fields: a conversion has a quarter of the rate, which 16-bit gradients at the memory's rate would need in full.
+// What is below f32's normal numbers, 0 among it, becomes some number below 2^-126, infinities and NaN some number from 2^128 on, so that
+// the norm as f32 is infinite; a norm below 2^-100 is 0.
+__device__ __forceinline__ double magnitude(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+    return __hiloint2double((int)((b >> 3) + (896u << 20)), (int)(b << 29));
+}
+template <int TYPE> __device__ __forceinline__ void squares(const Raw<TYPE> &r, double &s0, double &s1) {
+    float x[8];
+    widen8<TYPE>(r, x);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const double a = magnitude(x[k]), c = magnitude(x[k + 1]);
+        s0 = fma(a, a, s0);
+        s1 = fma(c, c, s1);
+    }
+}
+// A warp's part of a chunk; whole ones with all loads under way at once.
+template <int TYPE> __device__ __forceinline__ void chunk_squares(const NormItem &t, int64_t base, int64_t end, int lane, double &s0, double &s1) {
+    if (aligned(t.p, 16) && base + NORM_CHUNK - PASS + 256 <= end) {
+        Raw<TYPE> r[NORM_CHUNK / PASS];
+#pragma unroll
+        for (int i = 0; i < NORM_CHUNK / PASS; ++i) fetch<true, TYPE>(t.p, base + i * PASS, lane, t.numel, r[i]);
+#pragma unroll
+        for (int i = 0; i < NORM_CHUNK / PASS; ++i) squares<TYPE>(r[i], s0, s1);
+        return;
+    }
+#pragma unroll 1
+    for (; base < end; base += PASS) {
+        Raw<TYPE> r;
+        fetch<false, TYPE>(t.p, base, lane, t.numel, r);
+        squares<TYPE>(r, s0, s1);
+    }
+}
 
 // Sums in 64 bits: f32 sums of 10^9 squares would be off in the fifth digit, and the norm scales every gradient.
 template <int CAP>
@@ -394,19 +583,10 @@ __global__ void __launch_bounds__(THREADS_W) k_norm(const __grid_constant__ Norm
     double s0 = 0.0, s1 = 0.0;
     for (uint32_t c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
         const NormItem t = tab.t[tensor_of(tab, c)];
-        const bool vec = aligned(t.p, 16);
-        const int64_t start = (int64_t)(c - t.first) * NORM_CHUNK + warp * 256;
-#pragma unroll 4
-        for (int64_t base = start; base < start + NORM_CHUNK && base < t.numel; base += PASS) {
-            float x[8];
-            if (vec && base + 256 <= t.numel) load<true>(t.p, t.type, base, lane, t.numel, x);
-            else load<false>(t.p, t.type, base, lane, t.numel, x);
-#pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                s0 = fma((double)x[k], (double)x[k], s0);
-                s1 = fma((double)x[k + 1], (double)x[k + 1], s1);
-            }
-        }
+        const int64_t from = (int64_t)(c - t.first) * NORM_CHUNK, end = min(from + NORM_CHUNK, t.numel);
+        if (t.type == PACER_F32) chunk_squares<PACER_F32>(t, from + warp * 256, end, lane, s0, s1);
+        else if (t.type == PACER_BF16) chunk_squares<PACER_BF16>(t, from + warp * 256, end, lane, s0, s1);
+        else chunk_squares<PACER_F16>(t, from + warp * 256, end, lane, s0, s1);
     }
     s0 += s1;
 #pragma unroll
@@ -429,7 +609,8 @@ __global__ void __launch_bounds__(THREADS_W) k_norm_end(const double *part, int 
     __syncthreads();
     if (threadIdx.x) return;
     for (int w = 1; w < THREADS_W / 32; ++w) s += red[w];
-    *norm = (float)sqrt(s);
+    s = sqrt(s);
+    *norm = s < 0x1p-100 ? 0.f : (float)s;      // (what zeros add up to)
 }
 
 size_t norm_scratch_bytes(int n) { return (size_t)((n + NORM_CAP - 1) / NORM_CAP) * NORM_BLOCKS * sizeof(double); }
