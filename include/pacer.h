@@ -379,8 +379,8 @@ int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head,
  * dhidden = dz head and dhead = dz^T hidden, both bf16, rows ld_dhidden and ld_dhead apart, each may be NULL.  logp, lse, entropy: as
  * pacer_head_logprobs left them for the same hidden, head, tokens and bias.  Each of g_logp, g_entropy, g_lse (f32 [rows]) may be
  * NULL, not all three; tokens and logp may be NULL where g_logp is, entropy where g_entropy is.  A row whose token names nothing has
- * no g_logp term.  dz is rounded to bf16 once, as an operand of the products; their sums are fp32.  It is kept for as many tokens at a
- * time as 1 GB holds, so that the scratch stays bounded for any number of rows.
+ * no g_logp term.  dz is rounded to bf16 once, as an operand of the products (up to 128 rows its rounding remainders are multiplied too); their
+ * sums are fp32.  It is kept for as many tokens at a time as 2 GB holds, so that the scratch stays bounded for any number of rows.
  * Addresses 16-byte aligned, strides multiples of 8; the gradients overlap neither the operands nor each other.  rows = 0 sets dhead
  * to 0.  scratch: device, 256-byte aligned, at least pacer_head_logprobs_backward_scratch_bytes(rows, vocab, d) bytes, in use until the
  * call's kernels have run.  No atomics: the same call gives the same bits.  Enqueues two kernels for a piece of the vocabulary and one at
@@ -393,7 +393,7 @@ int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const vo
 
 /* Softmax cross entropy of given tokens straight from hidden rows and head, without keeping the logits, and its gradients in the same
  * call: loss[r] = lse - z[tokens[r]] (f32 [rows]; 0 where the token names nothing; may be NULL), dhidden and dhead (each may be NULL)
- * of sum_r weight[r] loss[r].  Arguments otherwise as above. */
+ * of sum_r weight[r] loss[r].  Arguments otherwise as above.  Where dz of the whole vocabulary fits 2 GB the logits are computed once, else twice. */
 size_t pacer_head_nll_grad_scratch_bytes(int rows, int vocab, int d);
 int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
                         const int32_t *tokens, const int32_t *bias_ids, float bias, const float *weight, float *loss, void *dhidden,

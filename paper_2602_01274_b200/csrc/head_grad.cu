@@ -23,7 +23,8 @@ using namespace pr;
 constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's half of a tile, columns of a tile; 64 rows x 64 columns
 constexpr int STAGE = 4 * PANEL, STAGES = 6, OUT = 32 * 128;
 constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT;
-constexpr size_t MOST_DZ = (size_t)1 << 30;
+constexpr size_t MOST_DZ = (size_t)2 << 30;               // bytes of dz (without remainders) that are kept at a time
+constexpr int FEW = 128;                                  // rows up to which dz comes with its rounding remainders
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct ZArgs {
@@ -31,15 +32,16 @@ struct ZArgs {
     const int32_t *tokens, *bias_ids;
     float bias, sign;
     const float *logp, *lse, *entropy, *g_logp, *g_entropy, *g_lse;
-    bf16 *dz;
+    bf16 *dz, *low;                            // low: the rounding remainders, or NULL
 };
 
 struct PArgs {
     int32_t rows, width, d, dp, bn, nt;        // nt: tiles of d
-    int32_t mt_w, mt_h, k_w, k_h, per, splits; // tiles of tokens and rows; k blocks of 64 of each product, of a share of dhidden's
+    int32_t mt_w, mt_h, k_w, k_h, per, splits; // tiles of tokens and rows; k blocks of 64 of each product (of all planes), of a share of dhidden's
     int32_t n_h, n_w, early;                   // items of dhidden and dhead, dhead's that the less loaded workers take first
     int32_t add;                               // dhidden's sums are added to those that are there
-    float *part;                               // [splits][rows][dp], or NULL: dhidden is written
+    int32_t planes;                            // 2: dz and its remainders (at most 128 rows)
+    float *part;                               // [planes][splits][rows][dp], or NULL: dhidden is written
 };
 
 // The roles of a pair's blocks (warps 0..7 epilogue, 8 copies, 9 tensor cores) and what they share.
@@ -99,11 +101,6 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ void st32(void *p, const uint32_t *v) {         // 32 bytes, aligned
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
-                 "r"(v[6]), "r"(v[7]) : "memory");
-}
-
 // ----------------------------------------------------------------------------- dz of a piece of the vocabulary
 
 // Persistent as k_head_score: row tiles vary fastest.
@@ -189,7 +186,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                 if (n0 + at >= a.ld) break;
                 uint32_t v[32];
                 tmem_ld32(acc + at, v);
-                uint32_t w[16];
+                uint32_t w[16], l16[16];
                 float g[2];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
@@ -198,7 +195,10 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                     const float l = fmaf(z, LOG2E, -lse), p = ex2(l);
                     g[e & 1] = p * fmaf(h, l, c);
                     if (tok - at == e) g[e & 1] = p * fmaf(h, l, c + gl) - gl * expm1f(lp);
-                    if (e & 1) w[e >> 1] = pack(g[0], g[1]);
+                    if (e & 1) {
+                        w[e >> 1] = pack(g[0], g[1]);
+                        if (a.low) l16[e >> 1] = pack(g[0] - __uint_as_float(w[e >> 1] << 16), g[1] - __uint_as_float(w[e >> 1] & 0xffff0000u));
+                    }
                 }
                 if (!ok)
 #pragma unroll
@@ -207,6 +207,11 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                     bf16 *p = a.dz + (size_t)r * a.ld + n0 + at;
                     st32(p, w);
                     st32(p + 16, w + 8);
+                    if (a.low) {
+                        p = a.low + (size_t)r * a.ld + n0 + at;
+                        st32(p, l16);
+                        st32(p + 16, l16 + 8);
+                    }
                 }
             }
             release_acc(s, i, lane);
@@ -239,7 +244,10 @@ __device__ __forceinline__ bool item_of(const PArgs &a, int worker, int workers,
 
 // dhead tiles: A = dz by its columns (MN-major), B = hidden (MN-major), k = rows.  dhidden tiles: A = dz (K-major), B = head (MN-major),
 // k = tokens.  All tensor copies are 64 x 64: a panel of an MN-major operand, half of a K-major one.
-__global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_x,
+// Up to 128 rows dz comes with its rounding remainders, which cost little there: dhead has twice the k blocks, which its stores outlast, and the
+// second block of a pair, whose rows would be empty, multiplies the remainders (its sums are a share of their own).
+__global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_low,
+                                                            const __grid_constant__ CUtensorMap map_x,
                                                             const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_dw,
                                                             const __grid_constant__ CUtensorMap map_dx, const PArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -258,7 +266,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
             bool ok = true;
             for (int j = 0; ok && item_of(a, worker, workers, j, it); ++j) {
                 const CUtensorMap *mb = it.to_head ? &map_x : &map_w;
-                const int m = it.m0 + rank * TM, nb = it.n0 + rank * half_n;
+                const int m = it.m0 + (it.to_head || a.planes == 1 ? rank * TM : 0), nb = it.n0 + rank * half_n, k_one = a.k_w / a.planes;
                 for (int kb = it.k0; kb < it.k1; ++kb, ++n) {
                     const int slot = n % STAGES;
                     ok = wait_h(&s.gave_up, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
@@ -266,9 +274,11 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                     unsigned char *st = smem + slot * STAGE;
                     if (rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * TM + a.bn) * 128u);
                     const uint32_t bar = first_block(s.full + slot);
-                    for (int q = 0; q < 2; ++q)
-                        tma_2d<true>(st + q * PANEL, &map_z, it.to_head ? m + q * 64 : kb * 64, it.to_head ? kb * 64 : m + q * 64, bar, normal);
-                    for (int q = 0; q * 64 < half_n; ++q) tma_2d<true>(st + (2 + q) * PANEL, mb, nb + q * 64, kb * 64, bar, normal);
+                    const bool second = it.to_head && kb >= k_one;
+                    const CUtensorMap *ma = second || (!it.to_head && a.planes == 2 && rank) ? &map_low : &map_z;
+                    const int k = (second ? kb - k_one : kb) * 64;
+                    for (int q = 0; q < 2; ++q) tma_2d<true>(st + q * PANEL, ma, it.to_head ? m + q * 64 : k, it.to_head ? k : m + q * 64, bar, normal);
+                    for (int q = 0; q * 64 < half_n; ++q) tma_2d<true>(st + (2 + q) * PANEL, mb, nb + q * 64, k, bar, normal);
                 }
             }
             drain(s, n, rank);
@@ -305,7 +315,8 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
             if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u);
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
-            const int m = it.m0 + rank * TM + quad * 32, n0 = it.n0 + half * half_n, last = it.to_head ? a.width : a.rows;
+            const int plane = !it.to_head && a.planes == 2 ? rank : 0;
+            const int m = it.m0 + (plane ? 0 : rank * TM) + quad * 32, n0 = it.n0 + half * half_n, last = it.to_head ? a.width : a.rows;
             const bool sums = !it.to_head && a.part;
             for (int c = 0; c < half_n; c += 64) {
                 if (m >= last || n0 + c >= a.dp) break;
@@ -317,7 +328,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                     for (int e = 0; e < 64; ++e) v[e] = ok ? 0u : 0x7fffffffu;
                 if (sums) {
                     if (m + lane < last) {
-                        float *p = a.part + ((size_t)it.split * a.rows + m + lane) * a.dp + n0 + c;
+                        float *p = a.part + ((size_t)(plane * a.splits + it.split) * a.rows + m + lane) * a.dp + n0 + c;
 #pragma unroll
                         for (int e = 0; e < 64; e += 8) {
                             if (a.add) {
@@ -356,21 +367,27 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
     pair_end(tmem, warp);
 }
 
-// dhidden = the sum of the shares, eight columns a thread.
+// dhidden = the sum of the shares: four lanes, 8 apart, for eight columns, each a quarter of the shares.
 __global__ void __launch_bounds__(256) k_head_sum(const float *part, int splits, int rows, int d, int dp, bf16 *out, int64_t ld) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int per = d >> 3;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)rows * per) return;
-    const int64_t r = i / per, c = (i - r * per) * 8;
+    const int per = d >> 3, q = (threadIdx.x >> 3) & 3;
+    const int64_t i = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 5) * 8 + (threadIdx.x & 7);
+    const bool on = i < (int64_t)rows * per;
+    const int64_t r = on ? i / per : 0, c = on ? (i - r * per) * 8 : 0;
     float v[8] = {};
-    for (int k = 0; k < splits; ++k) {
+#pragma unroll 4
+    for (int k = on ? q : splits; k < splits; k += 4) {
         const float4 *p = reinterpret_cast<const float4 *>(part + ((size_t)k * rows + r) * dp + c);
         const float4 x = __ldcg(p), y = __ldcg(p + 1);
         v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
     }
-    *reinterpret_cast<uint4 *>(out + r * ld + c) = make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] += __shfl_xor_sync(~0u, v[e], 8);
+        v[e] += __shfl_xor_sync(~0u, v[e], 16);
+    }
+    if (on && q == 0) *reinterpret_cast<uint4 *>(out + r * ld + c) = make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]), pack(v[6], v[7]));
 }
 
 // ----------------------------------------------------------------------------- host
@@ -378,8 +395,9 @@ __global__ void __launch_bounds__(256) k_head_sum(const float *part, int splits,
 struct Plan {
     int pieces, width;                     // tokens of a piece
     int ld;                                // of dz
-    int bn, nt, dp, mt_h, splits, per;
-    size_t dz_bytes, part_bytes;
+    int bn, nt, dp, mt_h, splits, per, planes;
+    size_t plane_bytes, part_bytes;
+    size_t bytes() const { return plane_bytes * planes + part_bytes; }
 };
 static int up(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
@@ -396,9 +414,10 @@ static Plan plan_of(int rows, int vocab, int d, bool to_hidden, bool to_head, in
     p.nt = up(d, p.bn);
     p.dp = up(d, 64) * 64;
     p.mt_h = up(rows, 2 * TM);
+    p.planes = rows <= FEW ? 2 : 1;
     const int workers = n_sm / 2, k_h = up(p.width, 64);
     // dhidden's product is cut along the tokens into the number of shares with the least time until the last worker is done
-    const int64_t tiles = (int64_t)p.mt_h * p.nt, head = to_head ? (int64_t)up(p.width, 2 * TM) * p.nt * (up(rows, 64) + EXTRA) : 0;
+    const int64_t tiles = (int64_t)p.mt_h * p.nt, head = to_head ? (int64_t)up(p.width, 2 * TM) * p.nt * (up(rows, 64) * p.planes + EXTRA) : 0;
     p.splits = 1;
     p.per = k_h;
     if (to_hidden) {
@@ -407,12 +426,12 @@ static Plan plan_of(int rows, int vocab, int d, bool to_hidden, bool to_head, in
             const int per = up(k_h, n), shares = up(k_h, per);
             const double own = (double)up(tiles * shares, workers) * (per + EXTRA), all = ((double)tiles * shares * (per + EXTRA) + head) / workers;
             // (sums written and read at 6 TB/s; a launch)
-            const double cost = std::max(own, all) + (shares > 1 || p.pieces > 1 ? 10 + (double)shares * rows * p.dp * 8 / 1.6e6 : 0);
+            const double cost = std::max(own, all) + (shares > 1 || p.pieces > 1 || p.planes > 1 ? 10 + (double)shares * p.planes * rows * p.dp * 8 / 1.6e6 : 0);
             if (n == 1 || cost < best) { best = cost; p.splits = shares; p.per = per; }
         }
     }
-    p.dz_bytes = ((size_t)rows * p.ld * 2 + 255) & ~(size_t)255;
-    p.part_bytes = to_hidden && (p.splits > 1 || p.pieces > 1) ? (size_t)p.splits * rows * p.dp * 4 : 0;
+    p.plane_bytes = ((size_t)rows * p.ld * 2 + 255) & ~(size_t)255;
+    p.part_bytes = to_hidden && (p.splits > 1 || p.pieces > 1 || p.planes > 1) ? (size_t)p.planes * p.splits * rows * p.dp * 4 : 0;
     return p;
 }
 
@@ -420,7 +439,7 @@ size_t scratch_bytes(int rows, int vocab, int d, int n_sm) {
     size_t most = 0;
     for (int k = 1; k < 4; ++k) {
         const Plan p = plan_of(rows, vocab, d, k & 1, k & 2, n_sm);
-        most = std::max(most, p.dz_bytes + p.part_bytes);
+        most = std::max(most, p.bytes());
     }
     return most;
 }
@@ -470,6 +489,45 @@ static int z_width(int mt, int width, int workers) {
     return best;
 }
 
+// The products of dz of one piece, and after the last one the sum.
+static cudaError_t products(const Args &a, const Plan &p, EncodeFn encode, int piece, bf16 *dz, bf16 *low, float *part, int workers, cudaStream_t st, bool *no_maps) {
+    const int v0 = piece * p.width, width = std::min(p.width, a.vocab - v0);
+    const bf16 *head = reinterpret_cast<const bf16 *>(a.head) + (size_t)v0 * a.ld_head;
+    bf16 *dhead = a.dhead ? reinterpret_cast<bf16 *>(a.dhead) + (size_t)v0 * a.ld_dhead : nullptr;
+    CUtensorMap mz, ml, mx, mw, mdw, mdx;
+    if (!make_map(encode, &mz, dz, p.ld, a.rows, width, 64) || (low && !make_map(encode, &ml, low, p.ld, a.rows, width, 64)) ||
+        !make_map(encode, &mx, a.hidden, a.ld_hidden, a.rows, a.d, 64) || !make_map(encode, &mw, head, a.ld_head, width, a.d, 64) ||
+        (dhead && !make_map(encode, &mdw, dhead, a.ld_dhead, width, a.d, 32)) ||
+        (a.dhidden && !part && !make_map(encode, &mdx, a.dhidden, a.ld_dhidden, a.rows, a.d, 32))) {
+        *no_maps = true;
+        return cudaSuccess;
+    }
+    if (!low) ml = mz;                     // (what is not used)
+    if (!dhead) mdw = mw;
+    if (!a.dhidden || part) mdx = mw;
+    PArgs q;
+    q.rows = a.rows; q.width = width; q.d = a.d; q.dp = p.dp; q.bn = p.bn; q.nt = p.nt;
+    q.mt_w = up(width, 2 * TM); q.mt_h = p.mt_h; q.planes = p.planes; q.k_w = up(a.rows, 64) * p.planes; q.k_h = up(width, 64);
+    q.splits = p.splits; q.per = up(q.k_h, p.splits);
+    q.n_h = a.dhidden ? p.splits * p.mt_h * p.nt : 0;
+    q.n_w = dhead ? q.mt_w * p.nt : 0;
+    q.early = (q.per + EXTRA) / (q.k_w + EXTRA);
+    q.add = piece > 0;
+    q.part = part;
+    Launch l((unsigned)std::min<int64_t>(workers, (int64_t)q.n_h + q.n_w) * 2, THREADS_G, SMEM_P, st, true, true);
+    cudaError_t e = cudaLaunchKernelEx(&l.c, k_head_prod, mz, ml, mx, mw, mdw, mdx, q);
+    if (e != cudaSuccess || !part || piece < p.pieces - 1) return e;
+    Launch s((unsigned)(((int64_t)a.rows * (a.d >> 3) + 63) / 64), 256, 0, st, false, true);
+    return cudaLaunchKernelEx(&s.c, k_head_sum, (const float *)part, p.splits * p.planes, a.rows, a.d, p.dp, reinterpret_cast<bf16 *>(a.dhidden), a.ld_dhidden);
+}
+
+struct Places { bf16 *dz, *low; float *part; };
+static Places places(const Plan &p, void *scratch) {
+    char *at = reinterpret_cast<char *>(scratch);
+    return {reinterpret_cast<bf16 *>(at), p.planes == 2 ? reinterpret_cast<bf16 *>(at + p.plane_bytes) : nullptr,
+            p.part_bytes ? reinterpret_cast<float *>(at + p.plane_bytes * p.planes) : nullptr};
+}
+
 cudaError_t run(const Args &a, void *scratch, int n_sm, bool after, cudaStream_t st, bool *no_maps) {
     *no_maps = false;
     EncodeFn encode;
@@ -480,68 +538,61 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, bool after, cudaStream_t
     if (e != cudaSuccess) return e;
     const Plan p = plan_of(a.rows, a.vocab, a.d, a.dhidden, a.dhead, n_sm);
     const int workers = n_sm / 2;
-    bf16 *dz = reinterpret_cast<bf16 *>(scratch);
-    float *part = p.part_bytes ? reinterpret_cast<float *>(reinterpret_cast<char *>(scratch) + p.dz_bytes) : nullptr;
-    bool early = after;
+    const Places at = places(p, scratch);
     for (int i = 0; i < p.pieces; ++i) {
-        const int v0 = i * p.width, width = std::min(p.width, a.vocab - v0);
-        const bf16 *head = reinterpret_cast<const bf16 *>(a.head) + (size_t)v0 * a.ld_head;
-        bf16 *dhead = a.dhead ? reinterpret_cast<bf16 *>(a.dhead) + (size_t)v0 * a.ld_dhead : nullptr;
         ZArgs z;
-        z.rows = a.rows; z.width = width; z.v0 = v0; z.vocab = a.vocab; z.nkb = up(a.d, 64); z.mt = up(a.rows, 2 * TM); z.ld = p.ld;
-        z.bn = z_width(z.mt, width, workers);
-        z.nt = up(width, z.bn);
+        z.v0 = i * p.width; z.width = std::min(p.width, a.vocab - z.v0);
+        z.rows = a.rows; z.vocab = a.vocab; z.nkb = up(a.d, 64); z.mt = up(a.rows, 2 * TM); z.ld = p.ld;
+        z.bn = z_width(z.mt, z.width, workers);
+        z.nt = up(z.width, z.bn);
         z.a_rows = std::min(TM, (a.rows + 7) & ~7);
         z.tokens = a.tokens; z.bias_ids = a.bias_ids; z.bias = a.bias; z.sign = a.sign;
         z.logp = a.logp; z.lse = a.lse; z.entropy = a.entropy; z.g_logp = a.g_logp; z.g_entropy = a.g_entropy; z.g_lse = a.g_lse;
-        z.dz = dz;
-        CUtensorMap ma, mb, mz, mx, mw, mdw, mdx;
-        if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, z.a_rows) || !make_map(encode, &mb, head, a.ld_head, width, a.d, z.bn / 2) ||
-            !make_map(encode, &mz, dz, p.ld, a.rows, width, 64) || !make_map(encode, &mx, a.hidden, a.ld_hidden, a.rows, a.d, 64) ||
-            !make_map(encode, &mw, head, a.ld_head, width, a.d, 64) || (dhead && !make_map(encode, &mdw, dhead, a.ld_dhead, width, a.d, 32)) ||
-            (a.dhidden && !part && !make_map(encode, &mdx, a.dhidden, a.ld_dhidden, a.rows, a.d, 32))) {
+        z.dz = at.dz; z.low = at.low;
+        CUtensorMap ma, mb;
+        if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, z.a_rows) ||
+            !make_map(encode, &mb, reinterpret_cast<const bf16 *>(a.head) + (size_t)z.v0 * a.ld_head, a.ld_head, z.width, a.d, z.bn / 2)) {
             *no_maps = true;
             return cudaSuccess;
         }
-        if (!dhead) mdw = mw;              // (not used)
-        if (!a.dhidden || part) mdx = mw;
-        {
-            Launch l((unsigned)std::min<int64_t>(workers, (int64_t)z.mt * z.nt) * 2, THREADS_G, SMEM_Z, st, true, early);
-            e = cudaLaunchKernelEx(&l.c, k_head_z, ma, mb, z);
-            if (e != cudaSuccess) return e;
-        }
-        early = true;
-        PArgs q;
-        q.rows = a.rows; q.width = width; q.d = a.d; q.dp = p.dp; q.bn = p.bn; q.nt = p.nt;
-        q.mt_w = up(width, 2 * TM); q.mt_h = p.mt_h; q.k_w = up(a.rows, 64); q.k_h = up(width, 64);
-        q.splits = p.splits; q.per = up(q.k_h, p.splits);
-        q.n_h = a.dhidden ? p.splits * p.mt_h * p.nt : 0;
-        q.n_w = dhead ? q.mt_w * p.nt : 0;
-        q.early = (q.per + EXTRA) / (q.k_w + EXTRA);
-        q.add = i > 0;
-        q.part = part;
-        Launch l((unsigned)std::min<int64_t>(workers, (int64_t)q.n_h + q.n_w) * 2, THREADS_G, SMEM_P, st, true, early);
-        e = cudaLaunchKernelEx(&l.c, k_head_prod, mz, mx, mw, mdw, mdx, q);
-        if (e != cudaSuccess) return e;
+        Launch l((unsigned)std::min<int64_t>(workers, (int64_t)z.mt * z.nt) * 2, THREADS_G, SMEM_Z, st, true, after || i);
+        e = cudaLaunchKernelEx(&l.c, k_head_z, ma, mb, z);
+        if (e == cudaSuccess) e = products(a, p, encode, i, at.dz, at.low, at.part, workers, st, no_maps);
+        if (e != cudaSuccess || *no_maps) return e;
     }
-    if (!part) return cudaSuccess;
-    Launch l((unsigned)(((int64_t)a.rows * (a.d >> 3) + 255) / 256), 256, 0, st, false, true);
-    return cudaLaunchKernelEx(&l.c, k_head_sum, (const float *)part, p.splits, a.rows, a.d, p.dp, reinterpret_cast<bf16 *>(a.dhidden), a.ld_dhidden);
+    return cudaSuccess;
 }
 
-// The head's own scratch is free again when dz is written, and shares its memory.
+// Where dz of the whole vocabulary is kept the loss's pass leaves it (hs::Args::dz), else z is computed again piece by piece.  The loss's own scratch
+// lies behind dz in the first case; in the second it is free again when dz is written, and shares its memory.
 static size_t rows_bytes(int rows) { return ((size_t)rows * 8 + 255) & ~(size_t)255; }
 
 size_t nll_scratch_bytes(int rows, int vocab, int d, int n_sm) {
-    return rows_bytes(rows) + std::max(hs::scratch_bytes(rows, vocab), scratch_bytes(rows, vocab, d, n_sm));
+    const size_t own = (hs::scratch_bytes(rows, vocab) + 255) & ~(size_t)255, most = scratch_bytes(rows, vocab, d, n_sm);
+    return plan_of(rows, vocab, d, true, true, n_sm).pieces == 1 ? own + most : rows_bytes(rows) + std::max(own, most);
 }
 
 cudaError_t run_nll(const Args &a, float *loss, void *scratch, int n_sm, cudaStream_t st, bool *no_maps) {
+    const Plan p = plan_of(a.rows, a.vocab, a.d, a.dhidden, a.dhead, n_sm);
+    const bool grads = a.dhidden || a.dhead;
+    hs::Args h = {a.hidden, a.head, a.ld_hidden, a.ld_head, a.rows, a.vocab, a.d, a.tokens, a.bias_ids, a.bias, nullptr, nullptr, nullptr};
+    h.loss = loss;
+    if (grads && p.pieces == 1) {
+        const size_t own = (hs::scratch_bytes(a.rows, a.vocab) + 255) & ~(size_t)255;
+        const Places at = places(p, reinterpret_cast<char *>(scratch) + own);
+        h.dz = at.dz; h.dz_low = at.low; h.ld_dz = p.ld; h.weight = a.g_logp;
+        cudaError_t e = hs::run(h, scratch, n_sm, st, no_maps);
+        if (e != cudaSuccess || *no_maps) return e;
+        EncodeFn encode;
+        e = encode_fn(&encode);
+        if (e == cudaSuccess) e = opt_in();
+        return e != cudaSuccess ? e : products(a, p, encode, 0, at.dz, at.low, at.part, n_sm / 2, st, no_maps);
+    }
     float *logp = reinterpret_cast<float *>(scratch), *lse = logp + a.rows;
     void *rest = reinterpret_cast<char *>(scratch) + rows_bytes(a.rows);
-    cudaError_t e = hs::run({a.hidden, a.head, a.ld_hidden, a.ld_head, a.rows, a.vocab, a.d, a.tokens, a.bias_ids, a.bias, logp, nullptr, lse, loss},
-                            rest, n_sm, st, no_maps);
-    if (e != cudaSuccess || *no_maps || (!a.dhidden && !a.dhead)) return e;
+    h.logp = logp; h.lse = lse;
+    cudaError_t e = hs::run(h, rest, n_sm, st, no_maps);
+    if (e != cudaSuccess || *no_maps || !grads) return e;
     Args b = a;
     b.logp = logp;
     b.lse = lse;

@@ -13,6 +13,8 @@
 // (m, sum 2^t, sum 2^t t), t = (z - m) log2(e), in the scratch, and a second kernel joins a row's halves.
 #include "head_score.h"
 
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "pair.cuh"
@@ -42,6 +44,8 @@ struct KArgs {
     float bias;
     Part *part;                            // [rows][2 * nt]
     float *ztok;                           // [rows]
+    __half *keep;                          // [rows][ld_keep], or NULL (see k_head_dz)
+    int32_t ld_keep;
 };
 
 struct Run {                               // a thread's running sums
@@ -64,7 +68,8 @@ struct Run {                               // a thread's running sums
 // Persistent: block b computes the tiles b, b + grid, ...; row tiles vary fastest, so that the blocks that run together share
 // their weights in L2.  Warps 0..7 epilogues (warp w reads accumulator lanes 32 (w % 4) .., the first or second half of the
 // tile's tokens), warp 8 copies, warp 9 tensor cores.
-template <bool PAIR>
+// KEEP: 2^t is kept besides, t relative to the half tile's maximum; the row's token is left out of maximum and sums (it has its logit in ztok).
+template <bool PAIR, bool KEEP>
 __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                              const KArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -202,6 +207,14 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                     if (left < 32)                                    // columns past the vocabulary
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = e < left ? v[e] : OUTSIDE;
+                    if (KEEP) {
+                        if ((uint32_t)(tok - at) < 32u)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = tok - at == e ? OUTSIDE : v[e];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s.m = fmaxf(s.m, v[e]);
+                        continue;
+                    }
                     float top = v[0];
 #pragma unroll
                     for (int e = 1; e < 32; ++e) top = fmaxf(top, v[e]);
@@ -215,6 +228,27 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                     }
                     s.S += S0 + S1;
                     s.S2 += q0 + q1;
+                }
+            if (KEEP && ok && reads)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int at = (c0 + c) * 32;
+                    if (c0 + c >= c1 || width - at <= 0) continue;
+                    float S0 = 0.f, S1 = 0.f;
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float x0 = ex2((z[c][e] - s.m) * LOG2E), x1 = ex2((z[c][e + 1] - s.m) * LOG2E);
+                        S0 += x0; S1 += x1;
+                        const __half2 h = __floats2half2_rn(x0, x1);
+                        w[e >> 1] = *reinterpret_cast<const uint32_t *>(&h);
+                    }
+                    s.S += S0 + S1;
+                    if (live) {
+                        __half *p = a.keep + (size_t)r * a.ld_keep + n0 + at;
+                        st32(p, w);
+                        st32(p + 16, w + 8);
+                    }
                 }
             if (live) {
                 if (!ok) s.S = s.S2 = __int_as_float(0x7fffffff);
@@ -262,6 +296,87 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
     }
 }
 
+// The gradient of sum_r weight_r (lse_r - z_r[token_r]) with respect to the logits, in place of what k_head_score kept: a block joins its row's
+// parts and takes a piece of the row.  What was kept has 11 bits (of a share of its half tile's largest; below 2^-14 of that fewer, below
+// 2^-25 nothing: next to the largest of the row's gradients that is far below a half step of bf16, the row's token being left out), so that
+// rounding it to bf16 after the row's factor is known is the only rounding that shows.  Kept in bf16 and scaled, it was rounded twice, and the products'
+// errors were 1.7 times those of exact gradients rounded at the end (1.4 with one rounding).  The token's 1 - p is the others' share, and its
+// loss log(1 + others / its own) where it has the largest logit: confident rows lose nothing.  low: the remainders bf16(x - bf16(x)), or NULL.
+struct DzArgs {
+    int32_t segs, seg;                     // pieces of a row and their columns, a multiple of 8
+    const float *weight;
+    float *loss;
+    __nv_bfloat16 *low;
+};
+constexpr int THREADS_D = 256;
+__global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzArgs g) {
+    __shared__ Part red[THREADS_D / 32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row = blockIdx.x / g.segs, at = (blockIdx.x - row * g.segs) * g.seg, lane = threadIdx.x & 31;
+    const float4 *p = reinterpret_cast<const float4 *>(a.part) + (size_t)row * (2 * a.nt);
+    float m = NO_REF, S = 0.f;
+    for (int i = threadIdx.x; i < 2 * a.nt; i += THREADS_D) {
+        const float4 v = __ldcg(p + i);
+        const float to = fmaxf(m, v.x);
+        S = fmaf(S, ex2(fmaxf((m - to) * LOG2E, FAR)), v.y * ex2(fmaxf((v.x - to) * LOG2E, FAR)));
+        m = to;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float qm = __shfl_xor_sync(~0u, m, o), qS = __shfl_xor_sync(~0u, S, o), to = fmaxf(m, qm);
+        S = fmaf(S, ex2(fmaxf((m - to) * LOG2E, FAR)), qS * ex2(fmaxf((qm - to) * LOG2E, FAR)));
+        m = to;
+    }
+    if (lane == 0) red[threadIdx.x >> 5] = Part{m, S, 0.f, 0.f};
+    __syncthreads();
+    m = red[0].m;
+#pragma unroll
+    for (int w = 1; w < THREADS_D / 32; ++w) m = fmaxf(m, red[w].m);
+    S = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS_D / 32; ++w) S = fmaf(red[w].S, ex2(fmaxf((red[w].m - m) * LOG2E, FAR)), S);
+    int tok = a.tokens[row];
+    if (tok >= a.vocab) tok = -1;
+    const float weight = tok >= 0 ? g.weight[row] : 0.f, zt = tok >= 0 ? __ldcg(a.ztok + row) : NO_REF, rest = m;
+    m = fmaxf(m, zt);
+    const float others = S * ex2(fmaxf((rest - m) * LOG2E, FAR)), mine = tok >= 0 ? ex2(fmaxf((zt - m) * LOG2E, FAR)) : 0.f;
+    S = others + mine;
+    const float l2 = log2f(S), of_token = -weight * (others / S);
+    if (at == 0 && threadIdx.x == 0 && g.loss) g.loss[row] = tok < 0 ? 0.f : zt == m ? log1pf(others) : (m - zt) + l2 * LN2;
+    const int end = min(at + g.seg, a.vocab), chunks = a.bn >> 5, first = (chunks + 1) >> 1;   // (32-token chunks of a tile's first half)
+    uint4 *z = reinterpret_cast<uint4 *>(a.keep + (size_t)row * a.ld_keep), *low = reinterpret_cast<uint4 *>(g.low ? g.low + (size_t)row * a.ld_keep : nullptr);
+    const auto scaled = [&](int c, uint4 v) {
+        const int tile = c / a.bn, half = (c - tile * a.bn) >> 5 >= first;
+        const float t = (p[2 * tile + half].x - m) * LOG2E - l2, f = t < FAR ? 0.f : weight * ex2(t);      // (NaN stays)
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t o[4], r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float2 x = __half22float2(*reinterpret_cast<const __half2 *>(w + e));
+            x.x *= f; x.y *= f;
+            if (tok == c + 2 * e) x.x = of_token;
+            if (tok == c + 2 * e + 1) x.y = of_token;
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x.x, x.y);
+            o[e] = *reinterpret_cast<const uint32_t *>(&b);
+            const __nv_bfloat162 d = __floats2bfloat162_rn(x.x - __low2float(b), x.y - __high2float(b));
+            r[e] = *reinterpret_cast<const uint32_t *>(&d);
+        }
+        z[c >> 3] = make_uint4(o[0], o[1], o[2], o[3]);
+        if (low) low[c >> 3] = make_uint4(r[0], r[1], r[2], r[3]);
+    };
+    constexpr int STEP = THREADS_D * 8;
+    int c = at + threadIdx.x * 8;
+    for (; c + 3 * STEP < end; c += 4 * STEP) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = z[(c + k * STEP) >> 3];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) scaled(c + k * STEP, v[k]);
+    }
+    for (; c < end; c += STEP) scaled(c, z[c >> 3]);
+}
+
 // Tokens of a tile: the width with the least waves x (width + 16).  The 16 stands for a tile's start and end: without it many rows would
 // be cut into the narrowest tiles for a fraction of a wave (2048 rows x 32 000: 32 tokens instead of 256; with 16 or 64 the same widths).
 static int tile_width(int mt, int vocab, int n_sm, int step) {
@@ -279,18 +394,19 @@ struct Tiles { int pair, mt, bn, nt; };
 // for it (2048 rows x 32 000 x 4096: 4.9 GB and 415 us, tensor pipe 91 % active; by single blocks 7.1 GB and 474 us).
 // With 32 000 tokens x 4096: 256 rows 60 us by pairs, 68 by single blocks; 384 rows (three tiles of 128) 100 and 92; 640 (five) 145 and
 // 141; 1100 (nine) 229 and 237.
-static Tiles tiles_of(int rows, int vocab) {
+// keep: tiles of whole chunks of 32.
+static Tiles tiles_of(int rows, int vocab, bool keep) {
     Tiles t;
     const int m128 = (rows + TM - 1) / TM;
     t.pair = m128 % 2 == 0 || m128 >= 9;
     t.mt = t.pair ? (m128 + 1) / 2 : m128;
-    t.bn = tile_width(t.mt, vocab, t.pair ? 74 : 148, t.pair ? 32 : 16);      // (a pair's product takes tokens by 32)
+    t.bn = tile_width(t.mt, vocab, t.pair ? 74 : 148, t.pair || keep ? 32 : 16);      // (a pair's product takes tokens by 32)
     t.nt = (vocab + t.bn - 1) / t.bn;
     return t;
 }
 
 size_t scratch_bytes(int rows, int vocab) {
-    return (size_t)rows * (2 * tiles_of(rows, vocab).nt) * sizeof(Part) + (((size_t)rows * sizeof(float) + 255) & ~(size_t)255);
+    return (size_t)rows * (2 * std::max(tiles_of(rows, vocab, false).nt, tiles_of(rows, vocab, true).nt)) * sizeof(Part) + (((size_t)rows * sizeof(float) + 255) & ~(size_t)255);
 }
 
 cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *no_maps) {
@@ -304,18 +420,21 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     if (e != cudaSuccess) return e;
     if (!encode) { *no_maps = true; return cudaSuccess; }
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-        e = cudaFuncSetAttribute(k_head_score<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        e = cudaFuncSetAttribute(k_head_score<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_score<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_H);
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    const Tiles t = tiles_of(a.rows, a.vocab);
+    const Tiles t = tiles_of(a.rows, a.vocab, a.dz != nullptr);
     KArgs k;
     k.rows = a.rows; k.vocab = a.vocab; k.nkb = (a.d + 63) / 64; k.bn = t.bn; k.mt = t.mt; k.nt = t.nt;
     k.a_rows = std::min(TM, (a.rows + 7) & ~7);
     k.tokens = a.tokens; k.bias_ids = a.bias_ids; k.bias = a.bias;
     k.part = reinterpret_cast<Part *>(scratch);
     k.ztok = reinterpret_cast<float *>(k.part + (size_t)a.rows * (2 * t.nt));
+    k.keep = reinterpret_cast<__half *>(a.dz); k.ld_keep = a.ld_dz;
     CUtensorMap ma, mb;
     if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, k.a_rows) || !make_map(encode, &mb, a.head, a.ld_head, a.vocab, a.d, t.pair ? t.bn / 2 : t.bn)) {
         *no_maps = true;
@@ -331,17 +450,27 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     two[0].val.clusterDim.x = 2; two[0].val.clusterDim.y = two[0].val.clusterDim.z = 1;
     m.attrs = two;
     m.numAttrs = t.pair ? 1 : 0;
-    e = t.pair ? cudaLaunchKernelEx(&m, k_head_score<true>, ma, mb, k) : cudaLaunchKernelEx(&m, k_head_score<false>, ma, mb, k);
+    e = a.dz ? t.pair ? cudaLaunchKernelEx(&m, k_head_score<true, true>, ma, mb, k) : cudaLaunchKernelEx(&m, k_head_score<false, true>, ma, mb, k)
+             : t.pair ? cudaLaunchKernelEx(&m, k_head_score<true, false>, ma, mb, k) : cudaLaunchKernelEx(&m, k_head_score<false, false>, ma, mb, k);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)((a.rows + 3) / 4));
     c.blockDim = dim3(128);
+    DzArgs g;
+    if (a.dz) {                            // rows cut into pieces until there are eight blocks an SM
+        g.segs = std::max(1, std::min((a.vocab + 8 * THREADS_D - 1) / (8 * THREADS_D), (8 * n_sm + a.rows - 1) / a.rows));
+        g.seg = ((a.vocab + g.segs - 1) / g.segs + 7) & ~7;
+        g.weight = a.weight; g.loss = a.loss; g.low = reinterpret_cast<__nv_bfloat16 *>(a.dz_low);
+        c.gridDim = dim3((unsigned)a.rows * (unsigned)g.segs);
+        c.blockDim = dim3(THREADS_D);
+    }
     c.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // it waits for the products by itself
     at[0].val.programmaticStreamSerializationAllowed = 1;
     c.attrs = at;
     c.numAttrs = 1;
+    if (a.dz) return cudaLaunchKernelEx(&c, k_head_dz, k, g);
     return cudaLaunchKernelEx(&c, k_head_join, k, a.logp, a.entropy, a.lse, a.loss);
 }
 

@@ -14,7 +14,12 @@ struct Args {
     const int32_t *tokens, *bias_ids;      // [rows]; bias_ids may be NULL
     float bias;
     float *logp, *entropy, *lse;           // [rows], each may be NULL
-    float *loss = nullptr;                 // -logp, only with logp
+    float *loss = nullptr;                 // -logp; only with logp or dz
+    // instead of logp, entropy and lse: the gradient of sum_r weight[r] loss[r] with respect to the logits, bf16 [rows][ld_dz] (ld_dz a multiple of
+    // 64, at least vocab), and its rounding remainders (may be NULL)
+    void *dz = nullptr, *dz_low = nullptr;
+    int32_t ld_dz = 0;
+    const float *weight = nullptr;
 };
 
 size_t scratch_bytes(int rows, int vocab);

@@ -43,6 +43,10 @@ __device__ __forceinline__ void umma2_commit_if(uint32_t on, uint64_t *bar) {
                  "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
                  ::"r"(smem_u32(bar)), "r"(on), "h"((uint16_t)3) : "memory");
 }
+__device__ __forceinline__ void st32(void *p, const uint32_t *v) {         // 32 bytes, aligned
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+                 "r"(v[6]), "r"(v[7]) : "memory");
+}
 // Bounded wait; one that runs out ends the block's work (its rows become NaN).
 __device__ __forceinline__ bool wait_h(volatile int32_t *gave_up, uint64_t *bar, uint32_t parity) {
     for (unsigned it = 1; !mbar_try_wait(bar, parity); ++it)
