@@ -7,6 +7,7 @@ fails loudly when the library has not been built; there is no CPU fallback.
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes as C
 import math
@@ -670,7 +671,8 @@ class AdamwTensors:
         self._types = np.array([_DTYPES[p.dtype] for p in params], dtype=np.int64)
         self.table = np.zeros((n, 8), dtype=np.int64)
         self.table[:, 6], self.table[:, 7] = self.numel, self._types
-        self._at = self._grads_at = None
+        self._at = self._grads_at = self._grads_types = None
+        self._address = self.table.ctypes.data
         self._gaps = any(t is None for t in self.all)
         self._place()
 
@@ -683,6 +685,7 @@ class AdamwTensors:
                 self.table[:, col] = at[i * n:(i + 1) * n]
 
     def with_grads(self, grads):
+        """The table's address."""
         if not self.numel:
             raise AssertionError("grads: one for each param")
         types, at = _gradients(grads, self.device)
@@ -691,9 +694,16 @@ class AdamwTensors:
         self._place()
         if at != self._grads_at:
             self._grads_at = at
-            self.table[:, 2] = at
-        self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32)
-        return self.table
+            self.table[:, 2] = _words(at)
+        if types != self._grads_types:
+            self._grads_types = types
+            self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32)
+        return self._address
+
+
+def _words(x) -> np.ndarray:
+    """A list of whole numbers as int64 (numpy takes three times as long)."""
+    return np.frombuffer(array.array("q", x), dtype=np.int64)
 
 
 def _gradients(grads, device):
@@ -712,13 +722,15 @@ def pacer_grad_norm(grads) -> torch.Tensor:
     if not grads:
         raise AssertionError("grads: at least one")
     dev, n = grads[0].device, len(grads)
-    table = np.empty((n, 3), dtype=np.int64)                                     # pacer_gradient
-    table[:, 2], table[:, 0] = _gradients(grads, dev)
-    table[:, 1] = list(map(torch.Tensor.numel, grads))
+    types, at = _gradients(grads, dev)
+    rows = array.array("q", bytes(24 * n))                                       # pacer_gradient: address, size, type
+    rows[0::3], rows[1::3] = array.array("q", at), array.array("q", map(torch.Tensor.numel, grads))
+    rows[2::3] = array.array("q", types if isinstance(types, list) else (types,) * n)
     nbytes = _lib.pacer_grad_norm_scratch_bytes(n)
     buf = torch.empty(nbytes // 4 + 2, dtype=torch.float32, device=dev)          # the result, then the scratch
-    _call(_lib.pacer_grad_norm, buf, table.ctypes.data, n, buf.data_ptr(), buf.data_ptr() + 8, nbytes)
-    return buf[0]
+    out = buf.data_ptr()
+    _call(_lib.pacer_grad_norm, buf, rows.buffer_info()[0], n, out, out + 8, nbytes)
+    return buf.select(0, 0)
 
 
 def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, seed=None, norm=None,
@@ -741,7 +753,7 @@ def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps:
     if norm is not None:
         assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == tensors.device, f"norm: one torch.float32 on {tensors.device}"
         cfg.norm = norm.data_ptr()
-    _call(_lib.pacer_adamw, tensors, table.ctypes.data, len(table), C.byref(cfg))
+    _call(_lib.pacer_adamw, tensors, table, len(tensors.numel), C.byref(cfg))
     _written(*tensors.all)
 
 
@@ -760,7 +772,7 @@ def pacer_adamw_states(tensors: AdamwTensors, out=None):
     if len(tensors.numel):
         tensors._place()
         m, v = (np.array([t.data_ptr() for t in x], dtype=np.int64) for x in out)
-        _call(_lib.pacer_adamw_states, tensors, tensors.table.ctypes.data, len(m), m.ctypes.data, v.ctypes.data)
+        _call(_lib.pacer_adamw_states, tensors, tensors._address, len(m), m.ctypes.data, v.ctypes.data)
         _written(*out[0], *out[1])
     return out
 

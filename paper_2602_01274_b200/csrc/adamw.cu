@@ -420,7 +420,7 @@ template <int BITS, int PT, int GT, bool SEEDED, int CAP> static cudaError_t lau
 }
 constexpr int MOST = 480;                  // tensors a launch: 32 KB of arguments
 template <int BITS, int PT, int GT, bool SEEDED> static cudaError_t launch_sized(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
-    return n <= 32 ? launch<BITS, PT, GT, SEEDED, 32>(tbl, at, n, h, st) : launch<BITS, PT, GT, SEEDED, MOST>(tbl, at, n, h, st);
+    return n <= 16 ? launch<BITS, PT, GT, SEEDED, 16>(tbl, at, n, h, st) : n <= 224 ? launch<BITS, PT, GT, SEEDED, 224>(tbl, at, n, h, st) : launch<BITS, PT, GT, SEEDED, MOST>(tbl, at, n, h, st);
 }
 template <int BITS, int PT, int GT> static cudaError_t launch_some(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
     if (h.seeded && (BITS == 8 || PT == PACER_BF16)) return launch_sized<BITS, PT, GT, BITS == 8 || PT == PACER_BF16>(tbl, at, n, h, st);

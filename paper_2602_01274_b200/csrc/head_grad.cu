@@ -21,8 +21,15 @@ using namespace fwd;
 using namespace pr;
 
 constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's half of a tile, columns of a tile; 64 rows x 64 columns
-constexpr int STAGE = 4 * PANEL, STAGES = 6, OUT = 32 * 128;
-constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT;
+#ifndef NST
+#define NST 5
+#define NOUT 2
+#endif
+#ifndef XTRA
+#define XTRA 4
+#endif
+constexpr int STAGE = 4 * PANEL, STAGES = NST, OUT = 32 * 128, OUTS = NOUT;
+constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT * OUTS;
 constexpr size_t MOST_DZ = (size_t)2 << 30;               // bytes of dz (without remainders) that are kept at a time
 constexpr int FEW = 128;                                  // rows up to which dz comes with its rounding remainders
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -309,7 +316,8 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;
-        unsigned char *out = smem + STAGES * STAGE + warp * OUT;
+        unsigned char *outs = smem + STAGES * STAGE + warp * OUT * OUTS;
+        int stored = 0;
         bool ok = true;
         for (int j = 0; item_of(a, worker, workers, j, it); ++j) {
             if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u);
@@ -342,7 +350,8 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                     }
                     continue;
                 }
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (the last tile's copy has left)
+                unsigned char *out = outs + (stored++ % OUTS) * OUT;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(OUTS - 1) : "memory");   // (its last copy has left)
                 __syncwarp();
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
@@ -402,7 +411,7 @@ struct Plan {
 static int up(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
 // A unit of time is a k block of a tile, 512 cycles.  A tile's epilogue and start count as four.
-constexpr int EXTRA = 4;
+constexpr int EXTRA = XTRA;
 static Plan plan_of(int rows, int vocab, int d, bool to_hidden, bool to_head, int n_sm) {
     Plan p;
     const int64_t most = std::max<int64_t>(256, (int64_t)(MOST_DZ / 2 / (size_t)rows) / 256 * 256);

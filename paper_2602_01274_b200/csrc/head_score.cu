@@ -29,7 +29,10 @@ constexpr int TM = 128, TN = 256, A_BYTES = TM * 128;
 template <bool PAIR> struct Cfg {
     static constexpr int B_BYTES = (PAIR ? TN / 2 : TN) * 128, STAGE = A_BYTES + B_BYTES, STAGES = PAIR ? 6 : 4;
 };
-constexpr int SEG = 8;                     // k blocks of 64 columns accumulated inside the tensor cores
+#ifndef SEGK
+#define SEGK 16
+#endif
+constexpr int SEG_SCORE = 8, SEG_KEEP = SEGK;   // k blocks of 64 columns accumulated inside the tensor cores
 constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = 192 * 1024 + 1024;
 static_assert(Cfg<true>::STAGE * Cfg<true>::STAGES == 192 * 1024 && Cfg<false>::STAGE * Cfg<false>::STAGES == 192 * 1024, "the stages");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -73,7 +76,7 @@ template <bool PAIR, bool KEEP>
 __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                              const KArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    constexpr int STAGES = Cfg<PAIR>::STAGES, STAGE = Cfg<PAIR>::STAGE;
+    constexpr int STAGES = Cfg<PAIR>::STAGES, STAGE = Cfg<PAIR>::STAGE, SEG = KEEP ? SEG_KEEP : SEG_SCORE;
     __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int32_t gave_up;
@@ -313,7 +316,14 @@ __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzAr
     __shared__ Part red[THREADS_D / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int row = blockIdx.x / g.segs, at = (blockIdx.x - row * g.segs) * g.seg, lane = threadIdx.x & 31;
+    const int row = blockIdx.x / g.segs, at = (blockIdx.x - row * g.segs) * g.seg, lane = threadIdx.x & 31, end = min(at + g.seg, a.vocab);
+    uint4 *z = reinterpret_cast<uint4 *>(a.keep + (size_t)row * a.ld_keep), *low = reinterpret_cast<uint4 *>(g.low ? g.low + (size_t)row * a.ld_keep : nullptr);
+    constexpr int STEP = THREADS_D * 8;
+    int c = at + threadIdx.x * 8;
+    uint4 v[4] = {};                       // (on their way while the parts are joined)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (c + k * STEP < end) v[k] = z[(c + k * STEP) >> 3];
     const float4 *p = reinterpret_cast<const float4 *>(a.part) + (size_t)row * (2 * a.nt);
     float m = NO_REF, S = 0.f;
     for (int i = threadIdx.x; i < 2 * a.nt; i += THREADS_D) {
@@ -344,8 +354,7 @@ __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzAr
     S = others + mine;
     const float l2 = log2f(S), of_token = -weight * (others / S);
     if (at == 0 && threadIdx.x == 0 && g.loss) g.loss[row] = tok < 0 ? 0.f : zt == m ? log1pf(others) : (m - zt) + l2 * LN2;
-    const int end = min(at + g.seg, a.vocab), chunks = a.bn >> 5, first = (chunks + 1) >> 1;   // (32-token chunks of a tile's first half)
-    uint4 *z = reinterpret_cast<uint4 *>(a.keep + (size_t)row * a.ld_keep), *low = reinterpret_cast<uint4 *>(g.low ? g.low + (size_t)row * a.ld_keep : nullptr);
+    const int chunks = a.bn >> 5, first = (chunks + 1) >> 1;           // (32-token chunks of a tile's first half)
     const auto scaled = [&](int c, uint4 v) {
         const int tile = c / a.bn, half = (c - tile * a.bn) >> 5 >= first;
         const float t = (p[2 * tile + half].x - m) * LOG2E - l2, f = t < FAR ? 0.f : weight * ex2(t);      // (NaN stays)
@@ -365,16 +374,15 @@ __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzAr
         z[c >> 3] = make_uint4(o[0], o[1], o[2], o[3]);
         if (low) low[c >> 3] = make_uint4(r[0], r[1], r[2], r[3]);
     };
-    constexpr int STEP = THREADS_D * 8;
-    int c = at + threadIdx.x * 8;
-    for (; c + 3 * STEP < end; c += 4 * STEP) {
-        uint4 v[4];
+    while (c < end) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = z[(c + k * STEP) >> 3];
+        for (int k = 0; k < 4; ++k)
+            if (c + k * STEP < end) scaled(c + k * STEP, v[k]);
+        c += 4 * STEP;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) scaled(c + k * STEP, v[k]);
+        for (int k = 0; k < 4; ++k)
+            if (c + k * STEP < end) v[k] = z[(c + k * STEP) >> 3];
     }
-    for (; c < end; c += STEP) scaled(c, z[c >> 3]);
 }
 
 // Tokens of a tile: the width with the least waves x (width + 16).  The 16 stands for a tile's start and end: without it many rows would
