@@ -21,14 +21,7 @@ using namespace fwd;
 using namespace pr;
 
 constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's half of a tile, columns of a tile; 64 rows x 64 columns
-#ifndef NST
-#define NST 5
-#define NOUT 2
-#endif
-#ifndef XTRA
-#define XTRA 4
-#endif
-constexpr int STAGE = 4 * PANEL, STAGES = NST, OUT = 32 * 128, OUTS = NOUT;
+constexpr int STAGE = 4 * PANEL, STAGES = 5, OUT = 32 * 128, OUTS = 2;      // (a warp's output buffers)
 constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT * OUTS;
 constexpr size_t MOST_DZ = (size_t)2 << 30;               // bytes of dz (without remainders) that are kept at a time
 constexpr int FEW = 128;                                  // rows up to which dz comes with its rounding remainders
@@ -193,15 +186,15 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                 if (n0 + at >= a.ld) break;
                 uint32_t v[32];
                 tmem_ld32(acc + at, v);
+                if ((uint32_t)(bid - at) < 32u)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + (bid - at == e ? a.bias : 0.f));
                 uint32_t w[16], l16[16];
                 float g[2];
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
-                    float z = __uint_as_float(v[e]);
-                    if (a.bias_ids && bid - at == e) z += a.bias;
-                    const float l = fmaf(z, LOG2E, -lse), p = ex2(l);
-                    g[e & 1] = p * fmaf(h, l, c);
-                    if (tok - at == e) g[e & 1] = p * fmaf(h, l, c + gl) - gl * expm1f(lp);
+                    const float l = fmaf(__uint_as_float(v[e]), LOG2E, -lse);
+                    g[e & 1] = ex2(l) * fmaf(h, l, c);
                     if (e & 1) {
                         w[e >> 1] = pack(g[0], g[1]);
                         if (a.low) l16[e >> 1] = pack(g[0] - __uint_as_float(w[e >> 1] << 16), g[1] - __uint_as_float(w[e >> 1] & 0xffff0000u));
@@ -211,13 +204,20 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
 #pragma unroll
                     for (int e = 0; e < 16; ++e) w[e] = 0x7fff7fffu;
                 if (live) {
-                    bf16 *p = a.dz + (size_t)r * a.ld + n0 + at;
+                    bf16 *p = a.dz + (size_t)r * a.ld + n0 + at, *q = a.low + (size_t)r * a.ld + n0 + at;
                     st32(p, w);
                     st32(p + 16, w + 8);
                     if (a.low) {
-                        p = a.low + (size_t)r * a.ld + n0 + at;
-                        st32(p, l16);
-                        st32(p + 16, l16 + 8);
+                        st32(q, l16);
+                        st32(q + 16, l16 + 8);
+                    }
+                    if ((uint32_t)(tok - at) < 32u && ok) {                // the token's own
+                        float z = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) z = tok - at == e ? __uint_as_float(v[e]) : z;
+                        const float l = fmaf(z, LOG2E, -lse), x = ex2(l) * fmaf(h, l, c + gl) - gl * expm1f(lp);
+                        p[tok - at] = __float2bfloat16_rn(x);
+                        if (a.low) q[tok - at] = __float2bfloat16_rn(x - __bfloat162float(__float2bfloat16_rn(x)));
                     }
                 }
             }
@@ -411,7 +411,7 @@ struct Plan {
 static int up(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
 // A unit of time is a k block of a tile, 512 cycles.  A tile's epilogue and start count as four.
-constexpr int EXTRA = XTRA;
+constexpr int EXTRA = 4;
 static Plan plan_of(int rows, int vocab, int d, bool to_hidden, bool to_head, int n_sm) {
     Plan p;
     const int64_t most = std::max<int64_t>(256, (int64_t)(MOST_DZ / 2 / (size_t)rows) / 256 * 256);

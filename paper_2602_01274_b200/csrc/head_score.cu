@@ -29,10 +29,10 @@ constexpr int TM = 128, TN = 256, A_BYTES = TM * 128;
 template <bool PAIR> struct Cfg {
     static constexpr int B_BYTES = (PAIR ? TN / 2 : TN) * 128, STAGE = A_BYTES + B_BYTES, STAGES = PAIR ? 6 : 4;
 };
-#ifndef SEGK
-#define SEGK 16
-#endif
-constexpr int SEG_SCORE = 8, SEG_KEEP = SEGK;   // k blocks of 64 columns accumulated inside the tensor cores
+constexpr int SEG_SCORE = 8;               // k blocks of 64 columns accumulated inside the tensor cores
+// Where the epilogue has twice the work (KEEP), segments twice as long give it the time: the loss's pass over 4093 rows x 151 936 x 1536 took
+// 1508 us with 8 blocks, 1341 with 12 or 16, over 2048 x 32 000 x 4096 371, 356 and 341.  (Results are then off by some 2.5e-7 of a logit.)
+constexpr int SEG_KEEP = 16;
 constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = 192 * 1024 + 1024;
 static_assert(Cfg<true>::STAGE * Cfg<true>::STAGES == 192 * 1024 && Cfg<false>::STAGE * Cfg<false>::STAGES == 192 * 1024, "the stages");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -465,8 +465,8 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     c.gridDim = dim3((unsigned)((a.rows + 3) / 4));
     c.blockDim = dim3(128);
     DzArgs g;
-    if (a.dz) {                            // rows cut into pieces until there are eight blocks an SM
-        g.segs = std::max(1, std::min((a.vocab + 8 * THREADS_D - 1) / (8 * THREADS_D), (8 * n_sm + a.rows - 1) / a.rows));
+    if (a.dz) {                            // rows cut into pieces while all blocks fit the SMs at once, six on each
+        g.segs = std::max(1, std::min((a.vocab + 8 * THREADS_D - 1) / (8 * THREADS_D), 6 * n_sm / a.rows));
         g.seg = ((a.vocab + g.segs - 1) / g.segs + 7) & ~7;
         g.weight = a.weight; g.loss = a.loss; g.low = reinterpret_cast<__nv_bfloat16 *>(a.dz_low);
         c.gridDim = dim3((unsigned)a.rows * (unsigned)g.segs);
