@@ -6,7 +6,8 @@ Sub-modules:
            Holds no arithmetic of the method; importing it loads no native code.
   binding  thin ctypes binding of the C-ABI library ``libpacer.so``; importing
            it fails loudly when the CUDA library has not been built.
-  losses   differentiable forms of the library's operators on rows of logits.
+  losses   differentiable forms of the library's operators on rows of logits and on the LM head.
+  optim    AdamW whose step over many tensors is one launch of the library.
   train_preverify, train_draft
            commands that train the pre-verification layer and the draft's LM head.
 
@@ -14,4 +15,4 @@ Nothing is imported eagerly, so the input generators can be used on a machine
 that has no GPU and no built library.
 """
 
-__all__ = ["synth", "binding", "losses", "train_preverify", "train_draft"]
+__all__ = ["synth", "binding", "losses", "optim", "train_preverify", "train_draft"]

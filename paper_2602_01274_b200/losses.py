@@ -4,6 +4,9 @@ Every function takes logits [..., vocab] (f32, bf16 or f16, on the GPU) and runs
 (``binding.pacer_logprobs``, ``binding.pacer_distill``); gradients come in the logits' type.  A second derivative is not
 defined.  What a training step needs of loss and gradient in one pass, with the gradient written over the logits if
 wanted, is ``binding.pacer_distill_grad``.
+
+``head_logprobs`` and ``head_nll`` take hidden rows [..., d] and the LM head [vocab, d] (bf16) instead, and never write the logits:
+``head_nll`` computes the gradients in its forward pass, together with the loss.
 """
 from __future__ import annotations
 
@@ -72,3 +75,61 @@ def distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor,
     loss = _Distill.apply(logits.reshape(-1, logits.shape[-1]), ids.reshape(-1, k), teacher.detach().reshape(-1, k),
                           None if teacher_lse is None else teacher_lse.detach().reshape(-1), temperature)
     return loss.view(lead)
+
+
+class _HeadLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, head, tokens, bias_ids, bias):
+        # (clones: logp may be changed in place where the three are views of one allocation)
+        logp, entropy, lse = (x.clone() for x in binding.pacer_head_logprobs(hidden, head, tokens, bias_ids, bias))
+        ctx.save_for_backward(hidden, head, tokens, bias_ids, logp, entropy, lse)
+        ctx.bias = bias
+        ctx.set_materialize_grads(False)
+        return logp, entropy, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g_logp, g_entropy, g_lse):
+        if g_logp is None and g_entropy is None and g_lse is None:
+            return (None,) * 5
+        hidden, head, tokens, bias_ids, logp, entropy, lse = ctx.saved_tensors
+        return (*binding.pacer_head_logprobs_backward(hidden, head, tokens, logp, lse, entropy, g_logp, g_entropy, g_lse, bias_ids, ctx.bias,
+                                                      grads=ctx.needs_input_grad[:2]), None, None, None)
+
+
+def _flat_rows(hidden, tokens, bias_ids):
+    shape = tokens.shape
+    assert hidden.shape[:-1] == shape and (bias_ids is None or bias_ids.shape == shape), "tokens and bias_ids: the hidden rows' leading shape"
+    return hidden.reshape(-1, hidden.shape[-1]), tokens.reshape(-1), None if bias_ids is None else bias_ids.reshape(-1)
+
+
+def head_logprobs(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, bias_ids: Optional[torch.Tensor] = None, bias: float = 0.0):
+    """(logp, entropy, lse) [...] of int32 tokens [...] under hidden @ head.T (see ``binding.pacer_head_logprobs``), differentiable in
+    hidden and head; the logits are computed again in the backward pass.  A token outside the vocabulary has logp 0 and passes
+    no gradient.  All three outputs are kept for the backward pass."""
+    h, t, i = _flat_rows(hidden, tokens, bias_ids)
+    return tuple(x.view(tokens.shape) for x in _HeadLogprobs.apply(h, head, t, i, bias))
+
+
+class _HeadNll(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, head, tokens, weight, bias_ids, bias):
+        loss, dhidden, dhead = binding.pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids, bias, grads=ctx.needs_input_grad[:2])
+        ctx.grads = dhidden, dhead, loss if ctx.needs_input_grad[3] else None
+        return (loss * weight).sum()
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g):
+        dhidden, dhead, loss = (None if x is None else x * g for x in ctx.grads)
+        return dhidden, dhead, None, loss, None, None
+
+
+def head_nll(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, weight: torch.Tensor, bias_ids: Optional[torch.Tensor] = None,
+             bias: float = 0.0) -> torch.Tensor:
+    """sum(weight * negative log-likelihood) of int32 tokens [...] under hidden @ head.T, weight f32 [...]: a scalar, whose gradients the forward
+    pass computes (``binding.pacer_head_nll_grad``); the backward pass multiplies them by the incoming scalar, which rounds them once more
+    unless it is a power of 2.  A token outside the vocabulary (-1: padding) adds nothing."""
+    h, t, i = _flat_rows(hidden, tokens, bias_ids)
+    assert weight.shape == tokens.shape, "weight: the hidden rows' leading shape"
+    return _HeadNll.apply(h, head, t, weight.reshape(-1), i, bias)

@@ -5,7 +5,9 @@ towards its target.  The target generates greedy responses to seeded random prom
 logits (``pacer_logprobs``) are the teacher's list, with all other tokens as one further class; the draft's LM head is
 trained on KL(target || draft) over the frozen draft's hidden states (``losses.distill_loss``, AdamW).  The held-out
 negative log-likelihood of the target's tokens under the draft is taken before and after, straight from hidden states
-and head (``pacer_head_logprobs``).
+and head (``pacer_head_logprobs``).  With ``--objective nll`` the head is trained on that likelihood itself, loss and
+gradient straight from hidden states and head (``losses.head_nll``), as a bf16 tensor with an f32 master; ``--optimizer f32`` or ``8bit``
+takes the library's AdamW (``optim.AdamW``), which the objective needs.
 
 Like ``train_preverify`` this is a small PyTorch job outside the decoding path; it needs a GPU (the operators have no
 CPU form).  It produces a bf16 ``head`` for ``pacer_load_weights(PACER_DRAFT, ...)``.
@@ -19,7 +21,7 @@ import time
 
 import torch
 
-from . import binding, losses, synth
+from . import binding, losses, optim, synth
 from .train_preverify import Decoder
 
 
@@ -62,6 +64,11 @@ def draft_loss(head, d, bias, temperature=1.0):
     return losses.distill_loss(logits, d["ids"], d["teacher"], temperature, whole).mean()
 
 
+def draft_nll(head, d, bias):
+    """Mean negative log-likelihood of the target's tokens under the draft's head, bf16 [V][d], differentiable in it."""
+    return losses.head_nll(d["hidden"], head, d["next"], torch.full_like(d["teacher"][:, 0], 1.0 / len(d["next"])), d["planted"], bias)
+
+
 def held_out_nll(head, d, bias):
     """Mean negative log-likelihood of the target's tokens under the draft."""
     logp, _, _ = binding.pacer_head_logprobs(d["hidden"], head.to(torch.bfloat16), d["next"], d["planted"], bias)
@@ -69,27 +76,36 @@ def held_out_nll(head, d, bias):
 
 
 def train(cfg: synth.PairConfig, pair, device="cuda:0", n_prompts=64, n_prompt_tokens=32, n_resp=64, epochs=4, lr=1e-3, top=32,
-          batch_prompts=8, temperature=1.0, seed=0, log=print, prompt_seed=5000):
-    """Returns ({"head": bf16 [V][d]}, report dict).  `pair` holds the target and draft tensors on `device`."""
+          batch_prompts=8, temperature=1.0, seed=0, log=print, prompt_seed=5000, objective="kl", optimizer="torch"):
+    """Returns ({"head": bf16 [V][d]}, report dict).  `pair` holds the target and draft tensors on `device`.  objective: "kl" or "nll";
+    optimizer: "torch", "f32" or "8bit" (the library's AdamW with such states)."""
+    if objective not in ("kl", "nll") or optimizer not in ("torch", "f32", "8bit"):
+        raise ValueError("objective: 'kl' or 'nll'; optimizer: 'torch', 'f32' or '8bit'")
+    if objective == "nll" and optimizer == "torch":
+        raise ValueError("objective 'nll' trains a bf16 head with an f32 master: optimizer 'f32' or '8bit'")
     t0 = time.time()
     data = [make_examples(cfg, pair, synth.make_prompts(cfg.target.vocab, batch_prompts, n_prompt_tokens, seed=prompt_seed + i).to(device).long(),
                           n_resp, top) for i in range(0, n_prompts + batch_prompts, batch_prompts)]
     held = data.pop()                                               # the last batch is held out
-    head = pair["draft"]["head"].detach().float().clone().requires_grad_(True)
+    head = pair["draft"]["head"].detach().to(torch.float32 if objective == "kl" else torch.bfloat16, copy=True).requires_grad_(True)
     rep = {"held_out_nll_before": held_out_nll(head.detach(), held, cfg.succ_bias)}
-    opt = torch.optim.AdamW([head], lr=lr, betas=(0.9, 0.999), weight_decay=0.0)
+    if optimizer == "torch":
+        opt = torch.optim.AdamW([head], lr=lr, betas=(0.9, 0.999), weight_decay=0.0)
+    else:
+        opt = optim.AdamW([head], lr=lr, betas=(0.9, 0.999), weight_decay=0.0, states=optimizer, seed=seed if optimizer == "8bit" else None)
     for ep in range(epochs):
         total = 0.0
         for i in torch.randperm(len(data), generator=torch.Generator().manual_seed(seed + ep)).tolist():
-            loss = draft_loss(head, data[i], cfg.succ_bias, temperature)
+            loss = draft_loss(head, data[i], cfg.succ_bias, temperature) if objective == "kl" else draft_nll(head, data[i], cfg.succ_bias)
             opt.zero_grad(set_to_none=True)
             loss.backward()
             opt.step()
             total += float(loss.detach())
-        log(f"[train_draft] epoch {ep + 1}/{epochs}: KL {total / len(data):.4f}")
+        log(f"[train_draft] epoch {ep + 1}/{epochs}: {objective.upper()} {total / len(data):.4f}")
     with torch.no_grad():
         rep.update(held_out_nll_after=held_out_nll(head, held, cfg.succ_bias), held_out_kl=float(draft_loss(head, held, cfg.succ_bias)),
-                   prompts=n_prompts, response_tokens=n_resp, epochs=epochs, lr=lr, top=top, seconds=time.time() - t0)
+                   prompts=n_prompts, response_tokens=n_resp, epochs=epochs, lr=lr, top=top, objective=objective, optimizer=optimizer,
+                   seconds=time.time() - t0)
     log(f"[train_draft] held-out NLL {rep['held_out_nll_before']:.3f} -> {rep['held_out_nll_after']:.3f}")
     return {"head": head.detach().to(torch.bfloat16).contiguous()}, rep
 
@@ -106,11 +122,13 @@ def main():
     ap.add_argument("--lr", type=float, default=1e-3)
     ap.add_argument("--top", type=int, default=32)
     ap.add_argument("--batch-prompts", type=int, default=8)
+    ap.add_argument("--objective", choices=("kl", "nll"), default="kl")
+    ap.add_argument("--optimizer", choices=("torch", "f32", "8bit"), default=None, help="default: torch, with --objective nll f32")
     args = ap.parse_args()
     cfg = synth.CONFIGS[args.config]
     pair = synth.make_pair(cfg, seed=0, device=args.device, which=("target", "draft"))
     w, rep = train(cfg, pair, args.device, args.prompts, args.prompt_tokens, args.response_tokens, args.epochs, args.lr, args.top,
-                   args.batch_prompts)
+                   args.batch_prompts, objective=args.objective, optimizer=args.optimizer or ("torch" if args.objective == "kl" else "f32"))
     torch.save({"tensors": {k: v.cpu() for k, v in w.items()}, "report": rep, "config": args.config}, args.out)
     print(rep)
 

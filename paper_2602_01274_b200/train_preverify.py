@@ -257,8 +257,11 @@ def auc(score, label):
 
 
 def train(cfg: synth.PairConfig, pair, device="cpu", n_prompts=64, n_prompt_tokens=32, n_resp=96, epochs=5, lr=5e-4,
-          batch_prompts=8, prefix_stride=1, seed=0, dtype=None, log=print, prompt_seed=1000):
-    """Returns (bf16 tensors of the trained M_B, report dict).  `pair` holds the target and draft tensors on `device`."""
+          batch_prompts=8, prefix_stride=1, seed=0, dtype=None, log=print, prompt_seed=1000, optimizer="torch"):
+    """Returns (bf16 tensors of the trained M_B, report dict).  `pair` holds the target and draft tensors on `device`.  optimizer: "torch", or
+    on a GPU "f32" or "8bit" (the library's AdamW with such states, one launch a step)."""
+    if optimizer not in ("torch", "f32", "8bit"):
+        raise ValueError("optimizer: 'torch', 'f32' or '8bit'")
     dtype = dtype or (torch.bfloat16 if str(device).startswith("cuda") else torch.float32)
     gamma = cfg.gamma_cap
     t0 = time.time()
@@ -272,7 +275,11 @@ def train(cfg: synth.PairConfig, pair, device="cpu", n_prompts=64, n_prompt_toke
         f"share of accepted labels {base:.3f}")
     torch.manual_seed(seed)
     mb = PreVerify(cfg.draft, gamma, seed).to(device)
-    opt = torch.optim.AdamW(mb.parameters(), lr=lr, betas=(0.9, 0.999))
+    if optimizer == "torch":
+        opt = torch.optim.AdamW(mb.parameters(), lr=lr, betas=(0.9, 0.999))
+    else:
+        from . import optim                                           # (it needs the library, this module does not)
+        opt = optim.AdamW(mb.parameters(), lr=lr, betas=(0.9, 0.999), states=optimizer, seed=seed if optimizer == "8bit" else None)
     steps = epochs * len(data)
     sched = torch.optim.lr_scheduler.OneCycleLR(opt, max_lr=lr, total_steps=max(steps, 2), pct_start=0.1)
     for ep in range(epochs):
@@ -312,11 +319,12 @@ def main():
     ap.add_argument("--epochs", type=int, default=5)
     ap.add_argument("--lr", type=float, default=5e-4)
     ap.add_argument("--batch-prompts", type=int, default=8)
+    ap.add_argument("--optimizer", choices=("torch", "f32", "8bit"), default="torch")
     args = ap.parse_args()
     cfg = synth.CONFIGS[args.config]
     pair = synth.make_pair(cfg, seed=0, device=args.device, which=("target", "draft"))
     w, rep = train(cfg, pair, args.device, args.prompts, args.prompt_tokens, args.response_tokens, args.epochs, args.lr,
-                   batch_prompts=args.batch_prompts)
+                   batch_prompts=args.batch_prompts, optimizer=args.optimizer)
     torch.save({"tensors": {k: v.cpu() for k, v in w.items()}, "report": rep, "config": args.config}, args.out)
     print(rep)
 
