@@ -12,6 +12,7 @@
 #include "head_grad.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pair.cuh"
 
@@ -37,10 +38,16 @@ struct ZArgs {
 
 struct PArgs {
     int32_t rows, width, d, dp, bn, nt;        // nt: tiles of d
+    uint32_t by_nt;                            // 2^32 / nt, rounded up (exact quotients below 2^32 / nt)
     int32_t mt_w, mt_h, k_w, k_h, per, splits; // tiles of tokens and rows; k blocks of 64 of each product (of all planes), of a share of dhidden's
     int32_t n_h, n_w, early;                   // items of dhidden and dhead, dhead's that the less loaded workers take first
     int32_t add;                               // dhidden's sums are added to those that are there
     int32_t planes;                            // 2: dz and its remainders (at most 128 rows)
+    // dhead by the threads' own stores, 32 bytes each, instead of copies out of shared memory: where a tile has more than a few k blocks they
+    // run under the next tile's products and cost less (33 rows, 2 blocks: 32 us, by copies 26; 512 rows, 8: 26.1, 27.8; 2048, 32: 671, 679)
+    int32_t direct;
+    bf16 *dhead;
+    int64_t ld_dhead;
     float *part;                               // [planes][splits][rows][dp], or NULL: dhidden is written
 };
 
@@ -92,10 +99,10 @@ __device__ __forceinline__ uint32_t pair_idesc(int n) { return (umma_idesc(n) & 
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(PANEL >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void release_acc(Pair &s, int i, int lane) {   // the next products may overwrite the accumulator
+__device__ __forceinline__ void release_acc(Pair &s, int i, int lane) {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(s.acc_empty + (i & 1))) : "memory");
+    if (lane == 0) acc_release(s.acc_empty + (i & 1));
 }
 __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -113,27 +120,23 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
     const uint32_t tmem = pair_begin(s, warp);
 
     if (warp == 8) {
-        if (lane == 0) {
-            uint64_t keep, stream;
-            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
-            asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(stream));
-            int n = 0;
-            bool ok = true;
-            for (int t = worker; t < tiles && ok; t += workers) {
-                const int r0 = (t % a.mt) * (2 * TM) + rank * TM, n0 = (t / a.mt) * a.bn + rank * (a.bn >> 1);
-                for (int kb = 0; kb < a.nkb; ++kb, ++n) {
-                    const int slot = n % STAGES;
-                    ok = wait_h(&s.gave_up, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
-                    if (!ok) break;
-                    unsigned char *st = smem + slot * STAGE;
-                    if (rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
-                    const uint32_t bar = first_block(s.full + slot);
-                    tma_2d<true>(st, &map_a, kb * 64, r0, bar, keep);
-                    tma_2d<true>(st + 2 * PANEL, &map_b, kb * 64, n0, bar, stream);
-                }
+        uint64_t policy;                                               // lane 0 hidden rows, lane 1 the head
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+        if (lane == 0) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+        const uint32_t full0 = first_block(s.full);
+        int n = 0;
+        bool ok = true;
+        for (int t = worker; t < tiles && ok; t += workers) {
+            const int y = lane ? (t / a.mt) * a.bn + rank * (a.bn >> 1) : (t % a.mt) * (2 * TM) + rank * TM;
+            for (int kb = 0; kb < a.nkb; ++kb, ++n) {
+                const int slot = n % STAGES;
+                ok = all_wait(s, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
+                if (!ok) break;
+                if (lane == 0 && rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
+                if (lane < 2) tma_2d<true>(smem + slot * STAGE + lane * 2 * PANEL, lane ? &map_b : &map_a, kb * 64, y, full0 + slot * 8, policy);
             }
-            drain(s, n, rank);
         }
+        if (lane == 0) drain(s, n, rank);
     } else if (warp == 9) {
         const uint32_t on = elect_lane(), idesc = pair_idesc(a.bn);        // (all lanes wait, one of the first block issues)
         int n = 0, i = 0;
@@ -230,24 +233,40 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
 // ----------------------------------------------------------------------------- the products
 
 struct Item { int32_t to_head, m0, n0, k0, k1, split; };
-// The j-th item of a worker; false: there is none.  dhidden's long ones are dealt out first; where they do not come out even, the workers
-// with one less take `early` rounds of dhead's before the others join.
-__device__ __forceinline__ bool item_of(const PArgs &a, int worker, int workers, int j, Item &it) {
-    const int rem = a.n_h % workers, mine = a.n_h / workers + (worker < rem);
-    if (j < mine) {
-        const int t = worker + j * workers, n = t % a.nt, q = t / a.nt, m = q % a.mt_h;
-        it.split = q / a.mt_h;
-        it.to_head = 0; it.m0 = m * 2 * TM; it.n0 = n * a.bn; it.k0 = it.split * a.per; it.k1 = min(a.k_h, it.k0 + a.per);
+// A worker's items one after another.  dhidden's long ones are dealt out first; where they do not come out even, the workers with one less take
+// `early` rounds of dhead's before the others join.
+struct Walk {
+    int t, left, next, early, less, workers, base;
+    __device__ __forceinline__ Walk(const PArgs &a, int worker, int n_workers) {
+        workers = n_workers;
+        const int rem = a.n_h % workers;
+        left = a.n_h / workers + (worker < rem);
+        t = worker;
+        const bool fewer = rem && worker >= rem;
+        less = workers - rem;
+        early = fewer ? a.early : 0;
+        base = rem ? a.early * less : 0;       // dhead's first tile that all workers take part in
+        next = fewer ? worker - rem : base + worker;
+        if (fewer && !early) next = base + worker;
+        base += worker;
+    }
+    __device__ __forceinline__ bool operator()(const PArgs &a, Item &it) {
+        if (left) {
+            --left;
+            const int n = t % a.nt, q = t / a.nt, m = q % a.mt_h;
+            it.split = q / a.mt_h;
+            it.to_head = 0; it.m0 = m * 2 * TM; it.n0 = n * a.bn; it.k0 = it.split * a.per; it.k1 = min(a.k_h, it.k0 + a.per);
+            t += workers;
+            return true;
+        }
+        if (next >= a.n_w) return false;
+        const int m = a.nt > 1 ? (int)__umulhi((uint32_t)next, a.by_nt) : next;       // next / nt
+        it.to_head = 1; it.m0 = m * 2 * TM; it.n0 = (next - m * a.nt) * a.bn; it.k0 = 0; it.k1 = a.k_w; it.split = 0;
+        if (early && --early == 0) next = base;
+        else next += early ? less : workers;
         return true;
     }
-    int k = j - mine, t;
-    const int less = rem ? workers - rem : 0, e = rem ? a.early : 0;
-    if (rem && worker >= rem) t = k < e ? k * less + worker - rem : e * less + (k - e) * workers + worker;
-    else t = e * less + k * workers + worker;
-    if (t >= a.n_w) return false;
-    it.to_head = 1; it.m0 = t / a.nt * 2 * TM; it.n0 = t % a.nt * a.bn; it.k0 = 0; it.k1 = a.k_w; it.split = 0;
-    return true;
-}
+};
 
 // dhead tiles: A = dz by its columns (MN-major), B = hidden (MN-major), k = rows.  dhidden tiles: A = dz (K-major), B = head (MN-major),
 // k = tokens.  All tensor copies are 64 x 64: a panel of an MN-major operand, half of a K-major one.
@@ -263,55 +282,65 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
     unsigned char *smem = smem_raw + (-(int)smem_u32(smem_raw) & 1023);
     const int rank = blockIdx.x & 1, worker = blockIdx.x >> 1, workers = gridDim.x >> 1, half_n = a.bn >> 1;
     const uint32_t tmem = pair_begin(s, warp);
+    Walk walk(a, worker, workers);
     Item it;
 
     if (warp == 8) {
-        if (lane == 0) {
-            uint64_t normal;
-            asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
-            int n = 0;
-            bool ok = true;
-            for (int j = 0; ok && item_of(a, worker, workers, j, it); ++j) {
-                const CUtensorMap *mb = it.to_head ? &map_x : &map_w;
-                const int m = it.m0 + (it.to_head || a.planes == 1 ? rank * TM : 0), nb = it.n0 + rank * half_n, k_one = a.k_w / a.planes;
-                for (int kb = it.k0; kb < it.k1; ++kb, ++n) {
-                    const int slot = n % STAGES;
-                    ok = wait_h(&s.gave_up, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
-                    if (!ok) break;
-                    unsigned char *st = smem + slot * STAGE;
-                    if (rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * TM + a.bn) * 128u);
-                    const uint32_t bar = first_block(s.full + slot);
-                    const bool second = it.to_head && kb >= k_one;
-                    const CUtensorMap *ma = second || (!it.to_head && a.planes == 2 && rank) ? &map_low : &map_z;
-                    const int k = (second ? kb - k_one : kb) * 64;
-                    for (int q = 0; q < 2; ++q) tma_2d<true>(st + q * PANEL, ma, it.to_head ? m + q * 64 : k, it.to_head ? k : m + q * 64, bar, normal);
-                    for (int q = 0; q * 64 < half_n; ++q) tma_2d<true>(st + (2 + q) * PANEL, mb, nb + q * 64, k, bar, normal);
-                }
-            }
-            drain(s, n, rank);
-        }
-    } else if (warp == 9) {
-        const uint32_t on = elect_lane(), id_h = pair_idesc(a.bn) | (1u << 16), id_w = id_h | (1u << 15);
+        // lanes 0, 1 the panels of A, lanes 2, 3 those of B, all four by one instruction: by one lane, with the kind looked up per copy, the copies
+        // did not keep up with the products (2048 x 32 000 x 4096: 750 us, with a loop for each kind 706)
+        const int q = lane & 1;
+        const bool copies = lane < 2 || (lane < 4 && q * 64 < half_n);
+        uint64_t normal;
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+        const uint32_t full0 = first_block(s.full);
         int n = 0;
         bool ok = true;
-        for (int j = 0; ok && rank == 0 && item_of(a, worker, workers, j, it); ++j) {
-            ok = all_wait(s, s.acc_empty + (j & 1), (((uint32_t)(j >> 1)) & 1u) ^ 1u);
-            if (!ok) break;
-            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u;
-            for (int kb = it.k0; kb < it.k1; ++kb, ++n) {
+        while (ok && walk(a, it)) {
+            const int m = it.m0 + (it.to_head || a.planes == 1 ? rank * TM : 0) + q * 64, nb = it.n0 + rank * half_n + q * 64;
+            const bool moves = !it.to_head && lane < 2;               // (k along the operand's rows)
+            const int dx = moves ? 64 : 0, dy = 64 - dx, planes = it.to_head ? a.planes : 1, k1 = it.to_head ? a.k_w / a.planes : it.k1;
+            for (int plane = 0; plane < planes && ok; ++plane) {
+                const bool low = it.to_head ? plane : a.planes == 2 && rank;
+                const CUtensorMap *map = lane < 2 ? low ? &map_low : &map_z : it.to_head ? &map_x : &map_w;
+                int x = lane < 2 ? moves ? it.k0 * 64 : m : nb, y = moves ? m : it.k0 * 64;
+                for (int kb = it.k0; kb < k1; ++kb, ++n) {
+                    const int slot = n % STAGES;
+                    ok = all_wait(s, s.empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
+                    if (!ok) break;
+                    if (lane == 0 && rank == 0) mbar_expect_tx(s.full + slot, (uint32_t)(2 * TM + a.bn) * 128u);
+                    if (copies) tma_2d<true>(smem + slot * STAGE + lane * PANEL, map, x, y, full0 + slot * 8, normal);
+                    x += dx;
+                    y += dy;
+                }
+            }
+        }
+        if (lane == 0) drain(s, n, rank);
+    } else if (warp == 9) {
+        const uint32_t on = elect_lane(), idesc = pair_idesc(a.bn) | (1u << 16);
+        int n = 0;
+        bool ok = true;
+        // (a loop for each kind: with the kind looked up per product the descriptors left the uniform registers, 717 -> 759 us in all)
+        const auto multiply = [&](auto kind, uint32_t acc, int blocks) {
+            constexpr bool to_head = decltype(kind)::value;
+            for (int kb = 0; kb < blocks; ++kb, ++n) {
                 const int slot = n % STAGES;
                 ok = all_wait(s, s.full + slot, ((uint32_t)(n / STAGES)) & 1u);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t a0 = smem_u32(smem + slot * STAGE), b0 = a0 + 2 * PANEL;
 #pragma unroll
-                for (int k16 = 0; k16 < 4; ++k16) {
-                    const uint32_t add = kb > it.k0 || k16 > 0 ? 1u : 0u;
-                    const uint64_t da = it.to_head ? desc_mn(a0 + k16 * 2048) : umma_desc(a0 + k16 * 32);
-                    umma2_if(on, acc, da, desc_mn(b0 + k16 * 2048), it.to_head ? id_w : id_h, add);
-                }
+                for (int k16 = 0; k16 < 4; ++k16)
+                    umma2_if(on, acc, to_head ? desc_mn(a0 + k16 * 2048) : umma_desc(a0 + k16 * 32), desc_mn(b0 + k16 * 2048),
+                             to_head ? idesc | (1u << 15) : idesc, kb > 0 || k16 > 0 ? 1u : 0u);
                 umma2_commit_if(on, s.empty + slot);
             }
+        };
+        for (int j = 0; ok && rank == 0 && walk(a, it); ++j) {
+            ok = all_wait(s, s.acc_empty + (j & 1), (((uint32_t)(j >> 1)) & 1u) ^ 1u);
+            if (!ok) break;
+            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u;
+            if (it.to_head) multiply(std::true_type{}, acc, a.k_w);
+            else multiply(std::false_type{}, acc, it.k1 - it.k0);
             if (ok) umma2_commit_if(on, s.acc_full + (j & 1));
         }
     } else {
@@ -319,7 +348,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
         unsigned char *outs = smem + STAGES * STAGE + warp * OUT * OUTS;
         int stored = 0;
         bool ok = true;
-        for (int j = 0; item_of(a, worker, workers, j, it); ++j) {
+        for (int j = 0; walk(a, it); ++j) {
             if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u);
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
@@ -346,6 +375,19 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                                 for (int f = 0; f < 8; ++f) v[e + f] = __float_as_uint(__uint_as_float(v[e + f]) + o[f]);
                             }
                             st32(p + e, v + e);
+                        }
+                    }
+                    continue;
+                }
+                if (it.to_head && a.direct) {
+                    if (m + lane < last) {
+                        bf16 *p = a.dhead + (size_t)(m + lane) * a.ld_dhead + n0 + c;
+#pragma unroll
+                        for (int e = 0; e < 64; e += 16) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int f = 0; f < 8; ++f) w[f] = pack(__uint_as_float(v[e + 2 * f]), __uint_as_float(v[e + 2 * f + 1]));
+                            if (n0 + c + e < a.d) st32(p + e, w);
                         }
                     }
                     continue;
@@ -516,13 +558,15 @@ static cudaError_t products(const Args &a, const Plan &p, EncodeFn encode, int p
     if (!a.dhidden || part) mdx = mw;
     PArgs q;
     q.rows = a.rows; q.width = width; q.d = a.d; q.dp = p.dp; q.bn = p.bn; q.nt = p.nt;
+    q.by_nt = (uint32_t)(((uint64_t)1 << 32) / p.nt + (p.nt & (p.nt - 1) ? 1 : 0));
     q.mt_w = up(width, 2 * TM); q.mt_h = p.mt_h; q.planes = p.planes; q.k_w = up(a.rows, 64) * p.planes; q.k_h = up(width, 64);
     q.splits = p.splits; q.per = up(q.k_h, p.splits);
     q.n_h = a.dhidden ? p.splits * p.mt_h * p.nt : 0;
     q.n_w = dhead ? q.mt_w * p.nt : 0;
     q.early = (q.per + EXTRA) / (q.k_w + EXTRA);
     q.add = piece > 0;
-    q.part = part;
+    q.part = part; q.dhead = dhead; q.ld_dhead = a.ld_dhead;
+    q.direct = q.k_w >= 4 && a.d % 16 == 0 && (((uintptr_t)dhead | (uintptr_t)(a.ld_dhead * 2)) & 31) == 0;
     Launch l((unsigned)std::min<int64_t>(workers, (int64_t)q.n_h + q.n_w) * 2, THREADS_G, SMEM_P, st, true, true);
     cudaError_t e = cudaLaunchKernelEx(&l.c, k_head_prod, mz, ml, mx, mw, mdw, mdx, q);
     if (e != cudaSuccess || !part || piece < p.pieces - 1) return e;

@@ -108,30 +108,27 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
     const int tiles = a.mt * a.nt;
 
     if (warp == 8) {
-        if (lane == 0) {
-            uint64_t keep, stream;
-            asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
-            if (a.mt == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(stream));
-            else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(stream));
-            int n = 0;
-            bool ok = true;
-            for (int t = worker; t < tiles && ok; t += workers) {
-                const int r0 = (t % a.mt) * (PAIR ? 2 * TM : TM) + rank * TM, n0 = (t / a.mt) * a.bn + (PAIR ? rank * (a.bn >> 1) : 0);
-                for (int kb = 0; kb < a.nkb; ++kb, ++n) {
-                    const int slot = n % STAGES;
-                    ok = wait_h(&gave_up, empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u);
-                    if (!ok) break;
-                    unsigned char *st = smem + slot * STAGE;
-                    if (rank == 0) mbar_expect_tx(full + slot, (uint32_t)(PAIR ? 2 * a.a_rows + a.bn : a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
-                    const uint32_t bar = PAIR ? first_block(full + slot) : smem_u32(full + slot);
-                    tma_2d<PAIR>(st, &map_a, kb * 64, r0, bar, keep);
-                    tma_2d<PAIR>(st + A_BYTES, &map_b, kb * 64, n0, bar, stream);
-                }
+        // lane 0 copies hidden rows, lane 1 the head, by one instruction
+        uint64_t policy;
+        if (a.mt == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
+        if (lane == 0) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+        const uint32_t full0 = PAIR ? first_block(full) : smem_u32(full);
+        int n = 0;
+        bool ok = true;
+        for (int t = worker; t < tiles && ok; t += workers) {
+            const int y = lane ? (t / a.mt) * a.bn + (PAIR ? rank * (a.bn >> 1) : 0) : (t % a.mt) * (PAIR ? 2 * TM : TM) + rank * TM;
+            for (int kb = 0; kb < a.nkb; ++kb, ++n) {
+                const int slot = n % STAGES;
+                ok = __all_sync(0xffffffffu, wait_h(&gave_up, empty + slot, (((uint32_t)(n / STAGES)) & 1u) ^ 1u));
+                if (!ok) break;
+                if (lane == 0 && rank == 0) mbar_expect_tx(full + slot, (uint32_t)(PAIR ? 2 * a.a_rows + a.bn : a.a_rows + a.bn) * 128u);   // (both blocks' bytes)
+                if (lane < 2) tma_2d<PAIR>(smem + slot * STAGE + lane * A_BYTES, lane ? &map_b : &map_a, kb * 64, y, full0 + slot * 8, policy);
             }
-            // no copy may be in flight when the block ends (a pair's arrive at its first block's barriers; the second ends after it)
-            for (int j = max(0, n - STAGES); j < n && rank == 0; ++j)
-                for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
         }
+        // no copy may be in flight when the block ends (a pair's arrive at its first block's barriers; the second ends after it)
+        for (int j = max(0, n - STAGES); j < n && rank == 0 && lane == 0; ++j)
+            for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
     } else if (warp == 9) {
         // (all lanes wait, one issues; of a pair the first block's)
         const uint32_t on = elect_lane(), idesc = PAIR ? (umma_idesc(a.bn) & ~(31u << 24)) | (256u >> 4) << 24 : umma_idesc(a.bn);
@@ -187,7 +184,7 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {                                      // the next products may overwrite the accumulator
-                    if (PAIR) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(acc_empty + (i & 1))) : "memory");
+                    if (PAIR) acc_release(acc_empty + (i & 1));
                     else mbar_arrive(acc_empty + (i & 1));
                 }
             }

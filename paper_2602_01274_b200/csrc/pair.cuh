@@ -32,6 +32,12 @@ __device__ __forceinline__ void cluster_sync() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// A warp's accumulator values are in registers (tcgen05.wait::ld): the next products may overwrite them.  Called by one lane for the first block's
+// barrier.  Relaxed: nothing else is handed over, and an arrival that releases at cluster scope waits for the warp's stores to global memory
+// (a tile of 128 x 256 gradients with two k blocks took 3 us instead of 1.1).
+__device__ __forceinline__ void acc_release(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(bar)) : "memory");
+}
 // As umma_if and umma_commit_if for both blocks' operands, accumulators and barriers; issued by the first block.
 __device__ __forceinline__ void umma2_if(uint32_t on, uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
