@@ -647,40 +647,52 @@ class AdamwTensors:
 
     def __init__(self, params, exp_avg, exp_avg_sq, scales=None, copies=None):
         self.tensors = tuple(None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales))
-        params, copies, exp_avg, exp_avg_sq, scales = self.tensors
+        params = self.tensors[0]
         self.state_bits, n = 32 if scales is None else 8, len(params)
-        for x in self.tensors:
-            if x is not None and len(x) != n:
-                raise AssertionError("AdamwTensors: lists of one length")
-        state = torch.float32 if scales is None else torch.uint8
+        if any(x is not None and len(x) != n for x in self.tensors):
+            raise AssertionError("AdamwTensors: lists of one length")
         self.device = params[0].device if n else None
-        for i, p in enumerate(params):
-            if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16)):
-                raise AssertionError(f"param {i}: f32 or bf16 on the GPU")
-            for t, dtype, name in ((exp_avg[i], state, "exp_avg"), (exp_avg_sq[i], state, "exp_avg_sq"), (copies and copies[i], torch.bfloat16, "copy")):
-                if t is not None and t is not False and (t.dtype != dtype or t.numel() != p.numel()):
-                    raise AssertionError(f"{name} {i}: {dtype} of the param's size")
-            if scales is not None and (scales[i].dtype != torch.float32 or scales[i].shape != (-(-p.numel() // 256), 2)):
-                raise AssertionError(f"scales {i}: torch.float32 [{-(-p.numel() // 256)}][2]")
-            for x in self.tensors:
-                if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == self.device):
-                    raise AssertionError(f"tensors of param {i}: contiguous, on {self.device}")
-        self.all = [t for x in self.tensors if x is not None for t in x]
-        # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type)
         self.numel = [p.numel() for p in params]
+        self._check()
+        self.all = [t for x in self.tensors if x is not None for t in x]
+        self.changed = [t for t in self.all if t is not None]
+        self._gaps = len(self.changed) < len(self.all)                  # (copies may be missing)
+        # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type)
         self._types = np.array([_DTYPES[p.dtype] for p in params], dtype=np.int64)
         self.table = np.zeros((n, 8), dtype=np.int64)
         self.table[:, 6], self.table[:, 7] = self.numel, self._types
-        self._at = self._grads_at = self._grads_types = None
         self._address = self.table.ctypes.data
-        self._gaps = any(t is None for t in self.all)
+        self._at = self._grads_at = self._grads_types = None
         self._place()
 
+    def _check(self):
+        params, copies, exp_avg, exp_avg_sq, scales = self.tensors
+        state = torch.float32 if scales is None else torch.uint8
+        for i, (p, n) in enumerate(zip(params, self.numel)):
+            if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16)):
+                raise AssertionError(f"param {i}: f32 or bf16 on the GPU")
+            if p.numel() != n:
+                raise AssertionError(f"param {i}: has another size than when it was given")
+            for t, dtype, name in ((exp_avg[i], state, "exp_avg"), (exp_avg_sq[i], state, "exp_avg_sq"), (copies[i] if copies else None, torch.bfloat16, "copy")):
+                if (t is not None or name != "copy") and (t.dtype != dtype or t.numel() != n):
+                    raise AssertionError(f"{name} {i}: {dtype} of the param's size")
+            if copies and copies[i] is not None and p.dtype != torch.float32:
+                raise AssertionError(f"copy {i}: only of an f32 param")
+            if scales is not None and (scales[i].dtype != torch.float32 or scales[i].shape != (-(-n // 256), 2)):
+                raise AssertionError(f"scales {i}: torch.float32 [{-(-n // 256)}][2]")
+            for x in self.tensors:
+                if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == self.device):
+                    raise AssertionError(f"tensors of param {i}: contiguous, on {self.device}")
+
     def _place(self):
-        """The addresses, as they are now (a program may exchange a parameter's storage)."""
+        """The addresses, as they are now: a program may exchange a tensor's storage (which is then looked at again)."""
         at = [0 if t is None else t.data_ptr() for t in self.all] if self._gaps else list(map(torch.Tensor.data_ptr, self.all))
         if at != self._at:
+            if self._at is not None:
+                self._check()
             self._at, n = at, len(self.numel)
+            self._types = np.array([_DTYPES[p.dtype] for p in self.tensors[0]], dtype=np.int64)
+            self._grads_types = None
             for i, col in enumerate(c for c, x in zip((0, 1, 3, 4, 5), self.tensors) if x is not None):
                 self.table[:, col] = at[i * n:(i + 1) * n]
 
@@ -754,7 +766,7 @@ def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps:
         assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == tensors.device, f"norm: one torch.float32 on {tensors.device}"
         cfg.norm = norm.data_ptr()
     _call(_lib.pacer_adamw, tensors, table, len(tensors.numel), C.byref(cfg))
-    _written(*tensors.all)
+    torch.autograd.graph.increment_version(tensors.changed)             # (as _written)
 
 
 def pacer_adamw_states(tensors: AdamwTensors, out=None):

@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(THREADS_W, BITS == 8 ? 3 : 4) k_adamw(const __
     }
     uint32_t step = h.step;
     if (h.step_dev || h.lr_dev) {
-        if (h.step_dev) step = (uint32_t)*h.step_dev;
+        if (h.step_dev) step = (uint32_t)max(*h.step_dev, 1);
         const double lr = h.lr_dev ? (double)*h.lr_dev : h.lr;
         q.a = (float)(lr / (1.0 - pow(h.b1d, (double)step)));
         q.s2 = (float)(1.0 / sqrt(1.0 - pow(h.b2d, (double)step)));

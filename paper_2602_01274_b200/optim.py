@@ -29,19 +29,35 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError("betas in [0, 1); eps, lr and max_norm at least 0")
         if torch.is_tensor(lr) and not capturable:
             raise ValueError("lr on the device: only with capturable")
-        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
         self.states, self.master, self.seed, self.max_norm, self.capturable = states, master, seed, max_norm, capturable
-        for group in self.param_groups:
-            for p in group["params"]:
-                if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16) and p.is_contiguous()):
-                    raise ValueError("params: f32 or bf16, contiguous, on the GPU")
+        self._tables = {}
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        for p in self.param_groups[-1]["params"]:
+            if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16) and p.is_contiguous()):
+                self.param_groups.pop()
+                raise ValueError("params: f32 or bf16, contiguous, on the GPU")
+
+    def __getstate__(self):
+        own = ("states", "master", "seed", "max_norm", "capturable")
+        return dict(super().__getstate__(), **{k: getattr(self, k) for k in own})
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
         self._tables = {}
 
-    def _state_of(self, p):
+    def _state_of(self, p, fresh):
+        """fresh: the count that parameters met for the first time in this step share, by device."""
         s = self.state[p]
         if not s:
             small = self.states == "f32" or p.numel() < SMALL
-            s["step"] = torch.zeros((), dtype=torch.int32, device=p.device) if self.capturable else 0
+            s["step"] = 0
+            if self.capturable:
+                if p.device not in fresh:
+                    fresh[p.device] = torch.zeros((), dtype=torch.int32, device=p.device)
+                s["step"] = fresh[p.device]
             for name in ("exp_avg", "exp_avg_sq"):
                 s[name] = torch.zeros(p.shape, dtype=torch.float32 if small else torch.uint8, device=p.device)
             if not small:
@@ -52,32 +68,47 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         """States keep their types (torch would take them to their parameter's)."""
-        held = [k for k in state_dict["state"]]
         super().load_state_dict(state_dict)
         params = [p for g in self.param_groups for p in g["params"]]
-        numbers = [n for g in state_dict["param_groups"] for n in g["params"]]
-        place = dict(zip(numbers, params))
-        for k in held:
+        place = dict(zip([n for g in state_dict["param_groups"] for n in g["params"]], params))
+        counts = {}
+        for k, held in state_dict["state"].items():
             p = place[k]
-            for name, x in state_dict["state"][k].items():
-                if name == "step":
-                    x = int(x)
-                    self.state[p][name] = torch.full((), x, dtype=torch.int32, device=p.device) if self.capturable else x
-                else:
+            for name, x in held.items():
+                if name != "step":
                     self.state[p][name] = x.detach().to(p.device, copy=True)
+                elif self.capturable:                                   # (equal counts are one tensor)
+                    key = (p.device, int(x))
+                    if key not in counts:
+                        counts[key] = torch.full((), int(x), dtype=torch.int32, device=p.device)
+                    self.state[p][name] = counts[key]
+                else:
+                    self.state[p][name] = int(x)
         self._tables = {}
 
     def _buckets(self):
         """Lists of parameters that one call takes: those of a group, device, count and kind of state."""
-        buckets = {}
+        buckets, fresh = {}, {}
         for gi, group in enumerate(self.param_groups):
             for p in group["params"]:
                 if p.grad is None:
                     continue
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW: no sparse gradients")
-                s = self._state_of(p)
-                buckets.setdefault((gi, p.device, None if self.capturable else s["step"], "scales" in s), []).append(p)
+                s = self._state_of(p, fresh)
+                buckets.setdefault((gi, p.device, id(s["step"]) if self.capturable else s["step"], "scales" in s), []).append(p)
+        if self.capturable:
+            # a count on the device is shared by the parameters that have had the same steps: where some of them have none now, the others go on
+            # with a copy of it
+            now = {p for ps in buckets.values() for p in ps}
+            stay = {id(s["step"]) for p, s in self.state.items() if p not in now and s}
+            copies = {}
+            for p in now:
+                t = self.state[p]["step"]
+                if id(t) in stay:
+                    if torch.cuda.is_current_stream_capturing():
+                        raise RuntimeError("AdamW: a captured step has to have the gradients of the steps before it")
+                    self.state[p]["step"] = copies.setdefault(id(t), t.clone())
         return buckets
 
     @torch.no_grad()
@@ -93,20 +124,22 @@ class AdamW(torch.optim.Optimizer):
             if len({p.device for p in grads}) > 1:
                 raise RuntimeError("AdamW: max_norm with parameters on one GPU only")
             norm = binding.pacer_grad_norm(list(grads.values()))
-        for (gi, device, count, coded), ps in buckets.items():
-            group = self.param_groups[gi]
+        if self.capturable:
+            for t in {id(s["step"]): s["step"] for s in map(self.state.__getitem__, grads)}.values():
+                t += 1
+        else:
+            for p in grads:
+                self.state[p]["step"] += 1
+        for (gi, device, _, coded), ps in buckets.items():
+            group, st = self.param_groups[gi], [self.state[p] for p in ps]
             key = (gi, device, coded, *map(id, ps))
             if key not in self._tables:
-                self._tables = {k: t for k, t in self._tables.items() if k[:3] != key[:3]}
-                st = [self.state[p] for p in ps]
+                if len(self._tables) >= 64:                             # (programs whose parameters take turns)
+                    self._tables.clear()
                 copies = [p if "master" in s else None for p, s in zip(ps, st)]
                 self._tables[key] = binding.AdamwTensors([s.get("master", p) for p, s in zip(ps, st)], [s["exp_avg"] for s in st],
                                                          [s["exp_avg_sq"] for s in st], [s["scales"] for s in st] if coded else None,
                                                          copies if any(c is not None for c in copies) else None)
-            for p in ps:
-                self.state[p]["step"] += 1
-            # (a capturable optimiser's parameters may have different counts: one call for each count would need to read them back)
-            step = self.state[ps[0]]["step"] if self.capturable else count + 1
-            binding.pacer_adamw(self._tables[key], [grads[p] for p in ps], step, group["lr"], group["betas"], group["eps"], group["weight_decay"],
-                                self.seed, norm, self.max_norm)
+            binding.pacer_adamw(self._tables[key], [grads[p] for p in ps], st[0]["step"], group["lr"], group["betas"], group["eps"],
+                                group["weight_decay"], self.seed, norm, self.max_norm)
         return loss

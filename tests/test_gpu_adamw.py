@@ -345,3 +345,51 @@ def test_optimiser_refusals():
     for q in (torch.zeros(8), torch.zeros(8, device=DEV, dtype=torch.float16), torch.zeros(8, 8, device=DEV).T[:4]):
         with pytest.raises(ValueError):
             optim.AdamW([torch.nn.Parameter(q)])
+
+
+def test_optimiser_whose_parameters_take_turns():
+    """Parameters without a gradient in some steps have counts of their own, on the host and on the device alike; copies of an optimiser, groups
+    that are added."""
+    import copy
+    from paper_2602_01274_b200 import optim
+    new = lambda: [torch.nn.Parameter(torch.randn(n, generator=gen(n), device=DEV)) for n in (500, 300, 70)]
+    sides = [new(), new()]
+    opts = [optim.AdamW(ps[:2], lr=1e-2, capturable=c) for ps, c in zip(sides, (False, True))]
+    for o, ps in zip(opts, sides):
+        o.add_param_group(dict(params=ps[2:], lr=1e-3))
+    turns = [(0, 1, 2), (0,), (0, 2), (1, 2), (0, 1, 2), (2,)]
+    for k, turn in enumerate(turns):
+        for o, ps in zip(opts, sides):
+            for i, p in enumerate(ps):
+                p.grad = torch.randn(p.shape, generator=gen(50 + k * 3 + i), device=DEV) if i in turn else None
+            o.step()
+    assert all(torch.equal(x, y) for x, y in zip(*sides))
+    want = [sum(i in t for t in turns) for i in range(3)]
+    for o, ps in zip(opts, sides):
+        assert [int(o.state[p]["step"]) for p in ps] == want
+    twin = copy.deepcopy(opts[0])
+    assert twin.states == "f32" and len(twin.param_groups) == 2
+    for p, g in zip([p for gr in twin.param_groups for p in gr["params"]], sides[0]):
+        p.grad = g.grad = torch.ones_like(p)
+    twin.step()
+    opts[0].step()
+    assert all(torch.equal(p, q) for p, q in zip([p for gr in twin.param_groups for p in gr["params"]], sides[0]))
+    with pytest.raises(ValueError):
+        opts[0].add_param_group(dict(params=[torch.nn.Parameter(torch.zeros(4))]))
+    assert len(opts[0].param_groups) == 2
+
+
+def test_tensors_whose_storage_is_exchanged():
+    from paper_2602_01274_b200 import binding as b
+    p, g, m, v, _, _ = make([1000, 40], "f32", "f32", 32, 9)
+    t = b.AdamwTensors(p, m, v)
+    b.pacer_adamw(t, g, 1, 1e-3)
+    q = [x.clone() for x in (p[0], m[0], v[0])]
+    b.pacer_adamw(b.AdamwTensors(q[:1], q[1:2], q[2:]), g[:1], 2, 1e-3)
+    kept = p[0].clone()
+    p[0].data = kept.clone()
+    b.pacer_adamw(t, g, 2, 1e-3)
+    assert torch.equal(p[0], q[0]) and torch.equal(m[0], q[1])
+    p[0].data = torch.zeros(999, device=DEV)
+    with pytest.raises(AssertionError, match="another size"):
+        b.pacer_adamw(t, g, 3, 1e-3)
