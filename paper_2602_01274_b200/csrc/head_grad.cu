@@ -15,11 +15,13 @@
 #include <type_traits>
 
 #include "pair.cuh"
+#include "two.cuh"
 
 namespace hg {
 
 using namespace fwd;
 using namespace pr;
+using namespace tw;
 
 constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's half of a tile, columns of a tile; 64 rows x 64 columns
 constexpr int STAGE = 4 * PANEL, STAGES = 5, OUT = 32 * 128, OUTS = 2;      // (a warp's output buffers)
@@ -193,15 +195,14 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + (bid - at == e ? a.bias : 0.f));
                 uint32_t w[16], l16[16];
-                float g[2];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float l = fmaf(__uint_as_float(v[e]), LOG2E, -lse);
-                    g[e & 1] = ex2(l) * fmaf(h, l, c);
-                    if (e & 1) {
-                        w[e >> 1] = pack(g[0], g[1]);
-                        if (a.low) l16[e >> 1] = pack(g[0] - __uint_as_float(w[e >> 1] << 16), g[1] - __uint_as_float(w[e >> 1] & 0xffff0000u));
-                    }
+                for (int e = 0; e < 32; e += 2) {
+                    const Two l = fma2(two(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), two(LOG2E, LOG2E), two(-lse, -lse));
+                    float l0, l1, g0, g1;
+                    apart(l, l0, l1);
+                    apart(mul2(two(ex2(l0), ex2(l1)), fma2(two(h, h), l, two(c, c))), g0, g1);
+                    w[e >> 1] = pack(g0, g1);
+                    if (a.low) l16[e >> 1] = pack(g0 - __uint_as_float(w[e >> 1] << 16), g1 - __uint_as_float(w[e >> 1] & 0xffff0000u));
                 }
                 if (!ok)
 #pragma unroll

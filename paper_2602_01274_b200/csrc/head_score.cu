@@ -18,11 +18,13 @@
 #include <algorithm>
 
 #include "pair.cuh"
+#include "two.cuh"
 
 namespace hs {
 
 using namespace fwd;
 using namespace pr;
+using namespace tw;
 
 constexpr int TM = 128, TN = 256, A_BYTES = TM * 128;
 // PAIR: two blocks of a cluster work on 256 rows, each with its 128 of them and half of the tile's tokens in shared memory.
@@ -212,7 +214,7 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
 #pragma unroll
                             for (int e = 0; e < 32; ++e) v[e] = tok - at == e ? OUTSIDE : v[e];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) s.m = fmaxf(s.m, v[e]);
+                        for (int e = 0; e < 32; e += 2) s.m = max3(s.m, v[e], v[e + 1]);
                         continue;
                     }
                     float top = v[0];
@@ -234,15 +236,20 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                 for (int c = 0; c < 4; ++c) {
                     const int at = (c0 + c) * 32;
                     if (c0 + c >= c1 || width - at <= 0) continue;
-                    float S0 = 0.f, S1 = 0.f;
+                    Two sum = two(0.f, 0.f);
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        const float x0 = ex2((z[c][e] - s.m) * LOG2E), x1 = ex2((z[c][e + 1] - s.m) * LOG2E);
-                        S0 += x0; S1 += x1;
+                        float x0, x1;
+                        apart(mul2(add2(two(z[c][e], z[c][e + 1]), two(-s.m, -s.m)), two(LOG2E, LOG2E)), x0, x1);
+                        x0 = ex2(x0);
+                        x1 = ex2(x1);
+                        sum = add2(sum, two(x0, x1));
                         const __half2 h = __floats2half2_rn(x0, x1);
                         w[e >> 1] = *reinterpret_cast<const uint32_t *>(&h);
                     }
+                    float S0, S1;
+                    apart(sum, S0, S1);
                     s.S += S0 + S1;
                     if (live) {
                         __half *p = a.keep + (size_t)r * a.ld_keep + n0 + at;

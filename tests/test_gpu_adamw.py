@@ -247,6 +247,26 @@ def test_many_tensors_streams_and_graphs():
     assert int(step) == 3 and all(torch.equal(x, y) for a, c in zip((p, m, v, s), q) for x, y in zip(a, c))
 
 
+def test_elements_beyond_32_bits():
+    """A tensor whose last elements have numbers above 2^32 (27 GB): they go as they would by themselves."""
+    from paper_2602_01274_b200 import binding as b
+    n, last = (1 << 32) + 300, 556                                       # (the last blocks of 256 begin at 2^32 - 256)
+    p, g = (torch.zeros(n, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    m, v = (torch.zeros(n, device=DEV, dtype=torch.uint8) for _ in range(2))
+    s = torch.zeros(-(-n // 256), 2, device=DEV)
+    q, h, c, d, e = make([last], "bf16", "bf16", 8, 10)[:5]
+    for big, small in zip((p, g, m, v), (q, h, c, d)):
+        big[-last:] = small[0]
+    s[-3:] = e[0]
+    norm = b.pacer_grad_norm([g])
+    assert torch.equal(norm, b.pacer_grad_norm(h))
+    b.pacer_adamw(b.AdamwTensors([p], [m], [v], [s]), [g], 4, 1e-3)
+    b.pacer_adamw(b.AdamwTensors(q, c, d, e), h, 4, 1e-3)
+    for big, small in zip((p, m, v), (q, c, d)):
+        assert torch.equal(big[-last:], small[0]) and not big[-last - 300:-last].any()
+    assert torch.equal(s[-3:], e[0])
+
+
 def test_refusals():
     from paper_2602_01274_b200 import binding as b
     p, g, m, v, _, _ = make([100, 50], "f32", "f32", 32, 8)

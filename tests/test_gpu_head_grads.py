@@ -54,6 +54,8 @@ SHAPES = [
     (1, 1, 8, 0), (1, 2, 64, 0), (2, 31, 72, 0), (7, 33, 128, 8), (8, 257, 64, 0), (9, 1000, 200, 0), (1, 4096, 256, 0), (33, 4099, 768, 0),
     (64, 512, 264, 0), (65, 513, 136, 64), (127, 5003, 256, 0), (128, 8000, 128, 0), (129, 8003, 1032, 0), (256, 256, 256, 0), (257, 255, 320, 8),
     (300, 32256, 512, 0), (1000, 7777, 1024, 0), (5, 40007, 64, 0), (2048, 4096, 2048, 0), (1153, 1201, 5120, 0),
+    # four k blocks of rows and more, with rows of the gradient that no 32-byte stores fit
+    (600, 1001, 1032, 0), (700, 2003, 264, 8), (193, 300, 24, 0),
 ]
 
 
@@ -193,9 +195,18 @@ def test_outputs_of_the_caller_strides_and_versions():
         b.pacer_head_nll_grad(h, w, tok, weight, out=(torch.empty(50, 136, device=DEV), None))
     with pytest.raises(b.PacerError, match="overlaps"):
         b.pacer_head_nll_grad(h, w, tok, weight, out=(h, None))
+    # more rows, gradients that begin off the 32-byte grid
+    h, w, tok, _ = make(400, 999, 144)
+    weight = weights(400)[0]
+    _, dh, dw = b.pacer_head_nll_grad(h, w, tok, weight)
+    out = tuple(torch.full((n, 160), 5.0, device=DEV, dtype=torch.bfloat16) for n in (400, 999))
+    b.pacer_head_nll_grad(h, w, tok, weight, out=[x[:, 8:152] for x in out])
+    assert torch.equal(out[0][:, 8:152], dh) and torch.equal(out[1][:, 8:152], dw)
+    assert all((x[:, :8] == 5.0).all() and (x[:, 152:] == 5.0).all() for x in out)
     both = torch.empty(1049, 136, device=DEV, dtype=torch.bfloat16)
+    h, w, tok, _ = make(50, 999, 136)
     with pytest.raises(b.PacerError, match="overlaps"):
-        b.pacer_head_nll_grad(h, w, tok, weight, out=(both[:50], both[49:1048]))
+        b.pacer_head_nll_grad(h, w, tok, weights(50)[0], out=(both[:50], both[49:1048]))
 
 
 def test_scratch_between_calls_graphs_and_streams():
