@@ -311,17 +311,19 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
 // loss log(1 + others / its own) where it has the largest logit: confident rows lose nothing.  low: the remainders bf16(x - bf16(x)), or NULL.
 struct DzArgs {
     int32_t segs, seg;                     // pieces of a row and their columns, a multiple of 8
+    uint32_t by_bn;                        // 2^32 / bn, rounded up (exact quotients below 2^32 / bn)
     const float *weight;
     float *loss;
     __nv_bfloat16 *low;
 };
 constexpr int THREADS_D = 256;
+template <bool LOW>
 __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzArgs g) {
     __shared__ Part red[THREADS_D / 32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int row = blockIdx.x / g.segs, at = (blockIdx.x - row * g.segs) * g.seg, lane = threadIdx.x & 31, end = min(at + g.seg, a.vocab);
-    uint4 *z = reinterpret_cast<uint4 *>(a.keep + (size_t)row * a.ld_keep), *low = reinterpret_cast<uint4 *>(g.low ? g.low + (size_t)row * a.ld_keep : nullptr);
+    uint4 *z = reinterpret_cast<uint4 *>(a.keep + (size_t)row * a.ld_keep), *low = LOW ? reinterpret_cast<uint4 *>(g.low + (size_t)row * a.ld_keep) : nullptr;
     constexpr int STEP = THREADS_D * 8;
     int c = at + threadIdx.x * 8;
     uint4 v[4] = {};                       // (on their way while the parts are joined)
@@ -358,25 +360,31 @@ __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzAr
     S = others + mine;
     const float l2 = log2f(S), of_token = -weight * (others / S);
     if (at == 0 && threadIdx.x == 0 && g.loss) g.loss[row] = tok < 0 ? 0.f : zt == m ? log1pf(others) : (m - zt) + l2 * LN2;
-    const int chunks = a.bn >> 5, first = (chunks + 1) >> 1;           // (32-token chunks of a tile's first half)
+    const int first = (a.bn + 32) >> 6 << 5;                           // tokens of a tile's first half (whole chunks of 32)
     const auto scaled = [&](int c, uint4 v) {
-        const int tile = c / a.bn, half = (c - tile * a.bn) >> 5 >= first;
+        const int tile = (int)__umulhi((uint32_t)c, g.by_bn), half = c - tile * a.bn >= first;             // (c / bn)
         const float t = (p[2 * tile + half].x - m) * LOG2E - l2, f = t < FAR ? 0.f : weight * ex2(t);      // (NaN stays)
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const Two ff = two(f, f);
         uint32_t o[4], r[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float2 x = __half22float2(*reinterpret_cast<const __half2 *>(w + e));
-            x.x *= f; x.y *= f;
-            if (tok == c + 2 * e) x.x = of_token;
-            if (tok == c + 2 * e + 1) x.y = of_token;
+            apart(mul2(two(x.x, x.y), ff), x.x, x.y);
             const __nv_bfloat162 b = __floats2bfloat162_rn(x.x, x.y);
             o[e] = *reinterpret_cast<const uint32_t *>(&b);
-            const __nv_bfloat162 d = __floats2bfloat162_rn(x.x - __low2float(b), x.y - __high2float(b));
-            r[e] = *reinterpret_cast<const uint32_t *>(&d);
+            if (LOW) {
+                const __nv_bfloat162 d = __floats2bfloat162_rn(x.x - __low2float(b), x.y - __high2float(b));
+                r[e] = *reinterpret_cast<const uint32_t *>(&d);
+            }
         }
         z[c >> 3] = make_uint4(o[0], o[1], o[2], o[3]);
-        if (low) low[c >> 3] = make_uint4(r[0], r[1], r[2], r[3]);
+        if (LOW) low[c >> 3] = make_uint4(r[0], r[1], r[2], r[3]);
+        if ((uint32_t)(tok - c) < 8u) {                                // (the token's own, by the same thread)
+            const __nv_bfloat16 b = __float2bfloat16_rn(of_token);
+            reinterpret_cast<__nv_bfloat16 *>(z)[tok] = b;
+            if (LOW) reinterpret_cast<__nv_bfloat16 *>(low)[tok] = __float2bfloat16_rn(of_token - __bfloat162float(b));
+        }
     };
     while (c < end) {
 #pragma unroll
@@ -472,6 +480,7 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     if (a.dz) {                            // rows cut into pieces while all blocks fit the SMs at once, six on each
         g.segs = std::max(1, std::min((a.vocab + 8 * THREADS_D - 1) / (8 * THREADS_D), 6 * n_sm / a.rows));
         g.seg = ((a.vocab + g.segs - 1) / g.segs + 7) & ~7;
+        g.by_bn = (uint32_t)((((uint64_t)1 << 32) + t.bn - 1) / t.bn);
         g.weight = a.weight; g.loss = a.loss; g.low = reinterpret_cast<__nv_bfloat16 *>(a.dz_low);
         c.gridDim = dim3((unsigned)a.rows * (unsigned)g.segs);
         c.blockDim = dim3(THREADS_D);
@@ -482,7 +491,7 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     at[0].val.programmaticStreamSerializationAllowed = 1;
     c.attrs = at;
     c.numAttrs = 1;
-    if (a.dz) return cudaLaunchKernelEx(&c, k_head_dz, k, g);
+    if (a.dz) return g.low ? cudaLaunchKernelEx(&c, k_head_dz<true>, k, g) : cudaLaunchKernelEx(&c, k_head_dz<false>, k, g);
     return cudaLaunchKernelEx(&c, k_head_join, k, a.logp, a.entropy, a.lse, a.loss);
 }
 
