@@ -383,7 +383,8 @@ int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head,
  * sums are fp32.  It is kept for as many tokens at a time as 2 GB holds, so that the scratch stays bounded for any number of rows.
  * Addresses 16-byte aligned, strides multiples of 8; the gradients overlap neither the operands nor each other.  rows = 0 sets dhead
  * to 0.  scratch: device, 256-byte aligned, at least pacer_head_logprobs_backward_scratch_bytes(rows, vocab, d) bytes, in use until the
- * call's kernels have run.  No atomics: the same call gives the same bits.  Enqueues two kernels for a piece of the vocabulary and one at
+ * call's kernels have run.  Inputs must be finite; a wait inside a kernel that ran out makes results NaN.  No atomics: the same call gives the
+ * same bits.  Enqueues two kernels for a piece of the vocabulary and one at
  * the end; may be captured into a graph (not as the first call on a device). */
 size_t pacer_head_logprobs_backward_scratch_bytes(int rows, int vocab, int d);
 int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,

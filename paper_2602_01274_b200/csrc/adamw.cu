@@ -1,6 +1,8 @@
 // AdamW over many tensors in one launch, states in 32 or in 8 bits; the global norm of their gradients; 8-bit states as f32.
 //   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
-// All of it is bound by memory: 28 bytes an element with f32 parameters, gradients and states, 10 with 16-bit ones and 8-bit states.
+// Bound by memory: 28 bytes an element with f32 parameters, gradients and states (50.6 M elements 220 us, 98 % of the copy rate; 131 M with a
+// 16-bit gradient and copy 575 us, 97 %), 14 with f32 parameters, 16-bit gradients and 8-bit states (607 M 1445 us, 90 %); with 16-bit
+// parameters rounded at random, 10 bytes an element, by its 69 instructions (233 M 544 us, 65 %).
 // The tensors' table travels in the launch's arguments (no copy to the device, nothing to keep), a block finds its chunk's tensor by bisection.
 //
 // States in 8 bits, in blocks of 256 elements, the share of a warp (eight elements a lane).  m: sign, 4 exponent and 3 mantissa bits;

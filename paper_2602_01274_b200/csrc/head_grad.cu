@@ -1,12 +1,15 @@
 // Gradients of the LM head fused with the scoring.  With z = hidden head^T (+ bias), p = exp(z - lse) and per row the incoming gradients,
 //   dz = g_logp ([v = token] - p) + g_lse p - g_entropy p (log p + entropy),   dhidden = dz head,   dhead = dz^T hidden.
-// z is computed again, and dz kept in bf16 for a piece of the vocabulary (all of it while that is at most 1 GB), as the operand of
-// the two products: three products of 2 rows vocab d operations, bound by the tensor cores for many rows, by reading the head
-// twice and writing dhead once for few.
+// z is computed again, and dz kept in bf16 for a piece of the vocabulary (all of it while that is at most 2 GB), as the operand of
+// the two products: three products of 2 rows vocab d operations, bound by the tensor cores for many rows (8192 x 32 256 x 2048: 2.42 ms,
+// 1.34 PFLOP/s, the rate that a long loop of library products holds under the power cap), by reading the head twice and writing dhead
+// once for few.
 //   k_head_z     z on tcgen05, dz by the epilogue
 //   k_head_prod  both products in one launch: 256 x 256 tiles by pairs of blocks, operands by tensor copies as they lie in memory (dz is
 //                read as its own transpose, hidden rows and head as MN-major operands: no transposed copies)
 //   k_head_sum   dhidden from partial sums, where its product was cut along the vocabulary
+// For the loss and its gradients in one call dz comes out of the loss's own pass (k_head_dz in head_score.cu): 2048 x 32 000 x 4096 1257 us, with
+// z computed twice 1690.
 // dz is rounded once, to bf16, as an operand has to be; sums are fp32.  1 - p of the row's token is -expm1(logp), so that confident
 // rows lose nothing to the difference.
 #include "head_grad.h"
