@@ -113,8 +113,9 @@ def head_logprobs(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor
 
 class _HeadNll(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, hidden, head, tokens, weight, bias_ids, bias):
-        loss, dhidden, dhead = binding.pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids, bias, grads=ctx.needs_input_grad[:2])
+    def forward(ctx, hidden, head, tokens, weight, bias_ids, bias, train):
+        grads = ctx.needs_input_grad[:2] if train else (False, False)
+        loss, dhidden, dhead = binding.pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids, bias, grads=grads)
         ctx.grads = dhidden, dhead, loss if ctx.needs_input_grad[3] else None
         return (loss * weight).sum()
 
@@ -122,7 +123,7 @@ class _HeadNll(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g):
         dhidden, dhead, loss = (None if x is None else x * g for x in ctx.grads)
-        return dhidden, dhead, None, loss, None, None
+        return dhidden, dhead, None, loss, None, None, None
 
 
 def head_nll(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, weight: torch.Tensor, bias_ids: Optional[torch.Tensor] = None,
@@ -132,4 +133,4 @@ def head_nll(hidden: torch.Tensor, head: torch.Tensor, tokens: torch.Tensor, wei
     unless it is a power of 2.  A token outside the vocabulary (-1: padding) adds nothing."""
     h, t, i = _flat_rows(hidden, tokens, bias_ids)
     assert weight.shape == tokens.shape, "weight: the hidden rows' leading shape"
-    return _HeadNll.apply(h, head, t, weight.reshape(-1), i, bias)
+    return _HeadNll.apply(h, head, t, weight.reshape(-1), i, bias, torch.is_grad_enabled())     # (inside the function it never is)

@@ -39,6 +39,16 @@ def test_head_nll_is_differentiable(trained):
         check(head.grad, 0.5 * dz, 0.5 * size, h.double(), False, sz, (60 / 16 + 1) * 2 * F32, "head")
     assert (h3.grad is None) == (not trained[0]) and (head.grad is None) == (not trained[1])
     assert torch.allclose(wt.grad.view(-1).double(), 0.5 * loss, rtol=1e-5, atol=1e-5)
+    # without gradients: the same sum, and none are computed
+    from paper_2602_01274_b200 import binding
+    asked, call = [], binding.pacer_head_nll_grad
+    binding.pacer_head_nll_grad = lambda *a, **kw: asked.append(kw["grads"]) or call(*a, **kw)
+    try:
+        with torch.no_grad():
+            again = losses.head_nll(h3, head, tok.view(4, 15), wt, bias_ids.view(4, 15), 8.0)
+    finally:
+        binding.pacer_head_nll_grad = call
+    assert asked == [(False, False)] and torch.allclose(again, total.detach(), rtol=1e-5)
 
 
 def test_head_logprobs_is_differentiable():
