@@ -152,6 +152,22 @@ def test_step_with_8_bit_states(ptype, gtype, shift, seed):
         assert ((p[i].double() - want).abs() <= off + half * 1.01 * want.abs() + 1e-38).all()
 
 
+def test_types_mixed_in_a_list():
+    """Every pair of types in one call, tensors on and off the 16-byte grid: the random numbers go by the place in the list."""
+    from paper_2602_01274_b200 import binding as b
+    kinds = [(pt, gt, shift) for pt in ("f32", "bf16") for gt in ("f32", "bf16", "f16") for shift in (0, 1)]
+    made = [make([n], pt, gt, 8, 20 + i, False, shift) for i, ((pt, gt, shift), n) in enumerate(zip(kinds, [700, 3000, 1, 9000, 512, 255, 4097, 31, 256, 8192, 100, 2047]))]
+    p, g, m, v, s = ([x[k][0] for x in made] for k in range(5))
+    old_m, old_v = b.pacer_adamw_states(b.AdamwTensors(p, m, v, s))
+    b.pacer_adamw(b.AdamwTensors(p, m, v, s), g, 6, seed=1234567890123, **HYPER)
+    for i in range(len(p)):
+        x = g[i].float()
+        rm, rv, _ = random_bits(len(x), 1234567890123, 6, i)
+        for new, codes, col, dither in ((old_m[i] * 0.9 + x * (1 - 0.9), m[i], 0, rm), (old_v[i] * 0.999 + (x * x) * (1 - 0.999), v[i], 1, rv)):
+            want, scale = encode(new, dither, col == 0)
+            assert torch.equal(codes, want) and torch.equal(s[i][:, col], scale), (i, kinds[i])
+
+
 def test_16_bit_parameters_rounded_at_random_move_as_they_should():
     """Updates far below a parameter's last bit: nearest never moves, at random the mean does."""
     from paper_2602_01274_b200 import binding as b
