@@ -403,7 +403,7 @@ int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head,
 /* An AdamW step over many tensors at once (in one launch up to 480 of them):
  *   m <- beta_one m + (1 - beta_one) g,   v <- beta_two v + (1 - beta_two) g^2,
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta_one^step) m / (sqrt(v) / sqrt(1 - beta_two^step) + eps)
- * in f32.  tbl: host array of n tensors, read before the call returns; all other pointers are device addresses, element-aligned (16 bytes
+ * in f32 (the quotient to 2^-22; a v below 2^-126 counts as 0 under the root).  tbl: host array of n tensors, read before the call returns; all other pointers are device addresses, element-aligned (16 bytes
  * let whole pieces be moved), arrays contiguous and apart; a tensor of no elements is passed over, a param listed twice refused. */
 typedef struct {
     void *param;             /* param_type: PACER_F32 or PACER_BF16 */

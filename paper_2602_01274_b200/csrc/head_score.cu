@@ -33,7 +33,7 @@ template <bool PAIR> struct Cfg {
 };
 constexpr int SEG_SCORE = 8;               // k blocks of 64 columns accumulated inside the tensor cores
 // Where the epilogue has twice the work (KEEP), segments twice as long give it the time: the loss's pass over 4093 rows x 151 936 x 1536 took
-// 1508 us with 8 blocks, 1341 with 12 or 16, over 2048 x 32 000 x 4096 371, 356 and 341.  (Results are then off by some 2.5e-7 of a logit.)
+// 1508 us with 8 blocks, 1341 with 12 or 16, over 2048 x 32 000 x 4096 371, 356 and 341.  (Losses are then 2.2e-7 off, relative.)
 constexpr int SEG_KEEP = 16;
 constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = 192 * 1024 + 1024;
 static_assert(Cfg<true>::STAGE * Cfg<true>::STAGES == 192 * 1024 && Cfg<false>::STAGE * Cfg<false>::STAGES == 192 * 1024, "the stages");
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
     if (warp == 8) {
         // lane 0 copies hidden rows, lane 1 the head, by one instruction
         uint64_t policy;
-        if (a.mt == 1) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        if (a.mt == 1 && !KEEP) asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));   // (the products read it again)
         else asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(policy));
         if (lane == 0) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
         const uint32_t full0 = PAIR ? first_block(full) : smem_u32(full);
