@@ -96,8 +96,9 @@ __device__ __forceinline__ void drain(Pair &s, int n, int rank) {
     for (int j = max(0, n - STAGES); j < n && rank == 0; ++j)
         for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(s.full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
 }
-__device__ __forceinline__ bool all_wait(Pair &s, uint64_t *bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, wait_h(&s.gave_up, bar, parity));
+// blocks: k blocks that are worked on meanwhile (a tile's sums over a million rows or tokens take milliseconds).
+__device__ __forceinline__ bool all_wait(Pair &s, uint64_t *bar, uint32_t parity, int blocks = 0) {
+    return __all_sync(0xffffffffu, wait_h(&s.gave_up, bar, parity, MBAR_SPIN_LIMIT * (1u + (unsigned)blocks / 1024u)));
 }
 __device__ __forceinline__ uint32_t pair_idesc(int n) { return (umma_idesc(n) & ~(31u << 24)) | (256u >> 4) << 24; }
 // An MN-major operand in the 128-byte swizzle: rows (k) of 64 channels, eight of them 1 KB, the next 64 channels a panel further.
@@ -353,7 +354,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
         int stored = 0;
         bool ok = true;
         for (int j = 0; walk(a, it); ++j) {
-            if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u);
+            if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u, it.k1 - it.k0);
             tc_fence_after();
             const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
             const int plane = !it.to_head && a.planes == 2 ? rank : 0;

@@ -54,9 +54,9 @@ __device__ __forceinline__ void st32(void *p, const uint32_t *v) {         // 32
                  "r"(v[6]), "r"(v[7]) : "memory");
 }
 // Bounded wait; one that runs out ends the block's work (its rows become NaN).
-__device__ __forceinline__ bool wait_h(volatile int32_t *gave_up, uint64_t *bar, uint32_t parity) {
+__device__ __forceinline__ bool wait_h(volatile int32_t *gave_up, uint64_t *bar, uint32_t parity, unsigned limit = MBAR_SPIN_LIMIT) {
     for (unsigned it = 1; !mbar_try_wait(bar, parity); ++it)
-        if ((it & 1023u) == 0 && (it > MBAR_SPIN_LIMIT || *gave_up)) { *gave_up = 1; return false; }
+        if ((it & 1023u) == 0 && (it > limit || *gave_up)) { *gave_up = 1; return false; }
     return true;
 }
 
