@@ -8,7 +8,7 @@
 //   k_head_prod  both products in one launch: 256 x 256 tiles by pairs of blocks, operands by tensor copies as they lie in memory (dz is
 //                read as its own transpose, hidden rows and head as MN-major operands: no transposed copies)
 //   k_head_sum   dhidden from partial sums, where its product was cut along the vocabulary
-// For the loss and its gradients in one call dz comes out of the loss's own pass (k_head_dz in head_score.cu): 2048 x 32 000 x 4096 1257 us, with
+// For the loss and its gradients in one call dz comes out of the loss's own pass (k_head_dz in head_score.cu): 2048 x 32 000 x 4096 1270 us, with
 // z computed twice 1690.
 // dz is rounded once, to bf16, as an operand has to be; sums are fp32.  1 - p of the row's token is -expm1(logp), so that confident
 // rows lose nothing to the difference.

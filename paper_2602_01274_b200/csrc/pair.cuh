@@ -34,7 +34,7 @@ __device__ __forceinline__ void cluster_sync() {
 }
 // A warp's accumulator values are in registers (tcgen05.wait::ld): the next products may overwrite them.  Called by one lane for the first block's
 // barrier.  Relaxed: nothing else is handed over, and an arrival that releases at cluster scope waits for the warp's stores to global memory
-// (a tile of 128 x 256 gradients with two k blocks took 3 us instead of 1.1).
+// (both gradients' products for 33 rows x 32 000 x 768: 28.8 us, 27.1 relaxed).
 __device__ __forceinline__ void acc_release(uint64_t *bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(bar)) : "memory");
 }

@@ -56,6 +56,8 @@ SHAPES = [
     (300, 32256, 512, 0), (1000, 7777, 1024, 0), (5, 40007, 64, 0), (2048, 4096, 2048, 0), (1153, 1201, 5120, 0),
     # four k blocks of rows and more, with rows of the gradient that no 32-byte stores fit
     (600, 1001, 1032, 0), (700, 2003, 264, 8), (193, 300, 24, 0),
+    # the largest vocabulary
+    (17, 1 << 21, 64, 0),
 ]
 
 
