@@ -8,9 +8,9 @@
 Sizes: the vocabularies and widths of ``synth.CONFIGS``, the rows of a short response up to those of a training batch, the tensors
 of the pre-verification layers, of a draft model, of heads, and odd ones.
 
-States in 8 bits: blocks of 256 elements with two f32 scales.  The first moment is held as sign, 4 exponent and 3 mantissa bits (0,
-2^-9 .. 480) times its scale, the second as 5 exponent and 3 mantissa bits (0, 2^-18 .. 61440) times its own; the block's largest
-gets the largest code, no code stands for infinities or NaN, and a second moment above 0 does not become 0.  With a seed, states and 16-bit parameters are rounded up or down at random with
+States in 8 bits: blocks of 256 elements with two f32 scales.  The first moment is held as sign, 4 exponent and 3 mantissa bits of
+its share of the block's largest (codes up to 480 steps of 1), the second as the root of its value, 4 exponent and 4 mantissa bits
+(up to 496); no code stands for infinities or NaN.  With a seed, states and 16-bit parameters are rounded up or down at random with
 16 random bits, a hash of (seed, step, tensor, element), the mean being the value; without one to nearest, halves up.
 """
 from __future__ import annotations
@@ -26,7 +26,7 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 MOST_FLOPS = 6.0 * 4093 * 151936 * 1536
 MOST_ELEMENTS = 6e8
 BETAS, EPS, DECAY, LR, STEP, SEED, MAX_NORM = (0.9, 0.999), 1e-8, 0.01, 1e-4, 37, 1234, 1.0
-BLOCK, TOP_M, TOP_V = 256, 480.0, 61440.0
+BLOCK, TOP_M, TOP_R = 256, 480.0, 496.0
 
 
 def _head(op, name, rows, vocab, d, **more):
@@ -161,7 +161,7 @@ def _prepare_adamw(case, g):
     s["scales"] = []
     for t in s["params"]:
         k = -(-t.numel() // BLOCK)
-        s["scales"].append((0.5 + torch.rand(k, 2, generator=g, device=DEVICE)) * torch.tensor([1e-2 / TOP_M, 4e-4 / TOP_V], device=DEVICE))
+        s["scales"].append((0.5 + torch.rand(k, 2, generator=g, device=DEVICE)) * torch.tensor([1e-2 / TOP_M, 2e-2 / TOP_R], device=DEVICE))
     return s
 
 
@@ -252,30 +252,33 @@ def _mix(x):
 
 
 def _random(n, tensor):
-    """Three 16-bit numbers for every element of a tensor."""
+    """Two 16-bit numbers and a third for every element of a tensor."""
     key = _mix(SEED ^ _mix(STEP ^ _mix(tensor)))
     h = _mix(torch.arange(n, device=DEVICE) ^ key)
     return h & 0xFFFF, h >> 16, ((h * 0x9E3779B1) & 0xFFFFFFFF) >> 16
 
 
+def _table(shift):
+    return (torch.arange(256, dtype=torch.int32, device=DEVICE) << shift).view(torch.float32) * 2.0 ** 120
+
+
 def _values(codes, scales, signed):
-    """What 8-bit codes of one tensor stand for: first or second moments."""
+    """What 8-bit codes of one tensor stand for: first moments, or roots of second ones."""
     c = codes.reshape(-1).long()
-    table = (torch.arange(256, dtype=torch.int32, device=DEVICE) << 20).view(torch.float32)
-    v = torch.where(c >= 128, -1.0, 1.0) * table[c & 127] * 2.0 ** 120 if signed else table[c] * 2.0 ** 111
+    v = torch.where(c >= 128, -1.0, 1.0) * _table(20)[c & 127] if signed else _table(19)[c]
     return v * scales[:, 0 if signed else 1].repeat_interleave(BLOCK)[:len(v)]
 
 
-def _codes(x, dither, signed):
-    """(codes, scales) of one tensor."""
-    n, a, top = len(x), x.abs(), TOP_M if signed else TOP_V
-    peak = torch.nn.functional.pad(a, (0, -n % BLOCK)).view(-1, BLOCK).max(1).values
+def _codes(x, dither, top, shift, most):
+    """(codes of |x|, scales) of one tensor."""
+    n, a = len(x), x.abs()
+    blocks = torch.nn.functional.pad(a, (0, -n % BLOCK)).view(-1, BLOCK)
+    peak = blocks.max(1).values
     inverse = torch.where(peak > 1e-30, torch.full_like(peak, top) / peak, 0.0)
     scale = torch.where(peak > 1e-30, peak * (1.0 / top), 0.0)
-    # as f32 numbers whose exponents begin where the codes' do: their upper bits are the code, subnormal ones included
-    bits = (a * inverse.repeat_interleave(BLOCK)[:n] * (2.0 ** -120 if signed else 2.0 ** -111)).view(torch.int32).long()
-    code = ((bits + (dither << 4 if dither is not None else 1 << 19)) >> 20).clamp(max=127 if signed else 255)
-    return torch.where(x < 0, code + 128, code) if signed else torch.where(x > 0, code.clamp(min=1), code), scale
+    bits = (a * inverse.repeat_interleave(BLOCK)[:n] * 2.0 ** -120).view(torch.int32).long()
+    code = (bits + (dither << (shift - 16) if dither is not None else 1 << (shift - 1))) >> shift
+    return code.clamp(max=most), scale
 
 
 def _clip(s):
@@ -295,21 +298,23 @@ def _plain_adamw(s):
             g = g * factor
         g = g.reshape(-1)
         if case["bits"] == 32:
-            m, v = m.view(-1), v.view(-1)
+            m, r2 = m.view(-1), v.view(-1)
         else:
-            m, v = _values(m, s["scales"][i], True), _values(v, s["scales"][i], False)
+            m, r = _values(m, s["scales"][i], True), _values(v, s["scales"][i], False)
+            r2 = r * r
         m = m * BETAS[0] + g * (1 - BETAS[0])
-        v = v * BETAS[1] + (g * g) * (1 - BETAS[1])
-        x = p.reshape(-1).float() * (1 - LR * DECAY) - (m / (v.sqrt() * s2 + EPS)) * a
-        rm, rv, rp = _random(len(x), i) if case["seeded"] else (None, None, None)
+        v = r2 * BETAS[1] + (g * g) * (1 - BETAS[1])
+        r = v.sqrt()
+        x = p.reshape(-1).float() * (1 - LR * DECAY) - (m / (r * s2 + EPS)) * a
+        rm, rr, rp = _random(len(x), i) if case["seeded"] else (None, None, None)
         if case["bits"] == 32:
             s["exp_avg"][i].view(-1).copy_(m)
             s["exp_avg_sq"][i].view(-1).copy_(v)
         else:
-            code, s["scales"][i][:, 0] = _codes(m, rm, True)
-            s["exp_avg"][i].view(-1).copy_(code)
-            code, s["scales"][i][:, 1] = _codes(v, rv, False)
-            s["exp_avg_sq"][i].view(-1).copy_(code)
+            code, s["scales"][i][:, 0] = _codes(m, rm, TOP_M, 20, 127)
+            s["exp_avg"][i].view(-1).copy_(torch.where(m < 0, code + 128, code))
+            code, s["scales"][i][:, 1] = _codes(r, rr, TOP_R, 19, 255)
+            s["exp_avg_sq"][i].view(-1).copy_(torch.where(r > 0, code.clamp(min=1), code))
         if p.dtype == torch.bfloat16 and case["seeded"]:
             x = ((x.view(torch.int32).long() + rp) >> 16 << 16).to(torch.int32).view(torch.float32)
         p.view(-1).copy_(x)
@@ -327,10 +332,10 @@ def _states(s):
         from paper_2602_01274_b200 import binding as b
         sizes = [t.numel() for t in s["params"]]
         m, v = torch.empty(2, sum(sizes), device=DEVICE).unbind()
-        b.pacer_adamw_states(s["tensors"], out=(m.split(sizes), v.split(sizes)))
+        b.pacer_adamw_states(s["exp_avg"], s["exp_avg_sq"], s["scales"], out=(m.split(sizes), v.split(sizes)))
     else:
         m = torch.cat([_values(c, k, True) for c, k in zip(s["exp_avg"], s["scales"])])
-        v = torch.cat([_values(c, k, False) for c, k in zip(s["exp_avg_sq"], s["scales"])])
+        v = torch.cat([_values(c, k, False).square() for c, k in zip(s["exp_avg_sq"], s["scales"])])
     return dict(params=s["flat"], exp_avg=m, exp_avg_sq=v, copies=s["flat_copy"])
 
 
@@ -347,9 +352,8 @@ def run(state):
                                                             s["grad_entropy"], s["grad_lse"], s["bias_ids"], 8.0, grads=want)
             return dict(dhidden=dhidden, dhead=dhead)
         norm = b.pacer_grad_norm(s["grads"]) if case["clip"] else None
-        if "tensors" not in s:                                          # (an optimiser keeps them)
-            s["tensors"] = b.AdamwTensors(s["params"], s["exp_avg"], s["exp_avg_sq"], s["scales"], s["copies"])
-        b.pacer_adamw(s["tensors"], s["grads"], STEP, LR, BETAS, EPS, DECAY, SEED if case["seeded"] else None, norm, MAX_NORM if case["clip"] else 0.0)
+        b.pacer_adamw(s["params"], s["grads"], s["exp_avg"], s["exp_avg_sq"], STEP, LR, BETAS, EPS, DECAY, scales=s["scales"], copies=s["copies"],
+                      seed=SEED if case["seeded"] else None, norm=norm, max_norm=MAX_NORM)
         return dict(_states(s), norm=norm)
     if case["op"] == "nll":
         return _plain_nll(s)
@@ -427,8 +431,8 @@ def _exact_adamw(case, s):
             e, x = (c >> 3) & 15, (c & 7).double()
             m = torch.where(e == 0, x / 8 * 2.0 ** -6, (1 + x / 8) * torch.exp2(e.double() - 7)) * (1 - 2 * (c >> 7)) * s["scales"][i][k, 0].double()
             c = s["exp_avg_sq"][i].reshape(-1).long()
-            e, x = c >> 3, (c & 7).double()
-            v = torch.where(e == 0, x / 8 * 2.0 ** -15, (1 + x / 8) * torch.exp2(e.double() - 16)) * s["scales"][i][k, 1].double()
+            e, x = c >> 4, (c & 15).double()
+            v = (torch.where(e == 0, x / 16 * 2.0 ** -6, (1 + x / 16) * torch.exp2(e.double() - 7)) * s["scales"][i][k, 1].double()) ** 2
         else:
             m, v = s["exp_avg"][i].double().reshape(-1), s["exp_avg_sq"][i].double().reshape(-1)
         m = BETAS[0] * m + (1 - BETAS[0]) * g
