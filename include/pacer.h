@@ -412,12 +412,17 @@ typedef struct {
     void *exp_avg, *exp_avg_sq;   /* m, v: f32, or 8-bit codes */
     float *scales;           /* with 8-bit states: [ceil(numel / 256)][2], else not read */
     int64_t numel;
-    int32_t param_type, grad_type;
+    int32_t param_type;
+    int16_t grad_type;
+    int16_t v_code;          /* with 8-bit states: PACER_V_SQUARE or PACER_V_ROOT, else not read */
 } pacer_adamw_tensor;
+#define PACER_V_SQUARE 0     /* exp_avg_sq holds v */
+#define PACER_V_ROOT 1       /* exp_avg_sq holds sqrt(v) */
 
 /* state_bits 8: m and v are held in blocks of 256 elements, m as sign, 4 exponent and 3 mantissa bits (0, 2^-9 .. 480) times scales[b][0], v as
- * 5 exponent and 3 mantissa bits (0, 2^-18 .. 61440) times scales[b][1]; the block's largest gets the largest code.  The step itself
- * uses the new moments before they are rounded.  A v above 0 does not become 0 (a block whose largest moment is at most 1e-30 is held as
+ * 5 exponent and 3 mantissa bits (0, 2^-18 .. 61440) times scales[b][1], or with PACER_V_ROOT sqrt(v) as 4 exponent and 4 mantissa bits (0, 2^-10 .. 496) times scales[b][1]; the block's largest gets the
+ * largest code.  The step itself
+ * uses the new moments before they are rounded.  A v above 0 does not become 0 (a block whose largest moment, or root, is at most 1e-30 is held as
  * 0).  Codes and scales of 0 are the start.  A NaN or infinite moment spoils its block.
  * seeded: 8-bit states and bf16 parameters are rounded up or down at random, with 16 bits of a hash of (seed, step, the tensor's place
  * in tbl, element), so that the mean is the value; else to nearest.  copies are rounded to nearest.

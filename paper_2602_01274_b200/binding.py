@@ -640,56 +640,76 @@ def pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids=None, bias: float
 # ----------------------------------------------------------------------------- AdamW over many tensors
 
 
+def _adamw_fits(tensors, numel, device):
+    """Whether all is as it has to be (_check_adamw says what is not, ten times as slowly)."""
+    params, copies, exp_avg, exp_avg_sq, scales = tensors
+    if any(x is not None and len(x) != len(params) for x in tensors) or (params and device.type != "cuda"):
+        return False
+    types, state = {p.dtype for p in params}, torch.float32 if scales is None else torch.uint8
+    given = [x for x in (params, exp_avg, exp_avg_sq, scales) if x is not None]
+    if copies is not None:
+        given.append([c for c in copies if c is not None])
+    return types <= {torch.float32, torch.bfloat16} and {t.dtype for x in (exp_avg, exp_avg_sq) for t in x} <= {state} and \
+        all(list(map(torch.Tensor.numel, x)) == numel for x in (params, exp_avg, exp_avg_sq)) and \
+        (copies is None or all(c is None or (c.dtype == torch.bfloat16 and c.numel() == n and p.dtype == torch.float32) for c, n, p in zip(copies, numel, params))) and \
+        (scales is None or all(x.dtype == torch.float32 and x.shape == (-(-n // 256), 2) for x, n in zip(scales, numel))) and \
+        all(all(map(torch.Tensor.is_contiguous, x)) and set(map(torch.Tensor.get_device, x)) <= {device.index} for x in given if x)
+
+
+def _check_adamw(tensors, numel, device):
+    if _adamw_fits(tensors, numel, device):
+        return
+    params, copies, exp_avg, exp_avg_sq, scales = tensors
+    if any(x is not None and len(x) != len(params) for x in tensors):
+        raise AssertionError("AdamwTensors: lists of one length")
+    state = torch.float32 if scales is None else torch.uint8
+    for i, (p, n) in enumerate(zip(params, numel)):
+        if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16)):
+            raise AssertionError(f"param {i}: f32 or bf16 on the GPU")
+        if p.numel() != n:
+            raise AssertionError(f"param {i}: has another size than when it was given")
+        for t, dtype, name in ((exp_avg[i], state, "exp_avg"), (exp_avg_sq[i], state, "exp_avg_sq"), (copies[i] if copies else None, torch.bfloat16, "copy")):
+            if (t is not None or name != "copy") and (t.dtype != dtype or t.numel() != n):
+                raise AssertionError(f"{name} {i}: {dtype} of the param's size")
+        if copies and copies[i] is not None and p.dtype != torch.float32:
+            raise AssertionError(f"copy {i}: only of an f32 param")
+        if scales is not None and (scales[i].dtype != torch.float32 or scales[i].shape != (-(-n // 256), 2)):
+            raise AssertionError(f"scales {i}: torch.float32 [{-(-n // 256)}][2]")
+        for x in tensors:
+            if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == device):
+                raise AssertionError(f"tensors of param {i}: contiguous, on {device}")
+
+
 class AdamwTensors:
     """The tensors of an optimiser as the library takes them, checked once and kept: params f32 or bf16, exp_avg and exp_avg_sq of the same
     sizes (f32; with `scales` uint8 codes, scales f32 [ceil(numel / 256)][2]), copies (bf16, with f32 params) or None; all contiguous, on
-    one GPU.  Holds references to them."""
+    one GPU.  roots: the codes of exp_avg_sq hold the second moments' roots.  Holds references to the tensors."""
 
-    def __init__(self, params, exp_avg, exp_avg_sq, scales=None, copies=None):
+    def __init__(self, params, exp_avg, exp_avg_sq, scales=None, copies=None, roots: bool = False):
         self.tensors = tuple(None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales))
         params = self.tensors[0]
         self.state_bits, n = 32 if scales is None else 8, len(params)
-        if any(x is not None and len(x) != n for x in self.tensors):
-            raise AssertionError("AdamwTensors: lists of one length")
         self.device = params[0].device if n else None
-        self.numel = [p.numel() for p in params]
-        self._check()
+        self.numel = list(map(torch.Tensor.numel, params))
+        _check_adamw(self.tensors, self.numel, self.device)
         self.all = [t for x in self.tensors if x is not None for t in x]
         self.changed = [t for t in self.all if t is not None]
         self._gaps = len(self.changed) < len(self.all)                  # (copies may be missing)
-        # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type)
+        # pacer_adamw_tensor: param, copy, grad, exp_avg, exp_avg_sq, scales, numel, (param_type, grad_type, v_code)
+        self._code = 1 << 48 if roots and scales is not None else 0
         self._types = np.array([_DTYPES[p.dtype] for p in params], dtype=np.int64)
         self.table = np.zeros((n, 8), dtype=np.int64)
-        self.table[:, 6], self.table[:, 7] = self.numel, self._types
+        self.table[:, 6], self.table[:, 7] = self.numel, self._types | self._code
         self._address = self.table.ctypes.data
         self._at = self._grads_at = self._grads_types = None
         self._place()
-
-    def _check(self):
-        params, copies, exp_avg, exp_avg_sq, scales = self.tensors
-        state = torch.float32 if scales is None else torch.uint8
-        for i, (p, n) in enumerate(zip(params, self.numel)):
-            if not (p.is_cuda and p.dtype in (torch.float32, torch.bfloat16)):
-                raise AssertionError(f"param {i}: f32 or bf16 on the GPU")
-            if p.numel() != n:
-                raise AssertionError(f"param {i}: has another size than when it was given")
-            for t, dtype, name in ((exp_avg[i], state, "exp_avg"), (exp_avg_sq[i], state, "exp_avg_sq"), (copies[i] if copies else None, torch.bfloat16, "copy")):
-                if (t is not None or name != "copy") and (t.dtype != dtype or t.numel() != n):
-                    raise AssertionError(f"{name} {i}: {dtype} of the param's size")
-            if copies and copies[i] is not None and p.dtype != torch.float32:
-                raise AssertionError(f"copy {i}: only of an f32 param")
-            if scales is not None and (scales[i].dtype != torch.float32 or scales[i].shape != (-(-n // 256), 2)):
-                raise AssertionError(f"scales {i}: torch.float32 [{-(-n // 256)}][2]")
-            for x in self.tensors:
-                if x is not None and x[i] is not None and not (x[i].is_contiguous() and x[i].device == self.device):
-                    raise AssertionError(f"tensors of param {i}: contiguous, on {self.device}")
 
     def _place(self):
         """The addresses, as they are now: a program may exchange a tensor's storage (which is then looked at again)."""
         at = [0 if t is None else t.data_ptr() for t in self.all] if self._gaps else list(map(torch.Tensor.data_ptr, self.all))
         if at != self._at:
             if self._at is not None:
-                self._check()
+                _check_adamw(self.tensors, self.numel, self.device)
             self._at, n = at, len(self.numel)
             self._types = np.array([_DTYPES[p.dtype] for p in self.tensors[0]], dtype=np.int64)
             self._grads_types = None
@@ -709,7 +729,7 @@ class AdamwTensors:
             self.table[:, 2] = _words(at)
         if types != self._grads_types:
             self._grads_types = types
-            self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32)
+            self.table[:, 7] = self._types | (np.array(types, dtype=np.int64) << 32) | self._code
         return self._address
 
 
@@ -745,46 +765,125 @@ def pacer_grad_norm(grads) -> torch.Tensor:
     return buf.select(0, 0)
 
 
-def pacer_adamw(tensors: AdamwTensors, grads, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, seed=None, norm=None,
-                max_norm: float = 0.0):
-    """An AdamW step over all of `tensors`, in place, in one launch for up to 480 of them.  step (1 for the first) and lr: numbers, or
-    int32 and f32 scalars on the device (for a call that is captured into a graph).  seed: 8-bit states and bf16 params are rounded
-    at random with a hash of it, the step and the element (None: to nearest).  norm: the gradients' global norm (pacer_grad_norm);
-    they are scaled to at most max_norm (0: not at all), and where it is not finite nothing is changed."""
-    if not tensors.numel and not len(grads):
+def pacer_adamw(tensors, grads, *args, **more):
+    """An AdamW step over all of `tensors`, in place, in one launch for up to 480 of them.  Called as
+
+        pacer_adamw(tensors, grads, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, seed=None, norm=None, max_norm=0.0)
+        pacer_adamw(params, grads, exp_avg, exp_avg_sq, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scales=None, copies=None,
+                    seed=None, norm=None, max_norm=0.0, roots=True)
+
+    with AdamwTensors, or with lists of tensors as AdamwTensors takes them, which are then checked in every call.  (As to codes of second
+    moments, lists hold their roots unless roots=False, AdamwTensors hold them as they are unless roots=True.)  step (1 for the first) and lr:
+    numbers, or int32 and f32 scalars on the device (for a call that is captured into a graph).  seed: 8-bit states and bf16 params are
+    rounded at random with a hash of it, the step and the element (None: to nearest).  norm: the gradients' global norm
+    (pacer_grad_norm); they are scaled to at most max_norm (0: not at all), and where it is not finite nothing is changed.  max_norm
+    takes a norm: without one AdamwTensors are refused, lists stepped without scaling."""
+    return (_adamw if isinstance(tensors, AdamwTensors) else _adamw_lists)(tensors, grads, *args, **more)
+
+
+def _adamw(tensors, grads, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, seed=None, norm=None, max_norm=0.0):
+    if tensors.numel or len(grads):
+        _step(tensors, tensors.with_grads(grads), len(tensors.numel), tensors.state_bits, step, lr, betas, eps, weight_decay, seed, norm, max_norm)
+        torch.autograd.graph.increment_version(tensors.changed)         # (as _written)
+
+
+def _adamw_lists(params, grads, exp_avg, exp_avg_sq, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scales=None, copies=None, seed=None,
+                 norm=None, max_norm=0.0, roots=True):
+    tensors = params, copies, exp_avg, exp_avg_sq, scales = tuple(None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales))
+    grads, n = list(grads), len(params)
+    states = _Lists(params, list(map(torch.Tensor.numel, params)))
+    _check_adamw(tensors, states.numel, states.device)
+    if not n and not grads:
         return
-    table = tensors.with_grads(grads)
-    cfg = AdamwCfg(beta_one=betas[0], beta_two=betas[1], eps=eps, weight_decay=weight_decay, max_norm=max_norm, state_bits=tensors.state_bits,
+    if list(map(torch.Tensor.numel, grads)) != states.numel:
+        raise AssertionError("grads: one for each param, of its size")
+    types, at = _gradients(grads, states.device)
+    states.put(2, at)
+    for col, x in ((0, params), (3, exp_avg), (4, exp_avg_sq), (5, scales)):
+        if x is not None:
+            states.put(col, map(torch.Tensor.data_ptr, x))
+    if copies is not None:
+        states.put(1, (0 if c is None else c.data_ptr() for c in copies))
+    code = 1 << 48 if roots and scales is not None else 0
+    states.put(7, (_DTYPES[p.dtype] | t << 32 | code for p, t in zip(params, types if isinstance(types, list) else (types,) * n)))
+    _step(states, states.address, n, 32 if scales is None else 8, step, lr, betas, eps, weight_decay, seed, norm, 0.0 if norm is None else max_norm)
+    _written(*(t for x in tensors if x is not None for t in x))
+
+
+def _step(like, table, n, bits, step, lr, betas, eps, weight_decay, seed, norm, max_norm):
+    cfg = AdamwCfg(beta_one=betas[0], beta_two=betas[1], eps=eps, weight_decay=weight_decay, max_norm=max_norm, state_bits=bits,
                    seeded=seed is not None, seed=0 if seed is None else seed & ((1 << 64) - 1))
     for name, x, dtype in (("step", step, torch.int32), ("lr", lr, torch.float32)):
         if torch.is_tensor(x):
-            assert x.dtype == dtype and x.numel() == 1 and x.device == tensors.device, f"{name}: one {dtype} on {tensors.device}"
+            assert x.dtype == dtype and x.numel() == 1 and x.device == like.device, f"{name}: one {dtype} on {like.device}"
             setattr(cfg, name + "_device", x.data_ptr())
         else:
             setattr(cfg, name, x)
     if norm is not None:
-        assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == tensors.device, f"norm: one torch.float32 on {tensors.device}"
+        assert norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == like.device, f"norm: one torch.float32 on {like.device}"
         cfg.norm = norm.data_ptr()
-    _call(_lib.pacer_adamw, tensors, table, len(tensors.numel), C.byref(cfg))
-    torch.autograd.graph.increment_version(tensors.changed)             # (as _written)
+    _call(_lib.pacer_adamw, like, table, n, C.byref(cfg))
 
 
-def pacer_adamw_states(tensors: AdamwTensors, out=None):
-    """What the 8-bit states stand for: (exp_avg, exp_avg_sq), lists of f32 tensors of the params' sizes, or written to `out` (two lists;
-    contiguous, of those sizes)."""
+class _Lists:
+    """A table of pacer_adamw_tensor for one call, columns as AdamwTensors has them."""
+
+    def __init__(self, like, numel):
+        self.device, self.numel = like[0].device if like else None, numel
+        self.rows = array.array("q", bytes(64 * len(numel)))
+        self.address = self.rows.buffer_info()[0]
+        self.put(6, numel)
+
+    def put(self, col, x):
+        self.rows[col::8] = array.array("q", x)
+
+
+def pacer_adamw_states(tensors, *args, **more):
+    """What 8-bit states stand for: (exp_avg, exp_avg_sq), lists of f32 tensors of the params' sizes, or written to `out` (two lists;
+    contiguous, of those sizes).  Called as
+
+        pacer_adamw_states(tensors, out=None)
+        pacer_adamw_states(exp_avg, exp_avg_sq, scales, out=None, roots=True)
+
+    with AdamwTensors or with lists (see pacer_adamw)."""
+    return (_adamw_states if isinstance(tensors, AdamwTensors) else _adamw_states_lists)(tensors, *args, **more)
+
+
+def _adamw_states_lists(exp_avg, exp_avg_sq, scales, out=None, roots=True):
+    exp_avg, exp_avg_sq, scales = list(exp_avg), list(exp_avg_sq), list(scales)
+    if not len(exp_avg) == len(exp_avg_sq) == len(scales):
+        raise AssertionError("exp_avg, exp_avg_sq, scales: lists of one length")
+    states = _Lists(exp_avg, list(map(torch.Tensor.numel, exp_avg)))
+    for i, (m, v, x, n) in enumerate(zip(exp_avg, exp_avg_sq, scales, states.numel)):
+        if not (m.dtype == v.dtype == torch.uint8 and v.numel() == n and x.dtype == torch.float32 and x.shape == (-(-n // 256), 2)):
+            raise AssertionError(f"states {i}: torch.uint8 of one size, scales torch.float32 [{-(-n // 256)}][2]")
+        if not all(t.is_cuda and t.device == states.device and t.is_contiguous() for t in (m, v, x)):
+            raise AssertionError(f"states {i}: contiguous, on one GPU ({states.device})")
+    for col, x in ((3, exp_avg), (4, exp_avg_sq), (5, scales)):
+        states.put(col, map(torch.Tensor.data_ptr, x))
+    states.put(7, [1 << 48 if roots else 0] * len(exp_avg))
+    return _read_states(states, states.address, exp_avg, out)
+
+
+def _adamw_states(tensors, out=None):
     assert tensors.state_bits == 8, "8-bit states"
-    if out is None:
-        out = tuple([torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in tensors.tensors[0]] for _ in range(2))
-    for x in out:
-        if len(x) != len(tensors.numel):
-            raise AssertionError("out: one for each param")
-        for t, n in zip(x, tensors.numel):
-            if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.device != tensors.device:
-                raise AssertionError(f"out: f32 of the params' sizes, contiguous, on {tensors.device}")
-    if len(tensors.numel):
+    if tensors.numel:
         tensors._place()
+    return _read_states(tensors, tensors._address, tensors.tensors[0], out)
+
+
+def _read_states(states, table, like, out):
+    if out is None:
+        out = tuple([torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in like] for _ in range(2))
+    for x in out:
+        if len(x) != len(states.numel):
+            raise AssertionError("out: one for each param")
+        for t, n in zip(x, states.numel):
+            if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.device != states.device:
+                raise AssertionError(f"out: f32 of the params' sizes, contiguous, on {states.device}")
+    if states.numel:
         m, v = (np.array([t.data_ptr() for t in x], dtype=np.int64) for x in out)
-        _call(_lib.pacer_adamw_states, tensors, tensors._address, len(m), m.ctypes.data, v.ctypes.data)
+        _call(_lib.pacer_adamw_states, states, table, len(m), m.ctypes.data, v.ctypes.data)
         _written(*out[0], *out[1])
     return out
 

@@ -6,8 +6,9 @@
 // The tensors' table travels in the launch's arguments (no copy to the device, nothing to keep), a block finds its chunk's tensor by bisection.
 //
 // States in 8 bits, in blocks of 256 elements, the share of a warp (eight elements a lane).  m: sign, 4 exponent and 3 mantissa bits;
-// v: 5 exponent and 3 mantissa bits (a second moment spans the square of a first one's range); each times a scale of its block, so that
-// the largest gets the largest code.  A code is the upper bits of an f32 number whose exponents were moved down to where the
+// v: 5 exponent and 3 mantissa bits (a second moment spans the square of a first one's range), or its root as 4 exponent and 4 mantissa
+// bits (the same range and steps; a correctly rounded root an element more); each times a scale of its block, so that the largest gets the
+// largest code.  A code is the upper bits of an f32 number whose exponents were moved down to where the
 // code's begin: below them f32 is as evenly spaced as the code, so that coding is one multiplication, an addition and a shift, subnormal values
 // included.  What the shift drops decides the rounding: half of it added is rounding to nearest (halves up), 16 random bits added make
 // the mean of the code the value.  Rounded to nearest, b2 = 0.999 cannot move a v with steps of an eighth as it should: after 2000 steps its mean
@@ -32,8 +33,15 @@ using namespace tw;
 typedef __nv_bfloat16 bf16;
 
 constexpr int THREADS_W = 256, PASS = 8 * THREADS_W, CHUNK = 4 * PASS;
-constexpr float TOP_M = 480.f, TOP_V = 61440.f, LEAST = 1e-30f;
-constexpr float DOWN_M = 0x1p-120f, UP_M = 0x1p120f, DOWN_V = 0x1p-111f, UP_V = 0x1p111f;
+constexpr int WIDE = 32, SQUARES = 8, ROOTS = 9;           // how states are held: f32; 8-bit codes, v as it is or by its root
+// What is held in codes: m, v, the root of v.  The largest code's value, the factors that move exponents to where the code's begin and back, the
+// bits of an f32 number below its code.
+enum Kind { M, V, R };
+template <Kind K> struct Code {
+    static constexpr float TOP = K == M ? 480.f : K == V ? 61440.f : 496.f, DOWN = K == V ? 0x1p-111f : 0x1p-120f, UP = K == V ? 0x1p111f : 0x1p120f;
+    static constexpr int SHIFT = K == R ? 19 : 20;
+};
+constexpr float LEAST = 1e-30f;
 
 struct Item {
     void *param;
@@ -171,16 +179,16 @@ __device__ __forceinline__ void scale2(float (&x)[8], float f) {
 }
 
 // What eight codes stand for.  The move of the exponents and the scale are one factor, unless that would overflow.
-template <bool SIGNED> __device__ __forceinline__ void values(uint2 c, float scale, float (&x)[8]) {
-    constexpr float UP = SIGNED ? UP_M : UP_V, MOST = SIGNED ? 128.f : 65536.f;
+template <Kind K> __device__ __forceinline__ void values(uint2 c, float scale, float (&x)[8]) {
+    constexpr float MOST = K == V ? 65536.f : 128.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const uint32_t w = k < 4 ? c.x : c.y;
-        if (SIGNED) x[k] = __uint_as_float((uint32_t)((int32_t)(w << (24 - 8 * (k & 3))) >> 4) & 0x87f00000u);
-        else x[k] = __uint_as_float(__byte_perm(w, 0u, (uint32_t)(k & 3) << 8 | 0x4044u) << 4);
+        if (K == M) x[k] = __uint_as_float((uint32_t)((int32_t)(w << (24 - 8 * (k & 3))) >> 4) & 0x87f00000u);
+        else x[k] = __uint_as_float(__byte_perm(w, 0u, (uint32_t)(k & 3) << 8 | 0x4044u) << (Code<K>::SHIFT - 16));
     }
-    if (scale < MOST) scale *= UP;
-    else scale2(x, UP);
+    if (scale < MOST) scale *= Code<K>::UP;
+    else scale2(x, Code<K>::UP);
     scale2(x, scale);
 }
 
@@ -205,7 +213,7 @@ template <int BITS, int PT, int GT> struct In {
 template <int BITS, int PT, int GT, bool VEC> __device__ __forceinline__ void fetch_all(const Item &t, int64_t base, int lane, In<BITS, PT, GT> &in) {
     fetch<VEC, GT>(t.grad, base, lane, t.numel, in.g);
     fetch<VEC, PT>(t.param, base, lane, t.numel, in.p);
-    if (BITS == 32) {
+    if (BITS == WIDE) {
         fetch<VEC, PACER_F32>(t.m, base, lane, t.numel, in.m);
         fetch<VEC, PACER_F32>(t.v, base, lane, t.numel, in.v);
     } else {
@@ -218,16 +226,20 @@ template <int BITS, int PT, int GT, bool VEC> __device__ __forceinline__ void fe
 // key: the tensor's.
 template <int BITS, int PT, int GT, bool SEEDED, bool VEC>
 __device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step &q, uint32_t key, int64_t base, int lane, const In<BITS, PT, GT> &in) {
+    constexpr Kind HELD = BITS == ROOTS ? R : V;
     const int64_t n = t.numel;
     float p[8], g[8], m[8], v[8];
     widen8<GT>(in.g, g);
     widen8<PT>(in.p, p);
-    if (BITS == 32) {
+    if (BITS == WIDE) {
         widen8<PACER_F32>(in.m, m);
         widen8<PACER_F32>(in.v, v);
     } else {
-        values<true>(in.cm, in.scale.x, m);
-        values<false>(in.cv, in.scale.y, v);
+        values<M>(in.cm, in.scale.x, m);
+        values<HELD>(in.cv, in.scale.y, v);
+        if (BITS == ROOTS)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __fmul_rn(v[k], v[k]);
     }
     if (q.clipped) scale2(g, q.clip);
     const Two b1 = two(h.b1, h.b1), c1 = two(h.c1, h.c1), b2 = two(h.b2, h.b2), c2 = two(h.c2, h.c2);
@@ -239,8 +251,13 @@ __device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step
         apart(fma2(mul2(two(m[k], m[k + 1]), b1), one, mul2(x, c1)), m[k], m[k + 1]);
         apart(fma2(mul2(two(v[k], v[k + 1]), b2), one, mul2(mul2(x, x), c2)), v[k], v[k + 1]);
         float r0, r1;
-        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v[k]));
-        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v[k + 1]));
+        if (BITS == ROOTS) {               // (from here on v is its root)
+            r0 = v[k] = __fsqrt_rn(v[k]);
+            r1 = v[k + 1] = __fsqrt_rn(v[k + 1]);
+        } else {
+            asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v[k]));
+            asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v[k + 1]));
+        }
         apart(fma2(two(r0, r1), two(q.s2, q.s2), two(h.eps, h.eps)), r0, r1);
         // (the update is a small part of the parameter: 2^-22 of it is far below the parameter's own rounding)
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(r0));
@@ -249,7 +266,7 @@ __device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step
         apart(fma2(share, two(-q.a, -q.a), mul2(two(p[k], p[k + 1]), two(q.decay, q.decay))), p[k], p[k + 1]);
     }
     uint32_t r[8];
-    constexpr bool seeded = SEEDED && (BITS == 8 || PT == PACER_BF16);
+    constexpr bool seeded = SEEDED && (BITS != WIDE || PT == PACER_BF16);
     if (seeded) {
         // (base is a multiple of 256: the number's lowest bits are the lane's)
         const uint32_t x = (uint32_t)base ^ key ^ ((base >> 32) ? mix((uint32_t)(base >> 32)) : 0u) ^ (uint32_t)(VEC ? lane * 8 : lane);
@@ -281,7 +298,7 @@ __device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step
         }
         store16<VEC>(reinterpret_cast<bf16 *>(t.param), base, lane, n, o);
     }
-    if (BITS == 32) {
+    if (BITS == WIDE) {
         store<VEC>(reinterpret_cast<float *>(t.m), base, lane, n, m);
         store<VEC>(reinterpret_cast<float *>(t.v), base, lane, n, v);
         return;
@@ -292,32 +309,33 @@ __device__ __forceinline__ void update(const Item &t, const Hyper &h, const Step
             if (place<VEC>(base, lane, k) >= n) m[k] = v[k] = 0.f;
     const uint32_t top_m = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(m))), top_v = __reduce_max_sync(0xffffffffu, __float_as_uint(largest(v)));
     float sm, im, sv, iv, um[8], uv[8];
-    scale_of(top_m, TOP_M, 1.f / TOP_M, sm, im);
-    scale_of(top_v, TOP_V, 1.f / TOP_V, sv, iv);
+    scale_of(top_m, Code<M>::TOP, 1.f / Code<M>::TOP, sm, im);
+    scale_of(top_v, Code<HELD>::TOP, 1.f / Code<HELD>::TOP, sv, iv);
 #pragma unroll
     for (int k = 0; k < 8; ++k) { um[k] = m[k]; uv[k] = v[k]; }
-    scale2(um, im); scale2(um, DOWN_M);
-    scale2(uv, iv); scale2(uv, DOWN_V);
+    scale2(um, im); scale2(um, Code<M>::DOWN);
+    scale2(uv, iv); scale2(uv, Code<HELD>::DOWN);
     // A code above the last (the largest, where its quotient was rounded up; NaN) or of 0 with v above 0 is rare, and looked for in a block as a whole.
+    constexpr int SM = Code<M>::SHIFT, SV = Code<HELD>::SHIFT;
     uint32_t low = __float_as_uint(uv[0]);
 #pragma unroll
     for (int k = 1; k < 8; ++k) low = min(low, __float_as_uint(uv[k]));
-    const bool plain = VEC && __reduce_min_sync(0xffffffffu, low) >= 1u << 20 &&
-                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_m), im), DOWN_M)) <= 127u << 20 &&
-                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_v), iv), DOWN_V)) <= 255u << 20;
+    const bool plain = VEC && __reduce_min_sync(0xffffffffu, low) >= 1u << SV &&
+                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_m), im), Code<M>::DOWN)) <= 127u << SM &&
+                       __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(top_v), iv), Code<HELD>::DOWN)) <= 255u << SV;
     uint32_t cm[8], cv[8];                 // the codes in the topmost bytes (m's sign has left)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const uint32_t dm = seeded ? __byte_perm(r[k], 0u, 0x4104) : 1u << 23, dv = seeded ? __byte_perm(r[k], 0u, 0x4324) : 1u << 23;
-        cm[k] = __float_as_uint(um[k]) * 16u + dm;
-        cv[k] = __float_as_uint(uv[k]) * 16u + dv;
+        cm[k] = (__float_as_uint(um[k]) << (24 - SM)) + dm;
+        cv[k] = (__float_as_uint(uv[k]) << (24 - SV)) + dv;
     }
     if (!plain)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint32_t dm = seeded ? (r[k] << 4) & 0xffff0u : 1u << 19, dv = seeded ? (r[k] >> 12) & 0xffff0u : 1u << 19;
-            cm[k] = min(((__float_as_uint(um[k]) & 0x7fffffffu) + dm) >> 20, 127u) << 24;
-            cv[k] = max(min((__float_as_uint(uv[k]) + dv) >> 20, 255u), min(__float_as_uint(v[k]), 1u)) << 24;
+            const uint32_t dm = seeded ? (r[k] & 0xffffu) << (SM - 16) : 1u << (SM - 1), dv = seeded ? r[k] >> 16 << (SV - 16) : 1u << (SV - 1);
+            cm[k] = min(((__float_as_uint(um[k]) & 0x7fffffffu) + dm) >> SM, 127u) << 24;
+            cv[k] = max(min((__float_as_uint(uv[k]) + dv) >> SV, 255u), min(__float_as_uint(v[k]), 1u)) << 24;
         }
     store_codes<VEC>(reinterpret_cast<uint8_t *>(t.m), base, lane, n,
                      make_uint2(top_bytes(cm[0], cm[1], cm[2], cm[3]) | (top_bytes(m) & 0x80808080u), top_bytes(cm[4], cm[5], cm[6], cm[7]) | (top_bytes(m + 4) & 0x80808080u)));
@@ -344,7 +362,7 @@ template <class T> __device__ __forceinline__ int tensor_of(const T &tab, uint32
 __device__ __forceinline__ bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 template <int BITS, int PT, int GT, bool SEEDED, int CAP>
-__global__ void __launch_bounds__(THREADS_W, BITS == 8 ? 3 : 4) k_adamw(const __grid_constant__ Table<CAP> tab) {
+__global__ void __launch_bounds__(THREADS_W, BITS != WIDE ? 3 : 4) k_adamw(const __grid_constant__ Table<CAP> tab) {
     const Hyper &h = tab.h;
     Step q{h.a, h.s2, h.decay, 1.f, false};
     if (h.norm) {
@@ -364,10 +382,10 @@ __global__ void __launch_bounds__(THREADS_W, BITS == 8 ? 3 : 4) k_adamw(const __
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Item &t = tab.t[tensor_of(tab, blockIdx.x)];
     const uint32_t key = mix(h.seed ^ mix(step ^ mix(t.number)));
-    const bool vec = aligned(t.param, 16) && aligned(t.copy, 16) && aligned(t.grad, 16) && aligned(t.m, BITS == 32 ? 16 : 8) && aligned(t.v, BITS == 32 ? 16 : 8);
+    const bool vec = aligned(t.param, 16) && aligned(t.copy, 16) && aligned(t.grad, 16) && aligned(t.m, BITS == WIDE ? 16 : 8) && aligned(t.v, BITS == WIDE ? 16 : 8);
     const int64_t start = (int64_t)(blockIdx.x - t.first) * CHUNK + warp * 256, end = min(start - warp * 256 + CHUNK, t.numel);
     int64_t base = start;
-    if (vec && BITS == 32) {
+    if (vec && BITS == WIDE) {
 #pragma unroll 1
         for (; base + 256 <= end; base += PASS) {
             In<BITS, PT, GT> in;
@@ -411,7 +429,7 @@ template <int BITS, int PT, int GT, bool SEEDED> static cudaError_t launch_sized
     return n <= 16 ? launch<BITS, PT, GT, SEEDED, 16>(tbl, at, n, h, st) : n <= 224 ? launch<BITS, PT, GT, SEEDED, 224>(tbl, at, n, h, st) : launch<BITS, PT, GT, SEEDED, MOST>(tbl, at, n, h, st);
 }
 template <int BITS, int PT, int GT> static cudaError_t launch_some(const pacer_adamw_tensor *tbl, const int *at, int n, const Hyper &h, cudaStream_t st) {
-    if (h.seeded && (BITS == 8 || PT == PACER_BF16)) return launch_sized<BITS, PT, GT, BITS == 8 || PT == PACER_BF16>(tbl, at, n, h, st);
+    if (h.seeded && (BITS != WIDE || PT == PACER_BF16)) return launch_sized<BITS, PT, GT, BITS != WIDE || PT == PACER_BF16>(tbl, at, n, h, st);
     return launch_sized<BITS, PT, GT, false>(tbl, at, n, h, st);
 }
 
@@ -430,20 +448,22 @@ cudaError_t adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg &c
     h.seed = (uint32_t)cfg.seed ^ mix((uint32_t)(cfg.seed >> 32));
     h.step = (uint32_t)cfg.step;
     typedef cudaError_t (*Fn)(const pacer_adamw_tensor *, const int *, int, const Hyper &, cudaStream_t);
-    static const Fn fn[2][2][3] = {
-        {{launch_some<32, PACER_F32, PACER_F32>, launch_some<32, PACER_F32, PACER_BF16>, launch_some<32, PACER_F32, PACER_F16>},
-         {launch_some<32, PACER_BF16, PACER_F32>, launch_some<32, PACER_BF16, PACER_BF16>, launch_some<32, PACER_BF16, PACER_F16>}},
-        {{launch_some<8, PACER_F32, PACER_F32>, launch_some<8, PACER_F32, PACER_BF16>, launch_some<8, PACER_F32, PACER_F16>},
-         {launch_some<8, PACER_BF16, PACER_F32>, launch_some<8, PACER_BF16, PACER_BF16>, launch_some<8, PACER_BF16, PACER_F16>}}};
-    for (int types = 0; types < 6; ++types) {                          // (one launch for each pair of types that there is)
+#define TYPES(BITS)                                                                                                                            \
+    {launch_some<BITS, PACER_F32, PACER_F32>, launch_some<BITS, PACER_F32, PACER_BF16>, launch_some<BITS, PACER_F32, PACER_F16>,                 \
+     launch_some<BITS, PACER_BF16, PACER_F32>, launch_some<BITS, PACER_BF16, PACER_BF16>, launch_some<BITS, PACER_BF16, PACER_F16>}
+    static const Fn fn[3][6] = {TYPES(WIDE), TYPES(SQUARES), TYPES(ROOTS)};
+#undef TYPES
+    const bool coded = cfg.state_bits == 8;
+    for (int kind = 0; kind < (coded ? 12 : 6); ++kind) {              // (one launch for each set of types that there is)
         int at[MOST], k = 0;
+        const int types = kind % 6, roots = kind / 6;
         for (int i = 0; i <= n; ++i) {
             if (k == MOST || (i == n && k)) {
-                const cudaError_t e = fn[cfg.state_bits == 8][types / 3][types % 3](tbl, at, k, h, st);
+                const cudaError_t e = fn[coded ? 1 + roots : 0][types](tbl, at, k, h, st);
                 if (e != cudaSuccess) return e;
                 k = 0;
             }
-            if (i < n && tbl[i].numel && tbl[i].param_type == types / 3 && tbl[i].grad_type == types % 3) at[k++] = i;
+            if (i < n && tbl[i].numel && tbl[i].param_type == types / 3 && tbl[i].grad_type == types % 3 && (!coded || tbl[i].v_code == roots)) at[k++] = i;
         }
     }
     return cudaSuccess;
@@ -456,7 +476,7 @@ struct StateItem {
     const float *scales;
     float *om, *ov;
     int64_t numel;
-    uint32_t first, pad;
+    uint32_t first, roots;
 };
 template <int CAP> struct StateTable {
     int32_t n, pad;
@@ -467,11 +487,18 @@ template <bool VEC> __device__ __forceinline__ void read_states(const StateItem 
     float x[8];
     const float2 s = *reinterpret_cast<const float2 *>(t.scales + (base >> 8) * 2);
     if (t.om) {
-        values<true>(load_codes<VEC>(t.m, base, lane, t.numel), s.x, x);
+        values<M>(load_codes<VEC>(t.m, base, lane, t.numel), s.x, x);
         store<VEC>(t.om, base, lane, t.numel, x);
     }
     if (t.ov) {
-        values<false>(load_codes<VEC>(t.v, base, lane, t.numel), s.y, x);
+        const uint2 c = load_codes<VEC>(t.v, base, lane, t.numel);
+        if (t.roots) {
+            values<R>(c, s.y, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(x[k], x[k]);
+        } else {
+            values<V>(c, s.y, x);
+        }
         store<VEC>(t.ov, base, lane, t.numel, x);
     }
 }
@@ -494,7 +521,7 @@ static cudaError_t launch_states(const pacer_adamw_tensor *tbl, int from, int to
     uint64_t chunks = 0;
     for (int i = from; i < to; ++i) {
         const pacer_adamw_tensor &t = tbl[i];
-        tab.t[tab.n++] = {(const uint8_t *)t.exp_avg, (const uint8_t *)t.exp_avg_sq, t.scales, om ? om[i] : nullptr, ov ? ov[i] : nullptr, t.numel, (uint32_t)chunks, 0};
+        tab.t[tab.n++] = {(const uint8_t *)t.exp_avg, (const uint8_t *)t.exp_avg_sq, t.scales, om ? om[i] : nullptr, ov ? ov[i] : nullptr, t.numel, (uint32_t)chunks, t.v_code == PACER_V_ROOT};
         chunks += (uint64_t)(t.numel + CHUNK - 1) / CHUNK;
     }
     if (!chunks) return cudaSuccess;

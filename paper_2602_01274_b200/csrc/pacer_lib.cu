@@ -1197,6 +1197,7 @@ static const char *bad_states(const pacer_adamw_tensor &t) {
     if (!t.numel) return nullptr;
     if (!t.exp_avg || !t.exp_avg_sq || !t.scales) return "a state is null";
     if (off(t.scales, 8)) return "misaligned scales";
+    if (t.v_code != PACER_V_SQUARE && t.v_code != PACER_V_ROOT) return "unknown code of exp_avg_sq";
     return nullptr;
 }
 static const char *bad_adamw(const pacer_adamw_tensor *tbl, int n, int bits) {
