@@ -7,6 +7,7 @@ than 4096 elements keep f32 states).  With ``seed`` 8-bit states and bf16 parame
 """
 from __future__ import annotations
 
+import operator
 from typing import Optional
 
 import torch
@@ -111,6 +112,19 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p]["step"] = copies.setdefault(id(t), t.clone())
         return buckets
 
+    def _table(self, key, ps, st, coded):
+        """The tensors that a call takes, kept between steps while the state holds these very ones (a program may drop or exchange them)."""
+        copies = [p if "master" in s else None for p, s in zip(ps, st)]
+        now = ([s.get("master", p) for p, s in zip(ps, st)], copies if any(c is not None for c in copies) else None, [s["exp_avg"] for s in st],
+               [s["exp_avg_sq"] for s in st], [s["scales"] for s in st] if coded else None)
+        kept = self._tables.get(key)
+        if kept is None or not all(x is y or (x is not None and y is not None and all(map(operator.is_, x, y))) for x, y in zip(kept.tensors, now)):
+            if kept is not None or len(self._tables) >= 64:             # (others may hold on to what was dropped; programs whose parameters take turns)
+                self._tables.clear()
+            params, copies, exp_avg, exp_avg_sq, scales = now
+            kept = self._tables[key] = binding.AdamwTensors(params, exp_avg, exp_avg_sq, scales, copies)
+        return kept
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
@@ -132,14 +146,6 @@ class AdamW(torch.optim.Optimizer):
                 self.state[p]["step"] += 1
         for (gi, device, _, coded), ps in buckets.items():
             group, st = self.param_groups[gi], [self.state[p] for p in ps]
-            key = (gi, device, coded, *map(id, ps))
-            if key not in self._tables:
-                if len(self._tables) >= 64:                             # (programs whose parameters take turns)
-                    self._tables.clear()
-                copies = [p if "master" in s else None for p, s in zip(ps, st)]
-                self._tables[key] = binding.AdamwTensors([s.get("master", p) for p, s in zip(ps, st)], [s["exp_avg"] for s in st],
-                                                         [s["exp_avg_sq"] for s in st], [s["scales"] for s in st] if coded else None,
-                                                         copies if any(c is not None for c in copies) else None)
-            binding.pacer_adamw(self._tables[key], [grads[p] for p in ps], st[0]["step"], group["lr"], group["betas"], group["eps"],
-                                group["weight_decay"], self.seed, norm, self.max_norm)
+            binding.pacer_adamw(self._table((gi, device, coded, *map(id, ps)), ps, st, coded), [grads[p] for p in ps], st[0]["step"], group["lr"],
+                                group["betas"], group["eps"], group["weight_decay"], self.seed, norm, self.max_norm)
         return loss

@@ -1,0 +1,78 @@
+"""The optimiser when a program changes its state, loads one, or captures its first step."""
+from collections import defaultdict
+
+import pytest
+import torch
+
+from tests.test_gpu_adamw import DEV, gen
+
+pytestmark = pytest.mark.gpu
+SIZES = (5000, 300, 70000)
+
+
+def params(dtype=torch.bfloat16):
+    return [torch.nn.Parameter(torch.randn(n, generator=gen(n), device=DEV).to(dtype)) for n in SIZES]
+
+
+def run(opt, ps, ks):
+    for k in ks:
+        for i, p in enumerate(ps):
+            x = torch.randn(p.shape, generator=gen(100 + 10 * k + i), device=DEV).to(p.dtype)
+            p.grad = x if p.grad is None else p.grad.copy_(x)
+        opt.step()
+
+
+def clones(ps):
+    return [torch.nn.Parameter(p.detach().clone()) for p in ps]
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+@pytest.mark.parametrize("capturable", [False, True])
+@pytest.mark.parametrize("how", ["clear", "new dict", "pop"])
+def test_state_started_anew(states, capturable, how):
+    """An optimiser whose state was dropped goes on as a new one does."""
+    from paper_2602_01274_b200 import optim
+    a = params()
+    oa = optim.AdamW(a, lr=1e-3, states=states, seed=4, capturable=capturable)
+    run(oa, a, range(3))
+    with torch.no_grad():
+        for p in a:                                                         # (weights of another place, no longer the masters')
+            p.mul_(0.5)
+    b = clones(a)
+    if how == "clear":
+        oa.state.clear()
+    elif how == "new dict":
+        oa.state = defaultdict(dict)
+    else:
+        for p in a:
+            oa.state.pop(p)
+    ob = optim.AdamW(b, lr=1e-3, states=states, seed=4, capturable=capturable)
+    run(oa, a, range(3, 6))
+    run(ob, b, range(3, 6))
+    for p, q in zip(a, b):
+        assert torch.equal(p, q)
+        assert oa.state[p].keys() == ob.state[q].keys()
+        for name in oa.state[p]:
+            x, y = oa.state[p][name], ob.state[q][name]
+            assert torch.equal(x, y) if torch.is_tensor(x) else x == y, name
+
+
+@pytest.mark.parametrize("name", ["exp_avg", "exp_avg_sq", "scales", "master"])
+def test_entry_of_the_state_exchanged(name):
+    """A tensor put into the state is the one that the next steps read and write."""
+    from paper_2602_01274_b200 import optim
+    a = params()
+    oa = optim.AdamW(a, lr=1e-3, states="8bit" if name == "scales" else "f32", seed=4)
+    run(oa, a, range(2))
+    b = clones(a)
+    ob = optim.AdamW(b, lr=1e-3, states="8bit" if name == "scales" else "f32", seed=4)
+    ob.load_state_dict(oa.state_dict())
+    old = oa.state[a[0]][name]
+    for o, ps in ((oa, a), (ob, b)):
+        o.state[ps[0]][name] = o.state[ps[0]][name] * 0.5                   # the one after steps, the other before its first
+    new, kept, before = oa.state[a[0]][name], old.clone(), oa.state[a[0]][name].clone()
+    run(oa, a, range(2, 4))
+    run(ob, b, range(2, 4))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert oa.state[a[0]][name] is new and not torch.equal(new, before) and torch.equal(old, kept)
+    assert all(torch.equal(oa.state[a[0]][k], ob.state[b[0]][k]) for k in ("exp_avg", "exp_avg_sq", "master"))
