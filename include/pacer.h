@@ -394,7 +394,10 @@ int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const vo
 
 /* Softmax cross entropy of given tokens straight from hidden rows and head, without keeping the logits, and its gradients in the same
  * call: loss[r] = lse - z[tokens[r]] (f32 [rows]; 0 where the token names nothing; may be NULL), dhidden and dhead (each may be NULL)
- * of sum_r weight[r] loss[r].  Arguments otherwise as above.  Where dz of the whole vocabulary fits 2 GB the logits are computed once, else twice. */
+ * of sum_r weight[r] loss[r].  Arguments otherwise as above. 
+ * Where dz of the whole vocabulary fits 2 GB the logits are computed once, else twice.  Computed once, each share of a row's mass is kept in 11
+ * bits until the row's sum is known, then rounded to bf16 (and remainder) as above; a share below 2^-62 of the largest of some 128 tokens next to
+ * it counts as 0. */
 size_t pacer_head_nll_grad_scratch_bytes(int rows, int vocab, int d);
 int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
                         const int32_t *tokens, const int32_t *bias_ids, float bias, const float *weight, float *loss, void *dhidden,

@@ -13,8 +13,6 @@
 // (m, sum 2^t, sum 2^t t), t = (z - m) log2(e), in the scratch, and a second kernel joins a row's halves.
 #include "head_score.h"
 
-#include <cuda_fp16.h>
-
 #include <algorithm>
 
 #include "pair.cuh"
@@ -41,6 +39,11 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_REF = -3.402823466e38f, SLACK = 11.f, FAR = -1000.f;
 constexpr float OUTSIDE = -1e30f;          // a logit past the vocabulary: 2^t is 0, and t finite
 
+// A share 2^t, t at most 0, is kept as 16 of the bits of 2^t KEEP_DOWN: 6 exponent and 10 mantissa bits (there is no sign, and no exponent above
+// that of 1), so that 11 bits of it are right down to 2^-62, 43 nats below the half tile's largest.  fp16's 5 exponent bits were not enough: 14 nats
+// below, dhead's row of a token that is rare in all rows was 2 % off, from 18 on it was 0.
+constexpr float KEEP_DOWN = 0x1p-64f, KEEP_UP = 0x1p64f;
+constexpr uint32_t KEEP_MASK = 0xffffu << 13;
 struct Part { float m, S, S2, pad; };
 
 struct KArgs {
@@ -49,7 +52,7 @@ struct KArgs {
     float bias;
     Part *part;                            // [rows][2 * nt]
     float *ztok;                           // [rows]
-    __half *keep;                          // [rows][ld_keep], or NULL (see k_head_dz)
+    uint16_t *keep;                        // [rows][ld_keep], or NULL: 2^t in codes (see KEEP_DOWN)
     int32_t ld_keep;
 };
 
@@ -245,14 +248,14 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                         x0 = ex2(x0);
                         x1 = ex2(x1);
                         sum = add2(sum, two(x0, x1));
-                        const __half2 h = __floats2half2_rn(x0, x1);
-                        w[e >> 1] = *reinterpret_cast<const uint32_t *>(&h);
+                        apart(mul2(two(x0, x1), two(KEEP_DOWN, KEEP_DOWN)), x0, x1);
+                        w[e >> 1] = __byte_perm(__float_as_uint(x0) * 8u + 0x8000u, __float_as_uint(x1) * 8u + 0x8000u, 0x7632);
                     }
                     float S0, S1;
                     apart(sum, S0, S1);
                     s.S += S0 + S1;
                     if (live) {
-                        __half *p = a.keep + (size_t)r * a.ld_keep + n0 + at;
+                        uint16_t *p = a.keep + (size_t)r * a.ld_keep + n0 + at;
                         st32(p, w);
                         st32(p + 16, w + 8);
                     }
@@ -304,11 +307,11 @@ __global__ void __launch_bounds__(128) k_head_join(const KArgs a, float *logp, f
 }
 
 // The gradient of sum_r weight_r (lse_r - z_r[token_r]) with respect to the logits, in place of what k_head_score kept: a block joins its row's
-// parts and takes a piece of the row.  What was kept has 11 bits (of a share of its half tile's largest; below 2^-14 of that fewer, below
-// 2^-25 nothing: next to the largest of the row's gradients that is far below a half step of bf16, the row's token being left out), so that
-// rounding it to bf16 after the row's factor is known is the only rounding that shows.  Kept in bf16 and scaled, it was rounded twice, and the products'
-// errors were 1.7 times those of exact gradients rounded at the end (1.4 with one rounding).  The token's 1 - p is the others' share, and its
-// loss log(1 + others / its own) where it has the largest logit: confident rows lose nothing.  low: the remainders bf16(x - bf16(x)), or NULL.
+// parts and takes a piece of the row.  What was kept has 11 bits, so that rounding it to bf16 after the row's factor is known is the only
+// rounding that shows (2^-11 of a gradient beside 2^-8; what is below 2^-62 of its half tile's largest, the row's token left out, loses bits
+// and becomes 0).  Kept in bf16 and scaled, it was rounded twice, and the products' errors were 1.7 times those of exact gradients rounded at
+// the end (1.4 with one rounding).  The token's 1 - p is the others' share, and its loss log(1 + others / its own) where it has the
+// largest logit: confident rows lose nothing.  low: the remainders bf16(x - bf16(x)), or NULL.
 struct DzArgs {
     int32_t segs, seg;                     // pieces of a row and their columns, a multiple of 8
     uint32_t by_bn;                        // 2^32 / bn, rounded up (exact quotients below 2^32 / bn)
@@ -369,8 +372,8 @@ __global__ void __launch_bounds__(THREADS_D) k_head_dz(const KArgs a, const DzAr
         uint32_t o[4], r[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float2 x = __half22float2(*reinterpret_cast<const __half2 *>(w + e));
-            apart(mul2(two(x.x, x.y), ff), x.x, x.y);
+            float2 x = make_float2(__uint_as_float(w[e] << 13 & KEEP_MASK), __uint_as_float(w[e] >> 3 & KEEP_MASK));
+            apart(mul2(mul2(two(x.x, x.y), two(KEEP_UP, KEEP_UP)), ff), x.x, x.y);
             const __nv_bfloat162 b = __floats2bfloat162_rn(x.x, x.y);
             o[e] = *reinterpret_cast<const uint32_t *>(&b);
             if (LOW) {
@@ -454,7 +457,7 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, cudaStream_t st, bool *n
     k.tokens = a.tokens; k.bias_ids = a.bias_ids; k.bias = a.bias;
     k.part = reinterpret_cast<Part *>(scratch);
     k.ztok = reinterpret_cast<float *>(k.part + (size_t)a.rows * (2 * t.nt));
-    k.keep = reinterpret_cast<__half *>(a.dz); k.ld_keep = a.ld_dz;
+    k.keep = reinterpret_cast<uint16_t *>(a.dz); k.ld_keep = a.ld_dz;
     CUtensorMap ma, mb;
     if (!make_map(encode, &ma, a.hidden, a.ld_hidden, a.rows, a.d, k.a_rows) || !make_map(encode, &mb, a.head, a.ld_head, a.vocab, a.d, t.pair ? t.bn / 2 : t.bn)) {
         *no_maps = true;
