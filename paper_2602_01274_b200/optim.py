@@ -20,7 +20,8 @@ SMALL = 4096                       # elements below which a tensor's states stay
 class AdamW(torch.optim.Optimizer):
     """max_norm: the gradients of all groups are scaled to at most this global norm (0: not at all); a step whose norm is not finite changes
     nothing but the count.  capturable: the count is kept on the device and lr may be an f32 scalar there, so that ``step`` can be
-    captured into a CUDA graph (gradients must then stay where they are: zero them, don't drop them)."""
+    captured into a CUDA graph, each parameter's first step excepted, which makes its state (gradients must then stay where they are: zero
+    them, don't drop them)."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, *, states: str = "f32",
                  master: bool = True, seed: Optional[int] = None, max_norm: float = 0.0, capturable: bool = False):
@@ -53,6 +54,8 @@ class AdamW(torch.optim.Optimizer):
         """fresh: the count that parameters met for the first time in this step share, by device."""
         s = self.state[p]
         if not s:
+            if torch.cuda.is_current_stream_capturing():                # (a replay would set the moments to 0 again)
+                raise RuntimeError("AdamW: a captured step has to come after a first one of each of its parameters")
             small = self.states == "f32" or p.numel() < SMALL
             s["step"] = 0
             if self.capturable:
@@ -131,6 +134,8 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        if not self.capturable and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW: captured steps need capturable=True (else every replay has the count and rate of now)")
         buckets = self._buckets()
         grads = {p: p.grad.contiguous() for ps in buckets.values() for p in ps}
         norm = None

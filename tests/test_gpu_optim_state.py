@@ -76,3 +76,31 @@ def test_entry_of_the_state_exchanged(name):
     assert all(torch.equal(p, q) for p, q in zip(a, b))
     assert oa.state[a[0]][name] is new and not torch.equal(new, before) and torch.equal(old, kept)
     assert all(torch.equal(oa.state[a[0]][k], ob.state[b[0]][k]) for k in ("exp_avg", "exp_avg_sq", "master"))
+
+
+def test_first_step_is_not_captured():
+    """Its zeroed moments and counts would be part of the graph: every replay would be a first step.  Nor is one whose count is on the host."""
+    from paper_2602_01274_b200 import optim
+    a = params(torch.float32)
+    o = optim.AdamW(a, lr=1e-3, capturable=True)
+    for p in a:
+        p.grad = torch.ones_like(p)
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(RuntimeError, match="after a first one"):
+            o.step()
+    a[1].grad = None
+    o.step()
+    assert not o.state.get(a[1]) and int(o.state[a[0]]["step"]) == 1
+    a[1].grad = torch.ones_like(a[1])
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(RuntimeError, match="after a first one"):
+            o.step()
+    o.step()                                                                # and goes on as if nothing had been
+    assert [int(o.state[p]["step"]) for p in a] == [2, 1, 2]
+    b = params(torch.float32)
+    h = optim.AdamW(b, lr=1e-3)
+    run(h, b, range(1))
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(RuntimeError, match="capturable"):
+            h.step()
+    assert h.state[b[0]]["step"] == 1
