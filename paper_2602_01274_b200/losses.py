@@ -116,13 +116,13 @@ class _HeadNll(torch.autograd.Function):
     def forward(ctx, hidden, head, tokens, weight, bias_ids, bias, train):
         grads = ctx.needs_input_grad[:2] if train else (False, False)
         loss, dhidden, dhead = binding.pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids, bias, grads=grads)
-        ctx.grads = dhidden, dhead, loss if ctx.needs_input_grad[3] else None
+        ctx.save_for_backward(dhidden, dhead, loss if ctx.needs_input_grad[3] else None)        # (freed by the backward pass)
         return (loss * weight).sum()
 
     @staticmethod
     @once_differentiable
     def backward(ctx, g):
-        dhidden, dhead, loss = (None if x is None else x * g for x in ctx.grads)
+        dhidden, dhead, loss = (None if x is None else x * g for x in ctx.saved_tensors)
         return dhidden, dhead, None, loss, None, None, None
 
 
