@@ -96,9 +96,13 @@ __device__ __forceinline__ void drain(Pair &s, int n, int rank) {
     for (int j = max(0, n - STAGES); j < n && rank == 0; ++j)
         for (unsigned it = 0; it < MBAR_SPIN_LIMIT && !mbar_try_wait(s.full + j % STAGES, ((uint32_t)(j / STAGES)) & 1u); ++it) {}
 }
-// blocks: k blocks that are worked on meanwhile (a tile's sums over a million rows or tokens take milliseconds).
+// k blocks that are worked on meanwhile: a tile's sums over a million rows or tokens take milliseconds.  (An empty share's may be below 0: one of 4
+// shares of the last 283 of 2 093 339 tokens.)
+__host__ __device__ constexpr unsigned wait_limit(int blocks) { return MBAR_SPIN_LIMIT * (1u + (unsigned)(blocks > 0 ? blocks : 0) / 1024u); }
+static_assert(wait_limit(-1) == MBAR_SPIN_LIMIT && wait_limit(-64) == MBAR_SPIN_LIMIT && wait_limit(1023) == MBAR_SPIN_LIMIT, "the usual wait");
+static_assert(wait_limit(1 << 15) == 33 * MBAR_SPIN_LIMIT, "2^21 tokens or rows");
 __device__ __forceinline__ bool all_wait(Pair &s, uint64_t *bar, uint32_t parity, int blocks = 0) {
-    return __all_sync(0xffffffffu, wait_h(&s.gave_up, bar, parity, MBAR_SPIN_LIMIT * (1u + (unsigned)blocks / 1024u)));
+    return __all_sync(0xffffffffu, wait_h(&s.gave_up, bar, parity, wait_limit(blocks)));
 }
 __device__ __forceinline__ uint32_t pair_idesc(int n) { return (umma_idesc(n) & ~(31u << 24)) | (256u >> 4) << 24; }
 // An MN-major operand in the 128-byte swizzle: rows (k) of 64 channels, eight of them 1 KB, the next 64 channels a panel further.
