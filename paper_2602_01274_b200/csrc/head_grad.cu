@@ -201,7 +201,10 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                 tmem_ld32(acc + at, v);
                 if ((uint32_t)(bid - at) < 32u)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + (bid - at == e ? a.bias : 0.f));
+                    for (int e = 0; e < 32; ++e) {                     // (no lower than -1e30: 2^t is 0, and t finite)
+                        const float z = __uint_as_float(v[e]) + a.bias;
+                        v[e] = bid - at == e ? __float_as_uint(z < -1e30f ? -1e30f : z) : v[e];
+                    }
                 uint32_t w[16], l16[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {

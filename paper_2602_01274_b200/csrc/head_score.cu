@@ -37,7 +37,7 @@ constexpr int EPI_WARPS = 8, THREADS_H = 32 * (EPI_WARPS + 2), SMEM_H = 192 * 10
 static_assert(Cfg<true>::STAGE * Cfg<true>::STAGES == 192 * 1024 && Cfg<false>::STAGE * Cfg<false>::STAGES == 192 * 1024, "the stages");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_REF = -3.402823466e38f, SLACK = 11.f, FAR = -1000.f;
-constexpr float OUTSIDE = -1e30f;          // a logit past the vocabulary: 2^t is 0, and t finite
+constexpr float OUTSIDE = -1e30f;          // a logit past the vocabulary, or below this by its bias: 2^t is 0, and t finite
 
 // A share 2^t, t at most 0, is kept as 16 of the bits of 2^t KEEP_DOWN: 6 exponent and 10 mantissa bits (there is no sign, and no exponent above
 // that of 1), so that 11 bits of it are right down to 2^-62, 43 nats below the half tile's largest.  fp16's 5 exponent bits were not enough: 14 nats
@@ -209,6 +209,9 @@ __global__ void __launch_bounds__(THREADS_H, 1) k_head_score(const __grid_consta
                         for (int e = 0; e < 32; ++e) x = tok - at == e ? v[e] : x;
                         a.ztok[r] = x;
                     }
+                    if ((uint32_t)(bid - at) < 32u)                   // (a bias of -infinity, say)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = bid - at == e && v[e] < OUTSIDE ? OUTSIDE : v[e];
                     if (left < 32)                                    // columns past the vocabulary
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = e < left ? v[e] : OUTSIDE;
