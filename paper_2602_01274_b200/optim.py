@@ -2,8 +2,9 @@
 training programs.
 
 Parameters are f32 or bf16, contiguous, on GPUs; gradients f32, bf16 or f16.  A bf16 parameter has an f32 master among the states,
-unless ``master=False``.  States are f32, or with ``states="8bit"`` 8-bit codes with a scale for 256 elements (tensors of fewer
-than 4096 elements keep f32 states).  With ``seed`` 8-bit states and bf16 parameters without a master are rounded at random.
+unless ``master=False``.  States are f32, or with ``states="8bit"`` 8-bit codes with a scale for 256 elements
+(tensors of fewer than 4096 elements keep f32 states).  With ``seed`` 8-bit states and bf16 parameters without a master are rounded
+at random.
 """
 from __future__ import annotations
 
@@ -71,8 +72,17 @@ class AdamW(torch.optim.Optimizer):
         return s
 
     def load_state_dict(self, state_dict):
-        """States keep their types (torch would take them to their parameter's)."""
-        super().load_state_dict(state_dict)
+        """States keep their types (torch would take them to their parameter's).  Registered hooks run as torch's do: ours see what the ones before loading return, and are done before those after it."""
+        seen = []
+        last = self.register_load_state_dict_pre_hook(lambda _, d: seen.append(d))
+        first = self.register_load_state_dict_post_hook(lambda _: self._take(seen[-1]), prepend=True)
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            last.remove()
+            first.remove()
+
+    def _take(self, state_dict):
         params = [p for g in self.param_groups for p in g["params"]]
         place = dict(zip([n for g in state_dict["param_groups"] for n in g["params"]], params))
         counts = {}

@@ -104,3 +104,28 @@ def test_first_step_is_not_captured():
         with pytest.raises(RuntimeError, match="capturable"):
             h.step()
     assert h.state[b[0]]["step"] == 1
+
+
+def test_hooks_of_loading():
+    """What a pre-hook returns is what is loaded; a post-hook sees states of their own types."""
+    from paper_2602_01274_b200 import optim
+    a = params()
+    oa = optim.AdamW(a, lr=1e-3, states="8bit", seed=4)
+    run(oa, a, range(2))
+    saved = oa.state_dict()
+    b = clones(a)
+    ob = optim.AdamW(b, lr=1e-3, states="8bit", seed=4)
+    seen = []
+
+    def nested(_, d):                                                       # (a checkpoint with a level of its own, counts moved on)
+        return {**d["optimizer"], "state": {k: {**s, "step": s["step"] + 5} for k, s in d["optimizer"]["state"].items()}}
+
+    ob.register_load_state_dict_pre_hook(nested)
+    ob.register_load_state_dict_post_hook(lambda o: seen.extend((o.state[p]["exp_avg"].dtype, o.state[p]["step"]) for p in b))
+    ob.load_state_dict({"optimizer": saved, "param_groups": saved["param_groups"], "state": {}})
+    assert seen == [(torch.uint8, 7), (torch.float32, 7), (torch.uint8, 7)]
+    for p in a:
+        oa.state[p]["step"] += 5
+    run(oa, a, range(2, 4))
+    run(ob, b, range(2, 4))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
