@@ -2,7 +2,8 @@
 training programs.
 
 Parameters are f32 or bf16, contiguous, on GPUs; gradients f32, bf16 or f16.  A bf16 parameter has an f32 master among the states,
-unless ``master=False``.  States are f32, or with ``states="8bit"`` 8-bit codes with a scale for 256 elements
+unless ``master=False``; the parameter is that master rounded, so that a program which writes to it between steps has to write
+``state[p]["master"]`` too, or drop the state.  States are f32, or with ``states="8bit"`` 8-bit codes with a scale for 256 elements
 (tensors of fewer than 4096 elements keep f32 states).  With ``seed`` 8-bit states and bf16 parameters without a master are rounded
 at random.
 """
@@ -72,7 +73,8 @@ class AdamW(torch.optim.Optimizer):
         return s
 
     def load_state_dict(self, state_dict):
-        """States keep their types (torch would take them to their parameter's).  Registered hooks run as torch's do: ours see what the ones before loading return, and are done before those after it."""
+        """States keep their types (torch would take them to their parameter's); a bf16 parameter whose state has no master gets one of its value
+        now.  Registered hooks run as torch's do: ours see what the ones before loading return, and are done before those after it."""
         seen = []
         last = self.register_load_state_dict_pre_hook(lambda _, d: seen.append(d))
         first = self.register_load_state_dict_post_hook(lambda _: self._take(seen[-1]), prepend=True)
@@ -98,6 +100,8 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p][name] = counts[key]
                 else:
                     self.state[p][name] = int(x)
+            if held and p.dtype == torch.bfloat16 and self.master and "master" not in held:
+                self.state[p]["master"] = p.detach().float()
         self._tables = {}
 
     def _buckets(self):

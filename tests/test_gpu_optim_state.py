@@ -129,3 +129,32 @@ def test_hooks_of_loading():
     run(oa, a, range(2, 4))
     run(ob, b, range(2, 4))
     assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_states_without_masters():
+    """Moments of an optimiser that had none: bf16 parameters go on from their value as masters."""
+    from paper_2602_01274_b200 import optim
+    a = params()
+    theirs = torch.optim.AdamW([torch.nn.Parameter(p.detach().float()) for p in a], lr=1e-3)
+    for p, q in zip(a, theirs.param_groups[0]["params"]):
+        q.grad = torch.ones_like(q)
+    theirs.step()
+    o = optim.AdamW(a, lr=1e-6)
+    o.load_state_dict(theirs.state_dict())
+    for g in o.param_groups:
+        g.update(lr=1e-6, weight_decay=0.0)
+    start = [p.detach().clone() for p in a]
+    for p in a:
+        p.grad = torch.ones_like(p)
+    for _ in range(3):
+        o.step()
+    for p, x in zip(a, start):
+        m = o.state[p]["master"]
+        assert m.dtype == torch.float32 and o.state[p]["step"] == 4
+        # (three updates of 1e-6 each, far below a bf16 step: the master holds them)
+        assert ((x.float() - m) - 3e-6).abs().max() < 2 * 2.0 ** -24 * float(m.abs().max()) * 3 + 1e-8 and torch.equal(p.detach(), m.to(torch.bfloat16))
+    # without masters where none are asked for
+    o = optim.AdamW(a, lr=1e-6, master=False)
+    o.load_state_dict(theirs.state_dict())
+    o.step()
+    assert "master" not in o.state[a[0]]
