@@ -158,3 +158,22 @@ def test_states_without_masters():
     o.load_state_dict(theirs.state_dict())
     o.step()
     assert "master" not in o.state[a[0]]
+
+
+def test_rounding_at_random_unless_nearest_is_asked_for():
+    """Second moments in 8 bits whose gradients become smaller: their mean follows that of f32 states (the bound of
+    test_gpu_adamw.test_8_bit_second_moments_follow), to nearest it does not."""
+    from paper_2602_01274_b200 import binding, optim
+    n, means = 1 << 14, {}
+    for name, more in (("f32", {}), ("8bit", dict(states="8bit")), ("nearest", dict(states="8bit", seed=None))):
+        p = torch.nn.Parameter(torch.zeros(n, device=DEV))
+        o = optim.AdamW([p], lr=1e-4, **more)
+        g = gen(4)
+        for k in range(600):
+            p.grad = torch.randn(n, generator=g, device=DEV) * (1.0 if k < 200 else 0.25)
+            o.step()
+        s = o.state[p]
+        v = s["exp_avg_sq"] if name == "f32" else binding.pacer_adamw_states([s["exp_avg"]], [s["exp_avg_sq"]], [s["scales"]], roots=False)[1][0]
+        means[name] = float(v.double().mean())
+    bound = 6 * (500 / n) ** 0.5 / 16
+    assert abs(means["8bit"] / means["f32"] - 1) < bound < abs(means["nearest"] / means["f32"] - 1)
