@@ -381,7 +381,8 @@ int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head,
  * pacer_head_logprobs left them for the same hidden, head, tokens and bias.  Each of g_logp, g_entropy, g_lse (f32 [rows]) may be
  * NULL, not all three; tokens and logp may be NULL where g_logp is, entropy where g_entropy is.  A row whose token names nothing has
  * no g_logp term.  dz is rounded to bf16 once, as an operand of the products (up to 128 rows its rounding remainders are multiplied too); their
- * sums are fp32.  It is kept for as many tokens at a time as 2 GB holds, so that the scratch stays bounded for any number of rows.
+ * sums are fp32, over at most 16 384 terms (8192 columns of a logit) inside the tensor cores, which truncate: 2^-23 of a sum for 16 terms at
+ * most.  1 - p of a row's token is taken from logp, and so off by some 2^-24 of 1, however small it is.  dz is kept for as many tokens at a time as 2 GB holds, so that the scratch stays bounded for any number of rows.
  * Addresses 16-byte aligned, strides multiples of 8; the gradients overlap neither the operands nor each other.  rows = 0 sets dhead
  * to 0.  scratch: device, 256-byte aligned, at least pacer_head_logprobs_backward_scratch_bytes(rows, vocab, d) bytes, in use until the
  * call's kernels have run.  Inputs must be finite; a wait inside a kernel that ran out makes results NaN.  No atomics: the same call gives the
@@ -398,7 +399,7 @@ int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const vo
  * of sum_r weight[r] loss[r].  Arguments otherwise as above. 
  * Where dz of the whole vocabulary fits 2 GB the logits are computed once, else twice.  Computed once, each share of a row's mass is kept in 11
  * bits until the row's sum is known, then rounded to bf16 (and remainder) as above; a share below 2^-62 of the largest of some 128 tokens next to
- * it counts as 0. */
+ * it counts as 0.  1 - p of a row's token, and its loss where it leads, are then right relative to themselves; computed twice, as above. */
 size_t pacer_head_nll_grad_scratch_bytes(int rows, int vocab, int d);
 int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
                         const int32_t *tokens, const int32_t *bias_ids, float bias, const float *weight, float *loss, void *dhidden,

@@ -10,8 +10,8 @@
 //   k_head_sum   dhidden from partial sums, where its product was cut along the vocabulary
 // For the loss and its gradients in one call dz comes out of the loss's own pass (k_head_dz in head_score.cu): 2048 x 32 000 x 4096 1270 us, with
 // z computed twice 1690.
-// dz is rounded once, to bf16, as an operand has to be; sums are fp32.  1 - p of the row's token is -expm1(logp), so that confident
-// rows lose nothing to the difference.
+// dz is rounded once, to bf16, as an operand has to be; sums are fp32.  1 - p of the row's token is -expm1(logp), off by what logp is: some 2^-24 of 1,
+// of the f32 sum that it is the logarithm of.  (k_head_dz, which has the others' sum by itself, is off by that share of 1 - p.)
 #include "head_grad.h"
 
 #include <algorithm>
@@ -30,6 +30,10 @@ constexpr int TM = 128, TN = 256, PANEL = 64 * 128;        // rows of a block's 
 constexpr int STAGE = 4 * PANEL, STAGES = 5, OUT = 32 * 128, OUTS = 2;      // (a warp's output buffers)
 constexpr int EPI_WARPS = 8, THREADS_G = 32 * (EPI_WARPS + 2), SMEM_Z = STAGE * STAGES + 1024, SMEM_P = SMEM_Z + EPI_WARPS * OUT * OUTS;
 constexpr size_t MOST_DZ = (size_t)2 << 30;               // bytes of dz (without remainders) that are kept at a time
+// The tensor cores truncate when they add to an accumulator.  Sums over more k blocks of 64 than these leave it every so often and are added in
+// ordinary fp32, in the other accumulator's columns (LONG: one accumulator; a segment takes 100 times its addition).  With one accumulator for
+// all of them dhead of rows whose terms have one sign was too small by 3e-5 for 8192 rows, 1.8e-3 for 300 000 and 6.5e-3 for a million.
+constexpr int SEG_Z = 128, SEG_P = 256;
 constexpr int FEW = 128;                                  // rows up to which dz comes with its rounding remainders
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -109,10 +113,29 @@ __device__ __forceinline__ uint32_t pair_idesc(int n) { return (umma_idesc(n) & 
 __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
     return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(PANEL >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void release_acc(Pair &s, int i, int lane) {
+// The i-th accumulator: which of the two, and the parity of its barriers' phase.
+template <bool LONG> __device__ __forceinline__ int which(int i) { return LONG ? 0 : i & 1; }
+template <bool LONG> __device__ __forceinline__ uint32_t phase(int i) { return (uint32_t)(LONG ? i : i >> 1) & 1u; }
+template <bool LONG> __device__ __forceinline__ void release_acc(Pair &s, int i, int lane) {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) acc_release(s.acc_empty + (i & 1));
+    if (lane == 0) acc_release(s.acc_empty + which<LONG>(i));
+}
+// sum (tensor memory, of the segments before; the first sets it) += acc, 32 columns.
+__device__ __forceinline__ void add_segment(uint32_t sum, uint32_t acc, bool first) {
+    uint32_t v[32], w[32];
+    tmem_ld32(acc, v);
+    if (!first) {
+        tmem_ld32(sum, w);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(w[e]) + __uint_as_float(v[e]));
+    }
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+                 "%28,%29,%30,%31,%32};"
+                 ::"r"(sum), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+                   "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+                   "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -121,6 +144,7 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 // ----------------------------------------------------------------------------- dz of a piece of the vocabulary
 
 // Persistent as k_head_score: row tiles vary fastest.
+template <bool LONG>
 __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ZArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ Pair s;
@@ -152,10 +176,16 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
         int n = 0, i = 0;
         bool ok = true;
         for (int t = worker; t < tiles && ok && rank == 0; t += workers, ++i) {
-            ok = all_wait(s, s.acc_empty + (i & 1), (((uint32_t)(i >> 1)) & 1u) ^ 1u);
+            ok = all_wait(s, s.acc_empty + which<LONG>(i), phase<LONG>(i) ^ 1u);
             if (!ok) break;
-            const uint32_t acc = tmem + (uint32_t)(i & 1) * 256u;
+            const uint32_t acc = tmem + which<LONG>(i) * 256u;
             for (int kb = 0; kb < a.nkb; ++kb, ++n) {
+                if (LONG && kb && kb % SEG_Z == 0) {
+                    umma2_commit_if(on, s.acc_full + which<LONG>(i));
+                    ++i;
+                    ok = all_wait(s, s.acc_empty + which<LONG>(i), phase<LONG>(i) ^ 1u);
+                    if (!ok) break;
+                }
                 const int slot = n % STAGES;
                 ok = all_wait(s, s.full + slot, ((uint32_t)(n / STAGES)) & 1u);
                 if (!ok) break;
@@ -163,10 +193,10 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                 const uint32_t a0 = smem_u32(smem + slot * STAGE), b0 = a0 + 2 * PANEL;
 #pragma unroll
                 for (int k16 = 0; k16 < 4; ++k16)
-                    umma2_if(on, acc, umma_desc(a0 + k16 * 32), umma_desc(b0 + k16 * 32), idesc, kb > 0 || k16 > 0 ? 1u : 0u);
+                    umma2_if(on, acc, umma_desc(a0 + k16 * 32), umma_desc(b0 + k16 * 32), idesc, (LONG ? kb % SEG_Z : kb) > 0 || k16 > 0 ? 1u : 0u);
                 umma2_commit_if(on, s.empty + slot);
             }
-            if (ok) umma2_commit_if(on, s.acc_full + (i & 1));
+            if (ok) umma2_commit_if(on, s.acc_full + which<LONG>(i));
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;
@@ -191,9 +221,20 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                 c = (a.g_lse ? a.g_lse[r] : 0.f) - gl;
                 if (a.g_entropy) { const float e = a.g_entropy[r]; c = fmaf(-e, a.entropy[r], c); h = -e * LN2; }
             }
-            if (ok) ok = all_wait(s, s.acc_full + (i & 1), ((uint32_t)(i >> 1)) & 1u);
-            tc_fence_after();
-            const uint32_t acc = tmem + (uint32_t)(i & 1) * 256u + ((uint32_t)(quad * 32) << 16);
+            uint32_t acc = tmem + which<LONG>(i) * 256u + ((uint32_t)(quad * 32) << 16);
+            if (LONG) {
+                for (int kb = 0;; ++i) {
+                    if (ok) ok = all_wait(s, s.acc_full + which<LONG>(i), phase<LONG>(i));
+                    tc_fence_after();
+                    for (int k = c0; k < c1 && ok; ++k) add_segment(acc + 256u + k * 32, acc + k * 32, kb == 0);
+                    release_acc<LONG>(s, i, lane);
+                    if ((kb += SEG_Z) >= a.nkb) break;
+                }
+                acc += 256u;
+            } else {
+                if (ok) ok = all_wait(s, s.acc_full + which<LONG>(i), phase<LONG>(i));
+                tc_fence_after();
+            }
             for (int k = c0; k < c1; ++k) {
                 const int at = k * 32;
                 if (n0 + at >= a.ld) break;
@@ -236,7 +277,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_z(const __grid_constant__
                     }
                 }
             }
-            release_acc(s, i, lane);
+            if (!LONG) release_acc<LONG>(s, i, lane);
         }
     }
     pair_end(tmem, warp);
@@ -284,6 +325,7 @@ struct Walk {
 // k = tokens.  All tensor copies are 64 x 64: a panel of an MN-major operand, half of a K-major one.
 // Up to 128 rows dz comes with its rounding remainders, which cost little there: dhead has twice the k blocks, which its stores outlast, and the
 // second block of a pair, whose rows would be empty, multiplies the remainders (its sums are a share of their own).
+template <bool LONG>
 __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_low,
                                                             const __grid_constant__ CUtensorMap map_x,
                                                             const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_dw,
@@ -347,13 +389,19 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                 umma2_commit_if(on, s.empty + slot);
             }
         };
-        for (int j = 0; ok && rank == 0 && walk(a, it); ++j) {
-            ok = all_wait(s, s.acc_empty + (j & 1), (((uint32_t)(j >> 1)) & 1u) ^ 1u);
-            if (!ok) break;
-            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u;
-            if (it.to_head) multiply(std::true_type{}, acc, a.k_w);
-            else multiply(std::false_type{}, acc, it.k1 - it.k0);
-            if (ok) umma2_commit_if(on, s.acc_full + (j & 1));
+        for (int j = 0; ok && rank == 0 && walk(a, it);) {
+            int left = it.to_head ? a.k_w : it.k1 - it.k0;
+            do {                                                       // (a segment; an empty share has one of no blocks)
+                ok = all_wait(s, s.acc_empty + which<LONG>(j), phase<LONG>(j) ^ 1u);
+                if (!ok) break;
+                const uint32_t acc = tmem + which<LONG>(j) * 256u;
+                const int blocks = LONG ? min(left, SEG_P) : left;
+                if (it.to_head) multiply(std::true_type{}, acc, blocks);
+                else multiply(std::false_type{}, acc, blocks);
+                if (ok) umma2_commit_if(on, s.acc_full + which<LONG>(j));
+                ++j;
+                left -= blocks;
+            } while (LONG && ok && left > 0);
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;
@@ -361,9 +409,20 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
         int stored = 0;
         bool ok = true;
         for (int j = 0; walk(a, it); ++j) {
-            if (ok) ok = all_wait(s, s.acc_full + (j & 1), ((uint32_t)(j >> 1)) & 1u, it.k1 - it.k0);
-            tc_fence_after();
-            const uint32_t acc = tmem + (uint32_t)(j & 1) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
+            uint32_t acc = tmem + which<LONG>(j) * 256u + ((uint32_t)(quad * 32) << 16) + half * half_n;
+            if (LONG) {
+                for (int k = it.k0;; ++j) {
+                    if (ok) ok = all_wait(s, s.acc_full + which<LONG>(j), phase<LONG>(j), SEG_P);
+                    tc_fence_after();
+                    for (int c = 0; c < half_n && ok; c += 32) add_segment(acc + 256u + c, acc + c, k == it.k0);
+                    release_acc<LONG>(s, j, lane);
+                    if ((k += SEG_P) >= it.k1) break;
+                }
+                acc += 256u;
+            } else {
+                if (ok) ok = all_wait(s, s.acc_full + which<LONG>(j), phase<LONG>(j), it.k1 - it.k0);
+                tc_fence_after();
+            }
             const int plane = !it.to_head && a.planes == 2 ? rank : 0;
             const int m = it.m0 + (plane ? 0 : rank * TM) + quad * 32, n0 = it.n0 + half * half_n, last = it.to_head ? a.width : a.rows;
             const bool sums = !it.to_head && a.part;
@@ -423,7 +482,7 @@ __global__ void __launch_bounds__(THREADS_G, 1) k_head_prod(const __grid_constan
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
             }
-            release_acc(s, j, lane);
+            if (!LONG) release_acc<LONG>(s, j, lane);
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
@@ -512,8 +571,10 @@ static cudaError_t opt_in() {              // (per device)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
-    e = cudaFuncSetAttribute(k_head_z, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_Z);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_prod, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_P);
+    e = cudaFuncSetAttribute(k_head_z<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_Z);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_z<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_Z);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_prod<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_P);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_head_prod<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_P);
     if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
     return e;
 }
@@ -580,7 +641,8 @@ static cudaError_t products(const Args &a, const Plan &p, EncodeFn encode, int p
     q.part = part; q.dhead = dhead; q.ld_dhead = a.ld_dhead;
     q.direct = q.k_w >= 4 && a.d % 16 == 0 && (((uintptr_t)dhead | (uintptr_t)(a.ld_dhead * 2)) & 31) == 0;
     Launch l((unsigned)std::min<int64_t>(workers, (int64_t)q.n_h + q.n_w) * 2, THREADS_G, SMEM_P, st, true, true);
-    cudaError_t e = cudaLaunchKernelEx(&l.c, k_head_prod, mz, ml, mx, mw, mdw, mdx, q);
+    const bool segments = (dhead && q.k_w > SEG_P) || (a.dhidden && q.per > SEG_P);
+    cudaError_t e = segments ? cudaLaunchKernelEx(&l.c, k_head_prod<true>, mz, ml, mx, mw, mdw, mdx, q) : cudaLaunchKernelEx(&l.c, k_head_prod<false>, mz, ml, mx, mw, mdw, mdx, q);
     if (e != cudaSuccess || !part || piece < p.pieces - 1) return e;
     Launch s((unsigned)(((int64_t)a.rows * (a.d >> 3) + 63) / 64), 256, 0, st, false, true);
     return cudaLaunchKernelEx(&s.c, k_head_sum, (const float *)part, p.splits * p.planes, a.rows, a.d, p.dp, reinterpret_cast<bf16 *>(a.dhidden), a.ld_dhidden);
@@ -621,7 +683,7 @@ cudaError_t run(const Args &a, void *scratch, int n_sm, bool after, cudaStream_t
             return cudaSuccess;
         }
         Launch l((unsigned)std::min<int64_t>(workers, (int64_t)z.mt * z.nt) * 2, THREADS_G, SMEM_Z, st, true, after || i);
-        e = cudaLaunchKernelEx(&l.c, k_head_z, ma, mb, z);
+        e = z.nkb > SEG_Z ? cudaLaunchKernelEx(&l.c, k_head_z<true>, ma, mb, z) : cudaLaunchKernelEx(&l.c, k_head_z<false>, ma, mb, z);
         if (e == cudaSuccess) e = products(a, p, encode, i, at.dz, at.low, at.part, workers, st, no_maps);
         if (e != cudaSuccess || *no_maps) return e;
     }
