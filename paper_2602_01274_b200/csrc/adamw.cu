@@ -476,14 +476,14 @@ struct StateItem {
     const float *scales;
     float *om, *ov;
     int64_t numel;
-    uint32_t first, roots;
+    uint32_t first, pad;
 };
 template <int CAP> struct StateTable {
     int32_t n, pad;
     StateItem t[CAP];
 };
 
-template <bool VEC> __device__ __forceinline__ void read_states(const StateItem &t, int64_t base, int lane) {
+template <bool VEC, Kind HELD> __device__ __forceinline__ void read_states(const StateItem &t, int64_t base, int lane) {
     float x[8];
     const float2 s = *reinterpret_cast<const float2 *>(t.scales + (base >> 8) * 2);
     if (t.om) {
@@ -491,18 +491,14 @@ template <bool VEC> __device__ __forceinline__ void read_states(const StateItem 
         store<VEC>(t.om, base, lane, t.numel, x);
     }
     if (t.ov) {
-        const uint2 c = load_codes<VEC>(t.v, base, lane, t.numel);
-        if (t.roots) {
-            values<R>(c, s.y, x);
+        values<HELD>(load_codes<VEC>(t.v, base, lane, t.numel), s.y, x);
+        if (HELD == R)
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = __fmul_rn(x[k], x[k]);
-        } else {
-            values<V>(c, s.y, x);
-        }
         store<VEC>(t.ov, base, lane, t.numel, x);
     }
 }
-template <int CAP>
+template <int CAP, Kind HELD>
 __global__ void __launch_bounds__(THREADS_W) k_states(const __grid_constant__ StateTable<CAP> tab) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const StateItem t = tab.t[tensor_of(tab, blockIdx.x)];
@@ -510,33 +506,42 @@ __global__ void __launch_bounds__(THREADS_W) k_states(const __grid_constant__ St
     const int64_t start = (int64_t)(blockIdx.x - t.first) * CHUNK + warp * 256;
 #pragma unroll 1
     for (int64_t base = start; base < start + CHUNK && base < t.numel; base += PASS) {
-        if (vec && base + 256 <= t.numel) read_states<true>(t, base, lane);
-        else read_states<false>(t, base, lane);
+        if (vec && base + 256 <= t.numel) read_states<true, HELD>(t, base, lane);
+        else read_states<false, HELD>(t, base, lane);
     }
 }
-template <int CAP>
-static cudaError_t launch_states(const pacer_adamw_tensor *tbl, int from, int to, float *const *om, float *const *ov, cudaStream_t st) {
+// The tensors at[0 .. n).
+template <int CAP, Kind HELD>
+static cudaError_t launch_states(const pacer_adamw_tensor *tbl, const int *at, int n, float *const *om, float *const *ov, cudaStream_t st) {
     StateTable<CAP> tab;
-    tab.n = 0;
+    tab.n = n;
     uint64_t chunks = 0;
-    for (int i = from; i < to; ++i) {
+    for (int k = 0; k < n; ++k) {
+        const int i = at[k];
         const pacer_adamw_tensor &t = tbl[i];
-        tab.t[tab.n++] = {(const uint8_t *)t.exp_avg, (const uint8_t *)t.exp_avg_sq, t.scales, om ? om[i] : nullptr, ov ? ov[i] : nullptr, t.numel, (uint32_t)chunks, t.v_code == PACER_V_ROOT};
+        tab.t[k] = {(const uint8_t *)t.exp_avg, (const uint8_t *)t.exp_avg_sq, t.scales, om ? om[i] : nullptr, ov ? ov[i] : nullptr, t.numel, (uint32_t)chunks, 0};
         chunks += (uint64_t)(t.numel + CHUNK - 1) / CHUNK;
     }
-    if (!chunks) return cudaSuccess;
     if (chunks > 0x7fffffffu) return cudaErrorInvalidValue;
-    k_states<CAP><<<(unsigned)chunks, THREADS_W, 0, st>>>(tab);
+    k_states<CAP, HELD><<<(unsigned)chunks, THREADS_W, 0, st>>>(tab);
     return cudaGetLastError();
 }
-cudaError_t states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, cudaStream_t st) {
-    for (int i = 0; i < n; i += MOST) {
-        const int to = std::min(n, i + MOST), k = to - i;
-        const cudaError_t e = k <= 16 ? launch_states<16>(tbl, i, to, exp_avg, exp_avg_sq, st) : k <= 96 ? launch_states<96>(tbl, i, to, exp_avg, exp_avg_sq, st)
-                                                                                             : launch_states<MOST>(tbl, i, to, exp_avg, exp_avg_sq, st);
-        if (e != cudaSuccess) return e;
+template <Kind HELD> static cudaError_t states_held(const pacer_adamw_tensor *tbl, int n, int code, float *const *om, float *const *ov, cudaStream_t st) {
+    int at[MOST], k = 0;
+    for (int i = 0; i <= n; ++i) {
+        if (k == MOST || (i == n && k)) {
+            const cudaError_t e = k <= 16 ? launch_states<16, HELD>(tbl, at, k, om, ov, st) : k <= 96 ? launch_states<96, HELD>(tbl, at, k, om, ov, st)
+                                                                                                 : launch_states<MOST, HELD>(tbl, at, k, om, ov, st);
+            if (e != cudaSuccess) return e;
+            k = 0;
+        }
+        if (i < n && tbl[i].numel && tbl[i].v_code == code) at[k++] = i;
     }
     return cudaSuccess;
+}
+cudaError_t states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, cudaStream_t st) {
+    const cudaError_t e = states_held<V>(tbl, n, PACER_V_SQUARE, exp_avg, exp_avg_sq, st);
+    return e != cudaSuccess ? e : states_held<R>(tbl, n, PACER_V_ROOT, exp_avg, exp_avg_sq, st);
 }
 
 // ----------------------------------------------------------------------------- the gradients' norm
