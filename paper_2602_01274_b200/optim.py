@@ -114,6 +114,8 @@ class AdamW(torch.optim.Optimizer):
                     continue
                 if p.grad.is_sparse:
                     raise RuntimeError("AdamW: no sparse gradients")
+                if not p.is_contiguous():                               # (a parameter may get other strides where it lies)
+                    raise RuntimeError("AdamW: params contiguous, as they were given")
                 s = self._state_of(p, fresh)
                 buckets.setdefault((gi, p.device, id(s["step"]) if self.capturable else s["step"], "scales" in s), []).append(p)
         if self.capturable:

@@ -177,3 +177,19 @@ def test_rounding_at_random_unless_nearest_is_asked_for():
         means[name] = float(v.double().mean())
     bound = 6 * (500 / n) ** 0.5 / 16
     assert abs(means["8bit"] / means["f32"] - 1) < bound < abs(means["nearest"] / means["f32"] - 1)
+
+
+def test_other_strides_in_place():
+    """A parameter that was transposed where it lies keeps address and size: its elements are no longer in the order of its moments."""
+    from paper_2602_01274_b200 import optim
+    p = torch.nn.Parameter(torch.randn(64, 64, generator=gen(1), device=DEV))
+    o = optim.AdamW([p], lr=1e-3)
+    p.grad = torch.ones_like(p)
+    o.step()
+    kept = p.detach().clone()
+    p.grad = None
+    p.data = p.data.t()
+    p.grad = torch.ones(64, 64, device=DEV)
+    with pytest.raises(RuntimeError, match="contiguous"):
+        o.step()
+    assert torch.equal(p.detach().t(), kept) and o.state[p]["step"] == 1
