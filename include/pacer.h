@@ -397,7 +397,8 @@ int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidden, const vo
 /* Softmax cross entropy of given tokens straight from hidden rows and head, without keeping the logits, and its gradients in the same
  * call: loss[r] = lse - z[tokens[r]] (f32 [rows]; 0 where the token names nothing; may be NULL), dhidden and dhead (each may be NULL)
  * of sum_r weight[r] loss[r].  Arguments otherwise as above. 
- * Where dz of the whole vocabulary fits 2 GB the logits are computed once, else twice.  Computed once, each share of a row's mass is kept in 11
+ * Where dz of the whole vocabulary, 2 rows vocab bytes in the scratch (up to 128 rows 4), fits 2 GB the logits are computed once, else
+ * twice and dz in pieces of the vocabulary of at most that size.  Computed once, each share of a row's mass is kept in 11
  * bits until the row's sum is known, then rounded to bf16 (and remainder) as above; a share below 2^-62 of the largest of some 128 tokens next to
  * it counts as 0.  1 - p of a row's token, and its loss where it leads, are then right relative to themselves; computed twice, as above. */
 size_t pacer_head_nll_grad_scratch_bytes(int rows, int vocab, int d);
@@ -451,7 +452,7 @@ int pacer_adamw(const pacer_adamw_tensor *tbl, int n, const pacer_adamw_cfg *cfg
 int pacer_adamw_states(const pacer_adamw_tensor *tbl, int n, float *const *exp_avg, float *const *exp_avg_sq, void *cuda_stream);
 
 /* norm (device f32) = sqrt of the sum of all squares of n gradients (host array tbl, read before the call returns), summed in 64 bits in a
- * fixed order.  scratch: device, 8-byte aligned, at least pacer_grad_norm_scratch_bytes(n) bytes. */
+ * fixed order; infinite where a gradient is infinite or NaN, or the norm above f32's range; 0 below 2^-100.  scratch: device, 8-byte aligned, at least pacer_grad_norm_scratch_bytes(n) bytes. */
 typedef struct {
     const void *grad;
     int64_t numel;

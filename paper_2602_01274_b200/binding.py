@@ -620,8 +620,8 @@ def pacer_head_logprobs_backward(hidden, head, tokens, logp, lse, entropy, grad_
 
 
 def pacer_head_nll_grad(hidden, head, tokens, weight, bias_ids=None, bias: float = 0.0, grads=(True, True), out=None):
-    """Softmax cross entropy of int32 tokens [rows] under the rows hidden @ head.T without keeping those logits, and in the same call the
-    gradients of sum(weight * loss): (loss f32 [rows], dhidden bf16 [rows][d], dhead bf16 [vocab][d]).  A token outside the vocabulary
+    """Softmax cross entropy of int32 tokens [rows] under the rows hidden @ head.T without keeping those logits (the call's scratch has 16 bits for each,
+    32 up to 128 rows, 2 GB at most), and in the same call the gradients of sum(weight * loss): (loss f32 [rows], dhidden bf16 [rows][d], dhead bf16 [vocab][d]).  A token outside the vocabulary
     (-1, say) has loss 0 and passes no gradient.  bias_ids, bias: as pacer_head_logprobs; grads, out: as
     pacer_head_logprobs_backward."""
     h, w = _head(hidden, head)
@@ -749,7 +749,7 @@ def _gradients(grads, device):
 
 def pacer_grad_norm(grads) -> torch.Tensor:
     """The global 2-norm of a list of gradients (f32, bf16 or f16, contiguous, on one GPU) as an f32 scalar on the device, summed in 64
-    bits.  Nothing is read back."""
+    bits; infinite where a gradient is infinite or NaN.  Nothing is read back."""
     grads = list(grads)
     if not grads:
         raise AssertionError("grads: at least one")

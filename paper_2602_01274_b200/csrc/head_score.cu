@@ -1,5 +1,6 @@
 // LM head fused with the scoring of given tokens: z = hidden head^T, and of each row of z only its log-sum-exp, its entropy and
-// the logit of one token.  The logits are never written: [rows][vocab] f32 would be 262 MB for 2048 rows of 32 000.
+// the logit of one token.  The logits are never written: [rows][vocab] f32 would be 262 MB for 2048 rows of 32 000.  (For the loss's gradients,
+// KEEP below, each share of a half tile's largest is, in 16 bits.)
 //
 // Many rows are bound by the tensor cores (2 rows vocab d operations), few by reading the head once.  One kernel does both: tiles
 // of 128 rows (256 by a pair of blocks) x up to 256 tokens on tcgen05, operands by tensor copies in the 128-byte swizzle, 192 KB of
