@@ -365,7 +365,7 @@ int pacer_distill_backward(const void *logits, int dtype, int64_t ld, int rows, 
  * row to row; both addresses 16-byte aligned, d and both strides multiples of 8, d <= 65536; rows <= 2^20, vocab <= 2^21.  Plain
  * bf16 products with fp32 sums on tcgen05.  tokens: device int32 [rows] or NULL (then logp too); bias_ids: device int32
  * [rows] or NULL, an id outside the vocabulary adds nothing; a bias of -infinity or f32's lowest value takes the token out of the
- * row.  logp, entropy, lse: device f32 [rows], each may be NULL.
+ * row (refused where it is the only one).  logp, entropy, lse: device f32 [rows], each may be NULL.
  * scratch: device, 256-byte aligned, at least pacer_head_logprobs_scratch_bytes(rows, vocab) bytes, in use until the call's kernels
  * have run (two calls that may overlap need one each).  Inputs must be finite: infinities and NaN make results NaN or infinite;
  * so does, for its rows, a wait inside the kernel that ran out.  Enqueues two kernels; may be captured into a graph (not as the

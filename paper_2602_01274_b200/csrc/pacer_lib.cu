@@ -1080,6 +1080,9 @@ extern "C" size_t pacer_head_logprobs_scratch_bytes(int rows, int vocab) {
     return hs::scratch_bytes(rows, vocab);
 }
 
+// A bias that takes the only token out of its row.
+static bool empties(int vocab, const int32_t *bias_ids, float bias) { return vocab == 1 && bias_ids && bias < -1e29f; }
+
 extern "C" int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const void *head, int64_t ld_head, int rows, int vocab, int d,
                                    const int32_t *tokens, const int32_t *bias_ids, float bias, float *logp, float *entropy, float *lse,
                                    void *scratch, size_t scratch_bytes, void *cuda_stream) {
@@ -1092,6 +1095,7 @@ extern "C" int pacer_head_logprobs(const void *hidden, int64_t ld_hidden, const 
     REFUSE_IF(!hidden || !head || !scratch, "hidden, head or scratch is null");
     REFUSE_IF(((uintptr_t)hidden | (uintptr_t)head) & 15 || (uintptr_t)scratch & 255, "misaligned pointer");
     REFUSE_IF(logp && !tokens, "logp without tokens");
+    REFUSE_IF(empties(vocab, bias_ids, bias), "a bias that leaves a row no token");
     if (scratch_bytes < hs::scratch_bytes(rows, vocab)) return fail(nullptr, PACER_ENOMEM, "pacer_head_logprobs: scratch too small");
     bool no_maps = false;
     CK(hs::run({hidden, head, ld_hidden, ld_head, rows, vocab, d, tokens, bias_ids, bias, logp, entropy, lse}, scratch, sm_count_or_default(),
@@ -1151,6 +1155,7 @@ extern "C" int pacer_head_logprobs_backward(const void *hidden, int64_t ld_hidde
     REFUSE_IF(!g_logp && !g_entropy && !g_lse, "no gradient comes in");
     REFUSE_IF(g_logp && (!tokens || !logp), "g_logp without tokens or logp");
     REFUSE_IF(g_entropy && !entropy, "g_entropy without entropy");
+    REFUSE_IF(empties(vocab, bias_ids, bias), "a bias that leaves a row no token");
     const int n_sm = sm_count_or_default();
     if (scratch_bytes < hg::scratch_bytes(rows, vocab, d, n_sm)) return fail(nullptr, PACER_ENOMEM, "pacer_head_logprobs_backward: scratch too small");
     bool no_maps = false;
@@ -1178,6 +1183,7 @@ extern "C" int pacer_head_nll_grad(const void *hidden, int64_t ld_hidden, const 
     REFUSE_IF(!scratch || (uintptr_t)scratch & 255, "scratch is null or misaligned");
     REFUSE_IF(!tokens, "tokens is null");
     REFUSE_IF((dhidden || dhead) && !weight, "a gradient without weight");
+    REFUSE_IF(empties(vocab, bias_ids, bias), "a bias that leaves a row no token");
     const int n_sm = sm_count_or_default();
     if (scratch_bytes < hg::nll_scratch_bytes(rows, vocab, d, n_sm)) return fail(nullptr, PACER_ENOMEM, "pacer_head_nll_grad: scratch too small");
     bool no_maps = false;
