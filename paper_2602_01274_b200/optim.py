@@ -132,8 +132,9 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p]["step"] = copies.setdefault(id(t), t.clone())
         return buckets
 
-    def _table(self, key, ps, st, coded):
+    def _table(self, key, ps, coded):
         """The tensors that a call takes, kept between steps while the state holds these very ones (a program may drop or exchange them)."""
+        st = [self.state[p] for p in ps]
         copies = [p if "master" in s else None for p, s in zip(ps, st)]
         now = ([s.get("master", p) for p, s in zip(ps, st)], copies if any(c is not None for c in copies) else None, [s["exp_avg"] for s in st],
                [s["exp_avg_sq"] for s in st], [s["scales"] for s in st] if coded else None)
@@ -154,6 +155,8 @@ class AdamW(torch.optim.Optimizer):
         if not self.capturable and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("AdamW: captured steps need capturable=True (else every replay has the count and rate of now)")
         buckets = self._buckets()
+        # (before anything is counted: a state that does not fit is refused)
+        tables = [self._table((gi, device, coded, *map(id, ps)), ps, coded) for (gi, device, _, coded), ps in buckets.items()]
         grads = {p: p.grad.contiguous() for ps in buckets.values() for p in ps}
         norm = None
         if self.max_norm > 0 and grads:
@@ -166,8 +169,8 @@ class AdamW(torch.optim.Optimizer):
         else:
             for p in grads:
                 self.state[p]["step"] += 1
-        for (gi, device, _, coded), ps in buckets.items():
-            group, st = self.param_groups[gi], [self.state[p] for p in ps]
-            binding.pacer_adamw(self._table((gi, device, coded, *map(id, ps)), ps, st, coded), [grads[p] for p in ps], st[0]["step"], group["lr"],
-                                group["betas"], group["eps"], group["weight_decay"], self.seed, norm, self.max_norm)
+        for ((gi, *_), ps), table in zip(buckets.items(), tables):
+            group = self.param_groups[gi]
+            binding.pacer_adamw(table, [grads[p] for p in ps], self.state[ps[0]]["step"], group["lr"], group["betas"], group["eps"],
+                                group["weight_decay"], self.seed, norm, self.max_norm)
         return loss

@@ -193,3 +193,19 @@ def test_other_strides_in_place():
     with pytest.raises(RuntimeError, match="contiguous"):
         o.step()
     assert torch.equal(p.detach().t(), kept) and o.state[p]["step"] == 1
+
+
+def test_a_refused_step_is_not_counted():
+    """A state that does not fit stops the step before any parameter of any group has moved or been counted."""
+    from paper_2602_01274_b200 import optim
+    a = params(torch.float32)
+    o = optim.AdamW([dict(params=a[:1]), dict(params=a[1:], lr=1e-4)], lr=1e-3)
+    run(o, a, range(2))
+    kept, m = [p.detach().clone() for p in a], o.state[a[2]]["exp_avg"]
+    o.state[a[2]]["exp_avg"] = m.double()
+    with pytest.raises(AssertionError, match="exp_avg"):
+        o.step()
+    assert [o.state[p]["step"] for p in a] == [2, 2, 2] and all(torch.equal(p.detach(), x) for p, x in zip(a, kept))
+    o.state[a[2]]["exp_avg"] = m
+    o.step()
+    assert [o.state[p]["step"] for p in a] == [3, 3, 3] and not any(torch.equal(p.detach(), x) for p, x in zip(a, kept))
